@@ -516,6 +516,105 @@ int dsv_adamw_step_grouped(const dsv_plan* plan, dsv_dtype dtype, int32_t n_proj
 int dsv_gemm_config(const dsv_plan* plan, dsv_dtype dtype, int32_t K, int32_t N, int32_t pass,
                     int32_t out[6]);
 
+/*
+ * Attention of a mixed batch (softmax(scale Q K^T) V, causal, grouped heads): the
+ * operator between the q/k/v and the o projections.  One call serves whole
+ * prompts, chunks behind a cached prefix, single decode tokens over long caches
+ * and fine-tuning samples; the backward serves the fine-tuning samples.
+ *
+ * For query i of a sequence (0 <= i < q_len), query head h and key head
+ * h / (heads_q / heads_kv), over the keys j <= i + k_len - q_len (the last query
+ * sees the last key):
+ *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
+ * A query that sees no key (i < q_len - k_len, or k_len = 0) has o = 0 and
+ * lse = -infinity, and no part in any gradient.  Keys that no query of a sequence
+ * sees are never part of a sum, whatever they hold.  Backward, with
+ * p_j = exp(s_j - lse) and D = do . o:
+ *     dv_j += p_j do      ds_j = scale p_j (do . v_j - D)
+ *     dq = sum_j ds_j k_j     dk_j += ds_j q     (sums over the key head's query heads)
+ *
+ * Scores, softmax statistics and sums are fp32 in both types; in bf16 mode the
+ * products run on bf16 operands, for which p and ds are rounded to bf16 once, and
+ * every output is rounded once.  No atomics: repeated calls give the same bits.
+ */
+
+/* One sequence: query rows [q_start, q_start + q_len) of Q and O, key rows
+ * [k_start, k_start + k_len) of K and V; is_train = 1: the backward computes its
+ * gradients. */
+typedef struct {
+  int32_t q_start;
+  int32_t q_len;
+  int32_t k_start;
+  int32_t k_len;
+  int32_t is_train;
+} dsv_attn_seq;
+
+typedef struct dsv_attn_plan dsv_attn_plan;
+
+/*
+ * dsv_attn_build -- validate a batch's sequences and pack the work lists of the
+ * attention calls (one plan serves every layer of the batch).
+ * seqs[n_seqs], in any order: query ranges lie in [0, n_q) and do not overlap
+ * (rows in no range are neither read nor written); key ranges lie in [0, n_kv) and
+ * may overlap (a shared prefix).  Zero lengths are allowed.  1 <= heads_kv,
+ * heads_q a multiple of heads_kv and at most 1024, head_dim 64 or 128.
+ * Gradient tensors hold the fine-tuning samples' rows alone, in ascending order of
+ * q_start ("compact order", that of the linear layers): sample after sample, q_len
+ * rows each in dO and dQ, k_len rows each in dK and dV.
+ * Returns the plan, on the host only, and the bytes of its device blob; nothing
+ * runs on the device.  Errors: DSV_ERR_ARG (null, negative count),
+ * DSV_ERR_RANGE (heads, head_dim, flag), DSV_ERR_LAYOUT (a range outside its
+ * rows, overlapping query ranges), DSV_ERR_SIZE (more than 2^31 - 1 work items).
+ */
+int dsv_attn_build(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv,
+                   int32_t heads_q, int32_t heads_kv, int32_t head_dim, size_t* meta_bytes,
+                   dsv_attn_plan** out_plan);
+/* Copies the blob to d_meta (256-byte aligned, at least *meta_bytes bytes),
+ * asynchronously on hip_stream; rules and errors of dsv_plan_upload. */
+int dsv_attn_upload(dsv_attn_plan* plan, void* d_meta, size_t meta_bytes, void* hip_stream);
+/* Rows of the gradient tensors: out[0] of dO and dQ, out[1] of dK and dV. */
+int dsv_attn_train_rows(const dsv_attn_plan* plan, int64_t out[2]);
+/* Releases the plan (NULL is a no-op); waits for its upload like dsv_plan_free. */
+void dsv_attn_free(dsv_attn_plan* plan);
+
+/* A tensor [rows][heads][head_dim]: element (t, h, c) at ptr[t * row + h * head + c].
+ * Strides in elements, multiples of 8, at least head_dim and at most 2^40; 0 stands
+ * for the dense one (row: heads * head_dim, head: head_dim).  ptr is 16-byte
+ * aligned.  So q, k and v may be columns of one product's rows, and a cache may be
+ * [row][head][d] or [head][row][d].  The vectors of an output must not overlap. */
+typedef struct {
+  void* ptr;
+  int64_t row;
+  int64_t head;
+} dsv_attn_view;
+
+/* Device workspace that dsv_attn_fwd and dsv_attn_bwd need for this plan (one
+ * buffer may serve both; 256-byte aligned). */
+int dsv_attn_workspace(const dsv_attn_plan* plan, dsv_dtype dtype, size_t* bytes);
+
+/*
+ * dsv_attn_fwd -- O, and lse [heads_q][n_q] (fp32; NULL: not written, a backward
+ * needs it), of every sequence of the plan.  Q and O have n_q rows of heads_q
+ * heads, K and V n_kv rows of heads_kv heads.  scale must be finite.
+ * Errors: DSV_ERR_ARG (null or misaligned pointer, plan not on the device),
+ * DSV_ERR_RANGE (dtype, scale), DSV_ERR_SIZE (strides, overlapping outputs,
+ * workspace).
+ */
+int dsv_attn_fwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const dsv_attn_view* Q,
+                 const dsv_attn_view* K, const dsv_attn_view* V, const dsv_attn_view* O, float* lse,
+                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * dsv_attn_bwd -- dQ, dK and dV of the fine-tuning samples (compact rows) from
+ * the forward's Q, K, V, O and lse and the upstream gradient dO (compact rows).
+ * Where samples share key rows, dK and dV hold each sample's own part.  Without
+ * fine-tuning samples the call is a no-op.  Errors as dsv_attn_fwd.
+ */
+int dsv_attn_bwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const dsv_attn_view* Q,
+                 const dsv_attn_view* K, const dsv_attn_view* V, const dsv_attn_view* O, const float* lse,
+                 const dsv_attn_view* dO, const dsv_attn_view* dQ, const dsv_attn_view* dK,
+                 const dsv_attn_view* dV, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static description of a status code. */
 const char* dsv_status_string(int status);
 

@@ -13,6 +13,7 @@ first.  It is for CPU-only runs of the host-side tests.
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -21,7 +22,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdsv.so")
-SOURCES = ["plan.cpp", "api.cpp", "gemm_bf16.hip", "gemm_part.hip", "kernels_bf16.hip", "kernels_f32.hip", "optim.hip", "dropout.hip", "scratch.hip"]
+SOURCES = ["plan.cpp", "attn_plan.cpp", "api.cpp", "gemm_bf16.hip", "gemm_part.hip", "kernels_bf16.hip", "kernels_f32.hip",
+           "optim.hip", "dropout.hip", "scratch.hip", "attn.hip", "attn_f32.hip"]
 HOST_SOURCES = [s for s in SOURCES if s.endswith(".cpp")]
 ASAN_DIR = os.path.join(PKG, "_build", "host_asan")
 ASAN_LIB = os.path.join(ASAN_DIR, "libdsv.so")
@@ -40,20 +42,23 @@ FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source into libdsv.so (always recompiles)."""
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
+    """Compile every source into libdsv.so (always recompiles; the sources side by side)."""
+    obj_dir = os.path.join(PKG, "_build", "obj%d" % os.getpid())
+    os.makedirs(obj_dir, exist_ok=True)
+    objs = [os.path.join(obj_dir, s + ".o") for s in SOURCES]
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + ["-o", tmp] + srcs
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, cwd=PKG, capture_output=True, text=True)
-    out = "\n".join(l for l in (res.stdout + res.stderr).splitlines()
-                    if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
+    flags = [f for f in FLAGS if f != "-shared"]
+    try:
+        with ThreadPoolExecutor(max_workers=min(len(objs), 8)) as ex:
+            outs = list(ex.map(lambda so: _run([HIPCC] + flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+                               zip(SOURCES, objs)))
+        outs.append(_run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs, verbose))
+        os.replace(tmp, LIB)
+    finally:
+        shutil.rmtree(obj_dir, ignore_errors=True)
+    out = "\n".join(o for o in outs if o.strip())
+    if verbose and out:
         print(out, flush=True)
-    os.replace(tmp, LIB)
     return LIB
 
 

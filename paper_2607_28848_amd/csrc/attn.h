@@ -1,0 +1,40 @@
+// attn.h -- arguments and host launchers of the attention kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace dsv {
+
+// A tensor [rows][heads][D] with its strides in elements.
+struct AttnView {
+  void* ptr;
+  int64_t row, head;
+};
+
+struct AttnArgs {
+  const int32_t* seqs;   // sequence descriptors (attn_plan.h)
+  const int32_t* items;  // the launch's work items
+  int32_t n_items;
+  int32_t hq, hkv, group, d;
+  int32_t n_q;           // row length of lse ([hq][n_q])
+  int64_t train_q;       // row length of delta ([hq][train_q])
+  float scale;           // of the scores
+  AttnView Q, K, V, O, dO, dQ, dK, dV;
+  float* lse;            // nullptr: not written (forward)
+  float* delta;          // do . o of the compact rows
+  // split form
+  const int32_t* split_keys;
+  const int32_t* join_items;
+  int32_t n_join;
+  float* part_o;         // [piece][hkv][kAttnPackRows][D], sums of exp(s - m) v
+  float* part_ml;        // [piece][hkv][2][kAttnPackRows]: m, sum of exp(s - m)
+};
+
+// fp32 mode: tiles of kAttnF32Rows.
+hipError_t launch_attn_f32_fwd(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s);  // dQ, and delta for the next launch
+hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s);  // dK, dV
+
+}  // namespace dsv

@@ -1,0 +1,730 @@
+// attn.hip -- CDNA4 (gfx950) attention of a mixed batch in bf16, and the C entry points.
+//
+//   attn_fwd    128 queries of one head against the keys they see, one pass with the running maximum
+//               and sum of the softmax.
+//   attn_split  the (query, head) pairs of a key head of a sequence of few queries (decode) against
+//               one piece of its keys; attn_join adds the pieces.
+//   attn_dq     dQ of 128 queries (and do . o); attn_dk: dK and dV of 128 keys.
+//
+// Products are v_mfma_f32_32x32x16_bf16: lane l holds A[l % 32][8 (l / 32) + e], B[8 (l / 32) + e][l % 32]
+// (e < 8) and C[8 (v / 4) + 4 (l / 32) + v % 4][l % 32] (v < 16).  The scores are computed with the
+// index that the second product sums over as rows, so a lane holds 16 of them for its own column, and
+// values 8 t .. 8 t + 7, rounded to bf16, are the second product's operand as they are: its contraction
+// slot (l / 32, e) stands for row 16 t + 8 (e / 4) + 4 (l / 32) + e % 4, and the other operand is read in that
+// order (two transposing LDS reads of four rows each).  No value crosses lanes but for a query's maximum and
+// sum, which two lanes share.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "attn.h"
+#include "attn_plan.h"
+#include "device_common.h"
+
+namespace dsv {
+namespace {
+
+extern "C" __device__ void llvm_amdgcn_raw_buffer_load_lds_a(i32x4 rsrc, lds_u32* lds, int size, int voffset,
+                                                             int soffset, int offset,
+                                                             int aux) __asm("llvm.amdgcn.raw.buffer.load.lds");
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Seq {
+  int q0, ql, k0, kl, cq, ck;
+  __device__ __forceinline__ Seq(const AttnArgs& a, int i) {
+    const int32_t* w = a.seqs + (int64_t)i * kAttnSeqWords;
+    q0 = w[0], ql = w[1], k0 = w[2], kl = w[3], cq = w[4], ck = w[5];
+  }
+};
+
+// Workgroup -> (item, query head): a key head's query heads are hkv apart, so that they land on one XCD
+// (ids go round the 8 XCDs) when the key heads are 8, and share K and V in its L2.
+__device__ __forceinline__ int head_of(const AttnArgs& a, int x) { return (x % a.hkv) * a.group + x / a.hkv; }
+
+// LDS image of staged rows (D bf16 each): 16-byte chunk c of row r sits in slot c ^ swz(r).  Eight
+// consecutive rows put one chunk in eight different bank groups (fragment reads), four consecutive rows
+// put a pair of chunks in four (transposing reads).
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+  return ((r & 3) << 1) | ((r >> 2) & 1) | (D == 128 ? r & 8 : 0);
+}
+
+// Descriptor over rows [r0, r_end) of a head (reads past them return zeros); rows are at most 64 at a
+// time and at most 2^23 elements apart, so offsets fit in 31 bits.
+__device__ __forceinline__ i32x4 rows_rsrc(const AttnView& t, int64_t row, int h, int n, int d) {
+  const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const uint16_t*>(t.ptr) + row * t.row + h * t.head);
+  const int64_t range = n > 0 ? ((int64_t)(n - 1) * t.row + d) * 2 : 0;
+  i32x4 r;
+  r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+  r.y = __builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+  r.z = __builtin_amdgcn_readfirstlane((int)range);
+  r.w = 0x00020000;
+  return r;
+}
+
+// Rows [0, ROWS) of the descriptor into LDS, the work shared by NW waves.
+template <int D, int ROWS, int NW>
+__device__ __forceinline__ void stage(const i32x4& rs, int row_bytes, char* lds, int wave) {
+  constexpr int RB = 2 * D, RPL = 1024 / RB, CH = RB / 16;  // row bytes, rows a load, chunks a row
+  constexpr int N = ROWS / RPL / NW;
+  static_assert(N * RPL * NW == ROWS, "rows");
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int q = wave * N + i;
+    const int r = q * RPL + lane / CH;
+    const int c = (lane % CH) ^ swz<D>(r);
+    llvm_amdgcn_raw_buffer_load_lds_a(rs, (lds_u32*)(lds + q * 1024), 16, r * row_bytes + 16 * c, 0, 0, 0);
+  }
+}
+
+// Fragment of rows 32 u ..: lane's row 32 u + l % 32, its 8 values of step s.
+template <int D>
+__device__ __forceinline__ bf16x8 frag(const char* lds, int u, int s) {
+  const int lane = threadIdx.x & 63, r = 32 * u + (lane & 31);
+  return as_bf(*reinterpret_cast<const u32x4*>(lds + r * 2 * D + 16 * ((2 * s + (lane >> 5)) ^ swz<D>(r))));
+}
+
+// Transposed fragment: lane's column 32 t + l % 32 of rows 16 w + 4 (l / 32) + {0..3} and 8 further on.
+template <int D>
+__device__ __forceinline__ bf16x8 frag_t(const char* lds, int w, int t) {
+  const int lane = threadIdx.x & 63, lam = lane & 15;
+  const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lam & 3) >> 1);
+  u32x4 v;
+#pragma unroll
+  for (int hh = 0; hh < 2; ++hh) {
+    const int r = 16 * w + 8 * hh + 4 * (lane >> 5) + (lam >> 2);
+    const char* p = lds + r * 2 * D + 16 * (c ^ swz<D>(r)) + 8 * (lam & 1);
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    v[2 * hh] = (uint32_t)(uint16_t)x[0] | ((uint32_t)(uint16_t)x[1] << 16);
+    v[2 * hh + 1] = (uint32_t)(uint16_t)x[2] | ((uint32_t)(uint16_t)x[3] << 16);
+  }
+  return as_bf(v);
+}
+
+// A lane's fragments of its own row (zeros where it does not exist).
+template <int D>
+__device__ __forceinline__ void row_frags(const AttnView& t, int64_t row, int h, bool in, bf16x8 (&f)[D / 16]) {
+  const uint16_t* p = static_cast<const uint16_t*>(t.ptr) + row * t.row + h * t.head + 8 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) f[s] = as_bf(in ? ld16(p + 16 * s) : zero4());
+}
+
+// The larger / the sum of the two lanes that share a column.
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ bf16x8 pack8(const f32x16& x, int t) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = f2bf2(x[8 * t + 2 * i], x[8 * t + 2 * i + 1]);
+  return as_bf(v);
+}
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) z[v] = 0.f;
+  return z;
+}
+
+// Row of value v of a 32 x 32 tile.
+__device__ __forceinline__ int tile_row(int v) { return 8 * (v >> 2) + 4 * ((threadIdx.x >> 5) & 1) + (v & 3); }
+
+// The running softmax of a lane's query: the reference that exponents are taken from (base 2, times
+// scale) and the lane's own part of the sum.
+struct Running {
+  float ref = -INFINITY, sum = 0.f;
+};
+
+// Scores x (16 N per lane, masked ones -inf) to exp2(c x - ref), with the sums and acc moved to a new
+// reference where a score exceeds the old one by more than 2^8: what leaves the reference alone is bounded
+// by that, and all but the first blocks of a row do.
+template <int N, int NA>
+__device__ __forceinline__ void softmax_step(f32x16 (&x)[N], float c, Running& r, f32x16 (&acc)[NA]) {
+  float mx = x[0][0];
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, x[u][v]);
+  const float top = pair_max(mx) * c;
+  if (__builtin_amdgcn_ballot_w64(top > r.ref + 8.f) != 0) {
+    const float ref = fmaxf(top, r.ref);
+    const float f = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r.ref - ref);
+    r.ref = ref;
+    r.sum *= f;
+#pragma unroll
+    for (int t = 0; t < NA; ++t) acc[t] *= f;
+  }
+  const float ref = r.ref == -INFINITY ? 0.f : r.ref;  // no key seen so far: every term is exp2(-inf) = 0
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      x[u][v] = __builtin_amdgcn_exp2f(x[u][v] * c - ref);
+      r.sum += x[u][v];
+    }
+}
+
+__device__ __forceinline__ float lse_of(float ref, float sum) {
+  return sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int D>
+__device__ __forceinline__ void store_cols(const AttnView& t, int64_t row, int h, const f32x16 (&acc)[D / 32], float f) {
+  uint16_t* p = static_cast<uint16_t*>(t.ptr) + row * t.row + h * t.head + 4 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const uint32_t w0 = f2bf2(acc[i][4 * a] * f, acc[i][4 * a + 1] * f);
+      const uint32_t w1 = f2bf2(acc[i][4 * a + 2] * f, acc[i][4 * a + 3] * f);
+      *reinterpret_cast<uint2*>(p + 32 * i + 8 * a) = make_uint2(w0, w1);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
+  constexpr int TK = 64, TILE = TK * 2 * D;
+  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
+  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
+  const int item = blockIdx.x / a.hq, h = head_of(a, blockIdx.x % a.hq);
+  const Seq s(a, a.items[2 * item]);
+  const int qt = a.items[2 * item + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int off = s.kl - s.ql, hk = h / a.group;
+  const int q = qt + 32 * wave + (lane & 31);
+  const int k_end = min(s.kl, min(qt + kAttnFwdRows, s.ql) + off);
+  const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
+  auto load = [&](int kt, char* b) {
+    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave);
+    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave);
+  };
+  if (k_end > 0) load(0, b0);
+  bf16x8 qf[D / 16];
+  row_frags<D>(a.Q, (int64_t)s.q0 + q, h, q < s.ql, qf);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
+  Running run;
+  const float c = a.scale * kLog2e;
+  const int seen = q + off;                                        // the lane's last key
+  const int wave_all = qt + 32 * wave + off;                       // keys up to here are seen by the whole wave
+  const int wave_end = min(s.kl, wave_all + 32);                   // keys from here on by none of it
+  auto step = [&](int kt, const char* cur, char* nxt) {
+    vmem_wait_all();
+    __syncthreads();
+    if (kt + TK < k_end) load(kt + TK, nxt);
+    if (kt >= wave_end) return;
+    f32x16 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      x[u] = zero16();
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x[u], 0, 0, 0);
+    }
+    if (kt + TK - 1 > wave_all) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[u][v] = kt + 32 * u + tile_row(v) <= seen ? x[u][v] : -INFINITY;
+    }
+    softmax_step(x, c, run, acc);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const bf16x8 p = pack8(x[w >> 1], w & 1);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, acc[t], 0, 0, 0);
+    }
+  };
+  for (int kt = 0; kt < k_end; kt += 2 * TK) {
+    step(kt, b0, b1);
+    if (kt + TK < k_end) step(kt + TK, b1, b0);
+  }
+  const float sum = pair_sum(run.sum);
+  if (q >= s.ql) return;
+  store_cols<D>(a.O, (int64_t)s.q0 + q, h, acc, sum == 0.f ? 0.f : 1.f / sum);
+  if (a.lse && lane < 32) a.lse[(int64_t)h * a.n_q + s.q0 + q] = lse_of(run.ref, sum);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// One piece of the keys of a sequence for 32 (query, head) pairs of a key head, row r being query
+// r / group and head r % group.  Each wave takes every fourth block of 32 keys through buffers of its
+// own (no barrier until the end), then the four waves' sums are added.
+template <int D>
+__global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
+  constexpr int TK = 32, TILE = TK * 2 * D, LDO = D + 4;
+  constexpr int kOut = 4 * 32 * LDO * 4, kBuf = 4 * 2 * TILE;
+  __shared__ __attribute__((aligned(1024))) char b0[kOut > kBuf ? kOut : kBuf];
+  __shared__ __attribute__((aligned(1024))) char b1[kBuf];
+  __shared__ float ml[2][4][32];
+  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
+  const int32_t* it = a.items + 4 * (int64_t)item;
+  const Seq s(a, it[0]);
+  const int r0 = it[1], n_pieces = it[3];
+  const int k_first = a.split_keys[2 * (int64_t)item], k_last = a.split_keys[2 * (int64_t)item + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int off = s.kl - s.ql, rows = s.ql * a.group;
+  const int r = r0 + (lane & 31), q = min(r, rows - 1) / a.group, h = hk * a.group + min(r, rows - 1) % a.group;
+  const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
+  char* const w0 = b0 + wave * 2 * TILE;
+  char* const w1 = b1 + wave * 2 * TILE;
+  auto load = [&](int kt, char* b) {
+    stage<D, TK, 1>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, 0);
+    stage<D, TK, 1>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, 0);
+  };
+  constexpr int LOADS = 2 * TILE / 1024;
+  const int kb = k_first + TK * wave;
+  bf16x8 qf[D / 16];
+  row_frags<D>(a.Q, (int64_t)s.q0 + q, h, r < rows, qf);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the counts below are the staged loads alone
+  if (kb < k_last) load(kb, w0);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
+  Running run;
+  const float c = a.scale * kLog2e;
+  const int seen = q + off;
+  const int all = min(r0, rows - 1) / a.group + off;  // keys up to here are seen by every row
+  auto step = [&](int kt, const char* cur, char* nxt) {
+    if (kt + 4 * TK < k_last) {
+      load(kt + 4 * TK, nxt);
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));
+    } else {
+      vmem_wait_all();
+    }
+    asm volatile("" ::: "memory");
+    f32x16 x[1];
+    x[0] = zero16();
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, 0, i), qf[i], x[0], 0, 0, 0);
+    if (kt + TK - 1 > all || kt + TK > k_last) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        x[0][v] = kt + tile_row(v) <= seen && kt + tile_row(v) < k_last ? x[0][v] : -INFINITY;
+    }
+    softmax_step(x, c, run, acc);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const bf16x8 p = pack8(x[0], w);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, acc[t], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // `cur` is read before it is loaded again
+  };
+  for (int kt = kb; kt < k_last; kt += 8 * TK) {
+    step(kt, w0, w1);
+    if (kt + 4 * TK < k_last) step(kt + 4 * TK, w1, w0);
+  }
+  const float sum = pair_sum(run.sum);
+  __syncthreads();  // every wave is done with its buffers
+  float* const out = reinterpret_cast<float*>(b0) + (wave * 32 + (lane & 31)) * LDO + 4 * (lane >> 5);
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(out + 32 * t + 8 * i) =
+          f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+  if (lane < 32) {
+    ml[0][wave][lane] = run.ref;
+    ml[1][wave][lane] = sum;
+  }
+  __syncthreads();
+  // row tid / 8, D / 8 columns each
+  const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8);
+  if (r0 + row >= rows) return;
+  float ref = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) ref = fmaxf(ref, ml[0][w][row]);
+  float f[4], total = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = ml[0][w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0][w][row] - ref);
+    total += f[w] * ml[1][w][row];
+  }
+  const bool whole = n_pieces == 1;
+  const float g = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
+  const int qr = (r0 + row) / a.group, hr = hk * a.group + (r0 + row) % a.group;
+  const int64_t slot = (int64_t)item * a.hkv + hk;
+#pragma unroll
+  for (int i = 0; i < D / 8; i += 4) {
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(b0) + (w * 32 + row) * LDO + c0 + i) * f[w];
+    o *= g;
+    if (whole) {
+      uint16_t* p = static_cast<uint16_t*>(a.O.ptr) + ((int64_t)s.q0 + qr) * a.O.row + hr * a.O.head + c0 + i;
+      *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(o[0], o[1]), f2bf2(o[2], o[3]));
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (slot * kAttnPackRows + row) * D + c0 + i) = o;
+    }
+  }
+  if ((threadIdx.x & 7) == 0) {
+    if (!whole) {
+      a.part_ml[slot * 2 * kAttnPackRows + row] = ref;
+      a.part_ml[(slot * 2 + 1) * kAttnPackRows + row] = total;
+    } else if (a.lse) {
+      a.lse[(int64_t)hr * a.n_q + s.q0 + qr] = lse_of(ref, total);
+    }
+  }
+}
+
+// The pieces of a tile of the split form, added in order: row tid / 8, D / 8 columns each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
+  const int32_t* it = a.join_items + 4 * (int64_t)item;
+  const int n = it[3];
+  if (n == 1) return;  // written by its only piece
+  const Seq s(a, it[0]);
+  const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8), r = it[1] + row;
+  if (r >= s.ql * a.group) return;
+  float ref = -INFINITY, total = 0.f;
+  for (int k = 0; k < n; ++k)
+    ref = fmaxf(ref, a.part_ml[((int64_t)(it[2] + k) * a.hkv + hk) * 2 * kAttnPackRows + row]);
+  f32x4 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < n; ++k) {
+    const int64_t slot = (int64_t)(it[2] + k) * a.hkv + hk;
+    const float m = a.part_ml[slot * 2 * kAttnPackRows + row];
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
+    total += f * a.part_ml[(slot * 2 + 1) * kAttnPackRows + row];
+    const float* p = a.part_o + (slot * kAttnPackRows + row) * D + c0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + 4 * i) * f;
+  }
+  const float g = total == 0.f ? 0.f : 1.f / total;
+  const int q = r / a.group, h = hk * a.group + r % a.group;
+  uint16_t* p = static_cast<uint16_t*>(a.O.ptr) + ((int64_t)s.q0 + q) * a.O.row + h * a.O.head + c0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+    *reinterpret_cast<uint2*>(p + 4 * i) = make_uint2(f2bf2(o[i][0] * g, o[i][1] * g), f2bf2(o[i][2] * g, o[i][3] * g));
+  if (a.lse && (threadIdx.x & 7) == 0) a.lse[(int64_t)h * a.n_q + s.q0 + q] = lse_of(ref, total);
+}
+
+// ---------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void attn_dq_kernel(AttnArgs a) {
+  constexpr int TK = 64, TILE = TK * 2 * D;
+  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
+  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
+  const int item = blockIdx.x / a.hq, h = head_of(a, blockIdx.x % a.hq);
+  const Seq s(a, a.items[2 * item]);
+  const int qt = a.items[2 * item + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int off = s.kl - s.ql, hk = h / a.group;
+  const int q = qt + 32 * wave + (lane & 31);
+  const bool in = q < s.ql;
+  const int k_end = min(s.kl, min(qt + kAttnBwdRows, s.ql) + off);
+  const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
+  auto load = [&](int kt, char* b) {
+    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave);
+    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave);
+  };
+  if (k_end > 0) load(0, b0);
+  bf16x8 qf[D / 16], df[D / 16];
+  row_frags<D>(a.Q, (int64_t)s.q0 + q, h, in, qf);
+  row_frags<D>(a.dO, (int64_t)s.cq + q, h, in, df);
+  float dot = 0.f;
+  {
+    bf16x8 of[D / 16];
+    row_frags<D>(a.O, (int64_t)s.q0 + q, h, in, of);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot += (float)df[i][e] * (float)of[i][e];
+  }
+  const float delta = pair_sum(dot);
+  if (in && lane < 32) a.delta[h * a.train_q + s.cq + q] = delta;
+  const float lse2 = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : 0.f;
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
+  const float c = a.scale * kLog2e;
+  const int seen = q + off, wave_all = qt + 32 * wave + off, wave_end = min(s.kl, wave_all + 32);
+  auto step = [&](int kt, const char* cur, char* nxt) {
+    vmem_wait_all();
+    __syncthreads();
+    if (kt + TK < k_end) load(kt + TK, nxt);
+    if (kt >= wave_end) return;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, u, i), df[i], dp, 0, 0, 0);
+      if (kt + 32 * u + 31 > wave_all) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          x[v] = kt + 32 * u + tile_row(v) <= seen ? __builtin_amdgcn_exp2f(x[v] * c - lse2) * (dp[v] - delta) : 0.f;
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] * c - lse2) * (dp[v] - delta);
+      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const bf16x8 p = pack8(x, w);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur, 2 * u + w, t), p, acc[t], 0, 0, 0);
+      }
+    }
+  };
+  for (int kt = 0; kt < k_end; kt += 2 * TK) {
+    step(kt, b0, b1);
+    if (kt + TK < k_end) step(kt + TK, b1, b0);
+  }
+  if (in) store_cols<D>(a.dQ, (int64_t)s.cq + q, h, acc, a.scale);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// dK and dV of 128 keys of one key head, 32 a wave, over 32 queries at a time, the key head's query
+// heads one after the other: the sums over them stay in registers.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dk_kernel(AttnArgs a) {
+  constexpr int TQ = 32, TILE = TQ * 2 * D;
+  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
+  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
+  __shared__ __attribute__((aligned(16))) float st[2][2][TQ];  // [buffer][lse (base 2), delta]
+  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
+  const Seq s(a, a.items[2 * item]);
+  const int k0 = a.items[2 * item + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int off = s.kl - s.ql;
+  const int k = k0 + 32 * wave + (lane & 31);
+  const bool in = k < s.kl;
+  const int qrow = (int)a.Q.row * 2, drow = (int)a.dO.row * 2;
+  const int q_first = max(0, k0 - off);
+  const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, steps = per_head * a.group;
+  float st_next = 0.f;  // of the next step: lse (threads 0 ..), delta (threads TQ ..)
+  auto load = [&](int n, char* b) {
+    const int h = hk * a.group + n / per_head, qt = q_first + n % per_head * TQ;
+    stage<D, TQ, 4>(rows_rsrc(a.Q, (int64_t)s.q0 + qt, h, min(TQ, s.ql - qt), D), qrow, b, wave);
+    stage<D, TQ, 4>(rows_rsrc(a.dO, (int64_t)s.cq + qt, h, min(TQ, s.ql - qt), D), drow, b + TILE, wave);
+    // queries past the last one: lse of +infinity makes their p and ds zero
+    if (threadIdx.x < 2 * TQ) {
+      const int r = threadIdx.x & (TQ - 1), q = qt + r;
+      if (threadIdx.x < TQ) st_next = q < s.ql ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : INFINITY;
+      else st_next = q < s.ql ? a.delta[h * a.train_q + s.cq + q] : 0.f;
+    }
+  };
+  if (steps > 0) load(0, b0);
+  bf16x8 kf[D / 16], vf[D / 16];
+  row_frags<D>(a.K, (int64_t)s.k0 + k, hk, in, kf);
+  row_frags<D>(a.V, (int64_t)s.k0 + k, hk, in, vf);
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zero16();
+  const float c = a.scale * kLog2e;
+  auto step = [&](int n, int b, const char* cur, char* nxt) {
+    vmem_wait_all();
+    if (threadIdx.x < 2 * TQ) st[b][threadIdx.x / TQ][threadIdx.x & (TQ - 1)] = st_next;
+    __syncthreads();
+    if (n + 1 < steps) load(n + 1, nxt);
+    const int qt = q_first + n % per_head * TQ;
+    f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, 0, i), kf[i], x, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, 0, i), vf[i], dp, 0, 0, 0);
+    const bool cut = k0 + 32 * wave + 31 > qt + off;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + 4 * (lane >> 5);
+      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st[b][0][r]), d4 = *reinterpret_cast<const f32x4*>(&st[b][1][r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = 4 * i + e;
+        float p = __builtin_amdgcn_exp2f(x[v] * c - l4[e]);
+        if (cut) p = k <= qt + r + e + off ? p : 0.f;
+        x[v] = p;
+        dp[v] = cut && k > qt + r + e + off ? 0.f : p * (dp[v] - d4[e]);
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const bf16x8 p = pack8(x, w), ds = pack8(dp, w);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+        dv[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, dv[t], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+        dk[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur, w, t), ds, dk[t], 0, 0, 0);
+    }
+  };
+  for (int n = 0; n < steps; n += 2) {
+    step(n, 0, b0, b1);
+    if (n + 1 < steps) step(n + 1, 1, b1, b0);
+  }
+  if (!in) return;
+  store_cols<D>(a.dK, (int64_t)s.ck + k, hk, dk, a.scale);
+  store_cols<D>(a.dV, (int64_t)s.ck + k, hk, dv, 1.f);
+}
+
+// ---- host -------------------------------------------------------------------------------------------
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct Workspace {
+  size_t part_o, part_ml, delta, total;
+};
+
+Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
+  Workspace w{};
+  size_t at = 0;
+  bool joined = false;  // some tile has more than one piece
+  const int32_t* join = p.meta.data() + p.lay.join_items;
+  for (int32_t i = 0; i < p.n_join; ++i) joined |= join[4 * i + 3] > 1;
+  const size_t slots = dt == DSV_BF16 && joined ? (size_t)p.n_split * p.hkv : 0;
+  w.part_o = at;
+  at += align256(slots * kAttnPackRows * p.d * sizeof(float));
+  w.part_ml = at;
+  at += align256(slots * 2 * kAttnPackRows * sizeof(float));
+  // the two directions do not overlap on a stream: delta shares the room
+  w.delta = 0;
+  w.total = std::max<size_t>(256, std::max(at, align256((size_t)p.train_q * p.hq * sizeof(float))));
+  return w;
+}
+
+constexpr int64_t kMaxRowStride = 1 << 23, kMaxHeadStride = (int64_t)1 << 40;
+
+// The view with dense strides filled in; out: its vectors must be apart.
+int view(const dsv_attn_view* v, int64_t rows, int32_t heads, int32_t d, bool out, AttnView* to) {
+  if (!v) return DSV_ERR_ARG;
+  to->ptr = v->ptr;
+  to->row = v->row == 0 ? (int64_t)heads * d : v->row;
+  to->head = v->head == 0 ? d : v->head;
+  if (reinterpret_cast<uintptr_t>(v->ptr) & 15) return DSV_ERR_ARG;
+  if (rows > 0 && !v->ptr) return DSV_ERR_ARG;
+  if (to->row < d || to->head < d || (to->row & 7) || (to->head & 7) || to->row > kMaxRowStride ||
+      to->head > kMaxHeadStride)
+    return DSV_ERR_SIZE;
+  if (out && rows > 0 && to->row < (heads - 1) * to->head + d && to->head < (rows - 1) * to->row + d) return DSV_ERR_SIZE;
+  return DSV_OK;
+}
+
+int check(const dsv_attn_plan* p, dsv_dtype dt, double scale) {
+  if (!p || !p->d_meta) return DSV_ERR_ARG;
+  if (dt != DSV_BF16 && dt != DSV_F32) return DSV_ERR_RANGE;
+  if (!std::isfinite(scale) || !(scale > 0) || !std::isfinite((float)scale)) return DSV_ERR_RANGE;
+  return DSV_OK;
+}
+
+AttnArgs common(const dsv_attn_plan& p, double scale) {
+  AttnArgs a{};
+  a.seqs = p.dptr(p.lay.seqs);
+  a.hq = p.hq;
+  a.hkv = p.hkv;
+  a.group = p.hq / p.hkv;
+  a.d = p.d;
+  a.n_q = p.n_q;
+  a.train_q = p.train_q;
+  a.scale = (float)scale;
+  return a;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? DSV_OK : DSV_ERR_DEVICE; }
+
+template <typename K>
+hipError_t launch(K k64, K k128, const AttnArgs& a, int64_t groups, hipStream_t s) {
+  if (groups <= 0) return hipSuccess;
+  hipLaunchKernelGGL(a.d == 64 ? k64 : k128, dim3((unsigned)groups), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace dsv
+
+using namespace dsv;
+
+extern "C" int dsv_attn_workspace(const dsv_attn_plan* p, dsv_dtype dt, size_t* bytes) {
+  if (!p || !bytes) return DSV_ERR_ARG;
+  if (dt != DSV_BF16 && dt != DSV_F32) return DSV_ERR_RANGE;
+  *bytes = carve(*p, dt).total;
+  return DSV_OK;
+}
+
+extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, const dsv_attn_view* Q,
+                            const dsv_attn_view* K, const dsv_attn_view* V, const dsv_attn_view* O, float* lse,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  int rc = check(p, dt, scale);
+  if (rc != DSV_OK) return rc;
+  AttnArgs a = common(*p, scale);
+  if ((rc = view(Q, p->n_q, p->hq, p->d, false, &a.Q)) != DSV_OK) return rc;
+  if ((rc = view(K, p->n_kv, p->hkv, p->d, false, &a.K)) != DSV_OK) return rc;
+  if ((rc = view(V, p->n_kv, p->hkv, p->d, false, &a.V)) != DSV_OK) return rc;
+  if ((rc = view(O, p->n_q, p->hq, p->d, true, &a.O)) != DSV_OK) return rc;
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return DSV_ERR_ARG;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
+  const Workspace w = carve(*p, dt);
+  if (ws_bytes < w.total) return DSV_ERR_SIZE;
+  a.lse = lse;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (dt == DSV_F32) {
+    a.items = p->dptr(p->lay.f32_items);
+    a.n_items = p->n_f32;
+    return status(launch_attn_f32_fwd(a, s));
+  }
+  a.items = p->dptr(p->lay.fwd_items);
+  a.n_items = p->n_fwd;
+  hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, (int64_t)p->n_fwd * p->hq, s);
+  if (e != hipSuccess || p->n_split == 0) return status(e);
+  a.items = p->dptr(p->lay.split_items);
+  a.n_items = p->n_split;
+  a.split_keys = p->dptr(p->lay.split_keys);
+  a.join_items = p->dptr(p->lay.join_items);
+  a.n_join = p->n_join;
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_o);
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_ml);
+  e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, (int64_t)p->n_split * p->hkv, s);
+  if (e != hipSuccess || p->n_split == p->n_join) return status(e);  // one piece each: nothing to join
+  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, (int64_t)p->n_join * p->hkv, s));
+}
+
+extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, const dsv_attn_view* Q,
+                            const dsv_attn_view* K, const dsv_attn_view* V, const dsv_attn_view* O, const float* lse,
+                            const dsv_attn_view* dO, const dsv_attn_view* dQ, const dsv_attn_view* dK,
+                            const dsv_attn_view* dV, void* ws, size_t ws_bytes, void* hip_stream) {
+  int rc = check(p, dt, scale);
+  if (rc != DSV_OK) return rc;
+  AttnArgs a = common(*p, scale);
+  if ((rc = view(Q, p->n_q, p->hq, p->d, false, &a.Q)) != DSV_OK) return rc;
+  if ((rc = view(K, p->n_kv, p->hkv, p->d, false, &a.K)) != DSV_OK) return rc;
+  if ((rc = view(V, p->n_kv, p->hkv, p->d, false, &a.V)) != DSV_OK) return rc;
+  if ((rc = view(O, p->n_q, p->hq, p->d, false, &a.O)) != DSV_OK) return rc;
+  if ((rc = view(dO, p->train_q, p->hq, p->d, false, &a.dO)) != DSV_OK) return rc;
+  if ((rc = view(dQ, p->train_q, p->hq, p->d, true, &a.dQ)) != DSV_OK) return rc;
+  if ((rc = view(dK, p->train_k, p->hkv, p->d, true, &a.dK)) != DSV_OK) return rc;
+  if ((rc = view(dV, p->train_k, p->hkv, p->d, true, &a.dV)) != DSV_OK) return rc;
+  if ((p->train_q > 0 && !lse) || (reinterpret_cast<uintptr_t>(lse) & 3)) return DSV_ERR_ARG;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
+  const Workspace w = carve(*p, dt);
+  if (ws_bytes < w.total) return DSV_ERR_SIZE;
+  a.lse = const_cast<float*>(lse);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(ws) + w.delta);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const bool f32 = dt == DSV_F32;
+  a.items = p->dptr(f32 ? p->lay.f32_dq_items : p->lay.dq_items);
+  a.n_items = f32 ? p->n_f32_dq : p->n_dq;
+  hipError_t e = f32 ? launch_attn_f32_dq(a, s) : launch(attn_dq_kernel<64>, attn_dq_kernel<128>, a, (int64_t)a.n_items * p->hq, s);
+  if (e != hipSuccess) return status(e);
+  a.items = p->dptr(f32 ? p->lay.f32_dk_items : p->lay.dk_items);
+  a.n_items = f32 ? p->n_f32_dk : p->n_dk;
+  return status(f32 ? launch_attn_f32_dk(a, s)
+                    : launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, (int64_t)a.n_items * p->hkv, s));
+}

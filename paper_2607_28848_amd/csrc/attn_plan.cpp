@@ -1,0 +1,243 @@
+// attn_plan.cpp -- validation and packing of a mixed batch's attention (host only, plus
+// one asynchronous host-to-device copy of the packed blob).
+//
+// The sequences of a batch (Sec. 3.2: inference entries and fine-tuning samples) are the
+// same for every layer, so the tiles, their order and the pieces of long caches are laid
+// down here, once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <new>
+#include <numeric>
+
+#include "attn_plan.h"
+
+namespace {
+
+using namespace dsv;
+
+// Tiles of `rows` rows, as {sequence, first row}, those with the most work first (ties: table
+// order), so that the last workgroups to start are short ones.
+struct Tiles {
+  std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t;
+  void add(int64_t work, int32_t seq, int64_t first) { t.push_back({-work, {seq, (int32_t)first}}); }
+  std::vector<int32_t> words() {
+    std::stable_sort(t.begin(), t.end(), [](const auto& a, const auto& b) { return a.first < b.first; });
+    std::vector<int32_t> w;
+    w.reserve(2 * t.size());
+    for (const auto& e : t) w.insert(w.end(), {e.second.first, e.second.second});
+    return w;
+  }
+};
+
+// Keys that queries [.., last] of a sequence see.
+int64_t keys_seen(const dsv_attn_seq& s, int64_t last) {
+  return std::max<int64_t>(0, std::min<int64_t>(s.k_len, last + 1 + s.k_len - s.q_len));
+}
+
+int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_t hq, int32_t hkv, int32_t d,
+          dsv_attn_plan& p) {
+  if (n < 0 || n_q < 0 || n_kv < 0 || (n > 0 && !seqs)) return DSV_ERR_ARG;
+  if (hkv < 1 || hq < hkv || hq > 1024 || hq % hkv != 0 || (d != 64 && d != 128)) return DSV_ERR_RANGE;
+  std::vector<int32_t> order(n);
+  std::iota(order.begin(), order.end(), 0);
+  for (int32_t i = 0; i < n; ++i) {
+    const dsv_attn_seq& s = seqs[i];
+    if (s.is_train != 0 && s.is_train != 1) return DSV_ERR_RANGE;
+    if (s.q_start < 0 || s.q_len < 0 || s.k_start < 0 || s.k_len < 0) return DSV_ERR_LAYOUT;
+    if ((int64_t)s.q_start + s.q_len > n_q || (int64_t)s.k_start + s.k_len > n_kv) return DSV_ERR_LAYOUT;
+  }
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return seqs[a].q_start < seqs[b].q_start; });
+  int64_t end = 0;
+  for (int32_t i : order) {
+    if (seqs[i].q_len == 0) continue;
+    if (seqs[i].q_start < end) return DSV_ERR_LAYOUT;  // overlapping query ranges
+    end = (int64_t)seqs[i].q_start + seqs[i].q_len;
+  }
+
+  // workgroups of a launch, before the work lists are laid down
+  int64_t tiles_q = 0, tiles_k = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    tiles_q += ((int64_t)seqs[i].q_len + kAttnF32Rows - 1) / kAttnF32Rows;
+    tiles_k += ((int64_t)seqs[i].k_len + kAttnF32Rows - 1) / kAttnF32Rows;
+  }
+  if (tiles_q * hq > INT32_MAX || tiles_k * hkv > INT32_MAX) return DSV_ERR_SIZE;
+
+  p.n_seqs = n;
+  p.n_q = n_q;
+  p.n_kv = n_kv;
+  p.hq = hq;
+  p.hkv = hkv;
+  p.d = d;
+  const int32_t group = hq / hkv;
+  std::vector<int32_t> desc((size_t)n * kAttnSeqWords, 0);
+  for (int32_t i : order) {
+    const dsv_attn_seq& s = seqs[i];
+    int32_t* w = &desc[(size_t)i * kAttnSeqWords];
+    w[0] = s.q_start;
+    w[1] = s.q_len;
+    w[2] = s.k_start;
+    w[3] = s.k_len;
+    w[4] = w[5] = -1;
+    if (s.is_train) {
+      if (p.train_q + s.q_len > INT32_MAX || p.train_k + s.k_len > INT32_MAX) return DSV_ERR_SIZE;
+      w[4] = (int32_t)p.train_q;
+      w[5] = (int32_t)p.train_k;
+      p.train_q += s.q_len;
+      p.train_k += s.k_len;
+    }
+  }
+
+  Tiles fwd, f32, dq, dk, f32_dq, f32_dk;
+  int64_t split_keys_all = 0;  // keys that the split form's tiles read
+  std::vector<int32_t> split;
+  for (int32_t i = 0; i < n; ++i) {
+    const dsv_attn_seq& s = seqs[i];
+    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows)
+      f32.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
+    if (s.q_len <= kAttnSplitQ) {
+      if (s.q_len == 0) continue;
+      split.push_back(i);
+      const int64_t tiles = ((int64_t)s.q_len * group + kAttnPackRows - 1) / kAttnPackRows;
+      split_keys_all += tiles * s.k_len;
+    } else {
+      for (int64_t q = 0; q < s.q_len; q += kAttnFwdRows)
+        fwd.add(keys_seen(s, std::min<int64_t>(q + kAttnFwdRows, s.q_len) - 1), i, q);
+    }
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    const dsv_attn_seq& s = seqs[i];
+    if (!s.is_train) continue;
+    for (int64_t q = 0; q < s.q_len; q += kAttnBwdRows)
+      dq.add(keys_seen(s, std::min<int64_t>(q + kAttnBwdRows, s.q_len) - 1), i, q);
+    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows)
+      f32_dq.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
+    // queries that see key k: from max(0, k - (k_len - q_len)) on
+    auto seen_by = [&](int64_t k) { return s.q_len - std::max<int64_t>(0, k - ((int64_t)s.k_len - s.q_len)); };
+    for (int64_t k = 0; k < s.k_len; k += kAttnBwdRows) dk.add(seen_by(k), i, k);
+    for (int64_t k = 0; k < s.k_len; k += kAttnF32Rows) f32_dk.add(seen_by(k), i, k);
+  }
+
+  // Pieces: one length for the whole call, such that all tiles' pieces are about
+  // kAttnSplitTarget workgroups.
+  int64_t piece = (split_keys_all * hkv + kAttnSplitTarget - 1) / kAttnSplitTarget;
+  piece = std::max<int64_t>(kAttnPieceKeys, (piece + kAttnPieceKeys - 1) / kAttnPieceKeys * kAttnPieceKeys);
+  std::vector<int32_t> split_items, split_keys, join_items;
+  for (int32_t i : split) {
+    const dsv_attn_seq& s = seqs[i];
+    const int64_t rows = (int64_t)s.q_len * group;
+    // pieces of equal length (to a multiple of 32 keys)
+    const int64_t np = std::max<int64_t>(1, (s.k_len + piece - 1) / piece);
+    const int64_t len = std::max<int64_t>(32, ((s.k_len + np - 1) / np + 31) / 32 * 32);
+    for (int64_t r = 0; r < rows; r += kAttnPackRows) {
+      const int64_t first = (int64_t)split_items.size() / 4;
+      if (first + np > INT32_MAX) return DSV_ERR_SIZE;
+      join_items.insert(join_items.end(), {i, (int32_t)r, (int32_t)first, (int32_t)np});
+      for (int64_t k = 0; k < np; ++k) {
+        split_items.insert(split_items.end(), {i, (int32_t)r, (int32_t)k, (int32_t)np});
+        split_keys.insert(split_keys.end(), {(int32_t)std::min<int64_t>(k * len, s.k_len),
+                                             (int32_t)std::min<int64_t>((k + 1) * len, s.k_len)});
+      }
+    }
+  }
+
+  std::vector<int32_t>& m = p.meta;
+  auto put = [&](const std::vector<int32_t>& w) {
+    const int64_t off = (int64_t)m.size();
+    m.insert(m.end(), w.begin(), w.end());
+    m.resize((m.size() + 3) & ~size_t(3), 0);
+    return off;
+  };
+  AttnLayout& L = p.lay;
+  auto count = [](const std::vector<int32_t>& w, int words, int32_t* out) {
+    const int64_t c = (int64_t)w.size() / words;
+    *out = (int32_t)c;
+    return c;
+  };
+  const std::vector<int32_t> wf = fwd.words(), w3 = f32.words(), wq = dq.words(), wk = dk.words(), w3q = f32_dq.words(),
+                             w3k = f32_dk.words();
+  int64_t most = 0;
+  most = std::max(most, count(wf, 2, &p.n_fwd));
+  most = std::max(most, count(w3, 2, &p.n_f32));
+  most = std::max(most, count(split_items, 4, &p.n_split));
+  most = std::max(most, count(join_items, 4, &p.n_join));
+  most = std::max(most, count(wq, 2, &p.n_dq));
+  most = std::max(most, count(wk, 2, &p.n_dk));
+  most = std::max(most, count(w3q, 2, &p.n_f32_dq));
+  most = std::max(most, count(w3k, 2, &p.n_f32_dk));
+  if (most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
+  L.seqs = put(desc);
+  L.fwd_items = put(wf);
+  L.f32_items = put(w3);
+  L.split_items = put(split_items);
+  L.split_keys = put(split_keys);
+  L.join_items = put(join_items);
+  L.dq_items = put(wq);
+  L.dk_items = put(wk);
+  L.f32_dq_items = put(w3q);
+  L.f32_dk_items = put(w3k);
+  m.resize(std::max<size_t>(64, (m.size() + 63) & ~size_t(63)), 0);
+  L.total_words = (int64_t)m.size();
+  return DSV_OK;
+}
+
+}  // namespace
+
+extern "C" int dsv_attn_build(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv, int32_t heads_q,
+                              int32_t heads_kv, int32_t head_dim, size_t* meta_bytes, dsv_attn_plan** out_plan) {
+  if (out_plan) *out_plan = nullptr;
+  if (!meta_bytes || !out_plan) return DSV_ERR_ARG;
+  dsv_attn_plan* p = nullptr;
+  int rc = DSV_OK;
+  try {
+    p = new dsv_attn_plan();
+    rc = build(seqs, n_seqs, n_q, n_kv, heads_q, heads_kv, head_dim, *p);
+  } catch (const std::bad_alloc&) {
+    rc = DSV_ERR_SIZE;
+  } catch (...) {
+    rc = DSV_ERR_ARG;
+  }
+  if (rc != DSV_OK) {
+    delete p;
+    return rc;
+  }
+  *meta_bytes = (size_t)p->lay.total_words * sizeof(int32_t);
+  *out_plan = p;
+  return DSV_OK;
+}
+
+extern "C" int dsv_attn_upload(dsv_attn_plan* p, void* d_meta, size_t meta_bytes, void* hip_stream) {
+  if (!p || !d_meta || p->d_meta || reinterpret_cast<uintptr_t>(d_meta) % 256 != 0) return DSV_ERR_ARG;
+  const size_t need = (size_t)p->lay.total_words * sizeof(int32_t);
+  if (meta_bytes < need) return DSV_ERR_SIZE;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  hipEvent_t ev = nullptr;
+  hipError_t e = hipEventCreateWithFlags(&ev, hipEventDisableTiming);
+  if (e == hipSuccess) e = hipMemcpyAsync(d_meta, p->meta.data(), need, hipMemcpyHostToDevice, st);
+  if (e == hipSuccess) e = hipEventRecord(ev, st);
+  if (e != hipSuccess) {
+    if (ev) (void)hipEventDestroy(ev);
+    return DSV_ERR_DEVICE;
+  }
+  p->copy_done = ev;
+  p->d_meta = d_meta;
+  return DSV_OK;
+}
+
+extern "C" int dsv_attn_train_rows(const dsv_attn_plan* p, int64_t out[2]) {
+  if (!p || !out) return DSV_ERR_ARG;
+  out[0] = p->train_q;
+  out[1] = p->train_k;
+  return DSV_OK;
+}
+
+extern "C" void dsv_attn_free(dsv_attn_plan* p) {
+  if (!p) return;
+  if (p->copy_done) {
+    // the host image is the source of the asynchronous upload: wait for it
+    hipEvent_t ev = static_cast<hipEvent_t>(p->copy_done);
+    (void)hipEventSynchronize(ev);
+    (void)hipEventDestroy(ev);
+  }
+  delete p;
+}

@@ -1,0 +1,54 @@
+// attn_plan.h -- host plan and packed device metadata of a mixed batch's attention.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <vector>
+
+#include "dsv.h"
+
+namespace dsv {
+
+// sequence descriptor: {q_start, q_len, k_start, k_len, compact q row, compact k row, 0, 0}
+// (compact rows: -1 unless the sequence is a fine-tuning sample)
+constexpr int kAttnSeqWords = 8;
+// Rows of a forward tile (bf16), of a gradient tile (bf16: queries, keys) and of the fp32 tiles.
+constexpr int kAttnFwdRows = 128;
+constexpr int kAttnBwdRows = 128;
+constexpr int kAttnF32Rows = 64;
+// A sequence of up to kAttnSplitQ queries takes the split form: the (query, head) pairs of a
+// key head form rows, kAttnPackRows to a tile, and the keys are split into pieces.
+constexpr int kAttnSplitQ = 16;
+constexpr int kAttnPackRows = 32;
+// Pieces of the split form: multiples of kAttnPieceKeys keys (each of the workgroup's four waves
+// takes blocks of 32 of them by turns), as many as bring about kAttnSplitTarget workgroups.
+constexpr int kAttnPieceKeys = 128;
+constexpr int kAttnSplitTarget = 512;
+
+// Word offsets inside the packed blob (int32 words).
+struct AttnLayout {
+  int64_t seqs;         // [n_seqs][kAttnSeqWords]
+  int64_t fwd_items;    // [n_fwd][2] {sequence, first query}: bf16 forward tiles, most keys first
+  int64_t f32_items;    // [n_f32][2] {sequence, first query}: fp32 forward tiles of every sequence
+  int64_t split_items;  // [n_split][4] {sequence, first row, piece, n_pieces}: pieces of the split form
+  int64_t split_keys;   // [n_split][2] {first key, last key + 1}
+  int64_t join_items;   // [n_join][4] {sequence, first row, first piece (index into split_items), n_pieces}
+  int64_t dq_items;     // [n_dq][2] {sequence, first query}: fine-tuning samples, most keys first
+  int64_t dk_items;     // [n_dk][2] {sequence, first key}: fine-tuning samples, most queries first
+  int64_t f32_dq_items; // the same in fp32 tiles
+  int64_t f32_dk_items;
+  int64_t total_words;
+};
+
+}  // namespace dsv
+
+struct dsv_attn_plan {
+  int32_t n_seqs = 0, n_q = 0, n_kv = 0, hq = 0, hkv = 0, d = 0;
+  int64_t train_q = 0, train_k = 0;
+  int32_t n_fwd = 0, n_f32 = 0, n_split = 0, n_join = 0, n_dq = 0, n_dk = 0, n_f32_dq = 0, n_f32_dk = 0;
+  std::vector<int32_t> meta;  // packed blob, host image
+  dsv::AttnLayout lay{};
+  void* d_meta = nullptr;     // device copy (nullptr: host-only plan)
+  void* copy_done = nullptr;  // hipEvent_t recorded after the upload
+  const int32_t* dptr(int64_t off) const { return static_cast<const int32_t*>(d_meta) + off; }
+};
