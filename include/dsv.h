@@ -615,6 +615,50 @@ int dsv_attn_bwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const
                  const dsv_attn_view* dO, const dsv_attn_view* dQ, const dsv_attn_view* dK,
                  const dsv_attn_view* dV, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Vocabulary loss: softmax cross entropy of rows against a large vocabulary, from the
+ * rows' last hidden state and the head's weight, with the gradient that reaches the
+ * rows (the start of the fine-tuning rows' backward; the head is frozen like every
+ * base weight here).  For row x with target t, z = x W^T over the vocabulary:
+ *     loss = log sum_v exp z_v - z_t
+ *     dx   = weight (sum_v softmax(z)_v W_v - W_t)
+ * A target outside [0, V) marks a row without one (a prompt's token): its loss is 0 and
+ * its dx zeros, whatever the row holds.  The logits are never held whole: the
+ * vocabulary is taken in pieces, whose exponentials, relative to a reference that a
+ * row carries from piece to piece, are at once summed and multiplied with the
+ * head again.  The target's own term is kept apart in fp32, so a loss near 0 and its
+ * gradient keep their relative accuracy.
+ * In bf16 mode the products run on bf16 operands with fp32 sums, the exponentials
+ * being rounded to bf16 once for the second one; losses are fp32 in both types.  No
+ * atomics: repeated calls give the same bits.
+ *
+ * X [T][K], dX [T][K], W [V][K] and Wt [K][V] of dtype, their row strides in elements
+ * (0: dense, else at least the row length, a multiple of 8, at most 2^20).  K is a
+ * positive multiple of 8, at most 2^20; T >= 0; 1 <= V <= 2^24.  Pointers are 16-byte
+ * aligned; target [T] int32, loss [T] and weight [T] fp32 (4-byte aligned).
+ */
+
+/* Device workspace of dsv_vocab_loss (grad = 0) or dsv_vocab_loss_grad (grad = 1);
+ * ldw as passed to the call. */
+int dsv_vocab_workspace(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_t ldw, int32_t grad,
+                        size_t* bytes);
+
+/* The losses alone (scoring): the head is read once.  Errors: DSV_ERR_ARG (null or
+ * misaligned pointer, T < 0), DSV_ERR_RANGE (dtype), DSV_ERR_SIZE (shape, stride,
+ * workspace). */
+int dsv_vocab_loss(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const void* X, int32_t ldx, const void* W,
+                   int32_t ldw, const int32_t* target, float* loss, void* workspace, size_t workspace_bytes,
+                   void* hip_stream);
+
+/* Losses (NULL: not written) and dX.  weight NULL: ones; the losses are not
+ * multiplied by it.  Wt (optional, bf16): the head transposed, the same values, for a
+ * second product that reads it contraction-contiguous; used where V is a multiple of
+ * 8, else, and for fp32, ignored.  Errors as dsv_vocab_loss. */
+int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const void* X, int32_t ldx, const void* W,
+                        int32_t ldw, const void* Wt, int32_t ldwt, const int32_t* target, const float* weight,
+                        float* loss, void* dX, int32_t lddx, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
 /* Static description of a status code. */
 const char* dsv_status_string(int status);
 

@@ -1,0 +1,209 @@
+// gemm_tile.h -- the contraction loop of a 256-column bf16 tile (v_mfma_f32_16x16x32_bf16) as a function
+// that leaves the fp32 sums in registers for the caller's epilogue.
+//
+// 4 waves in a 2 x 2 grid, each FM x 8 blocks of 16 x 16 (FM 8: 256 rows, FM 4: 128).  Operand tiles go
+// from global memory straight into LDS, two buffers; one barrier per step of 64.  Rows and columns past
+// the operands, and contraction values past C, read zeros.
+//   NT: out[m][n] = sum_c P[m][c] Q[n][c]      NN: out[m][n] = sum_c P[m][c] Q[c][n]
+// Sums: acc[i][j][v] is row wm * 16 FM + 16 i + l % 16, column wn * 128 + 16 j + 4 (l / 16) + v.
+#pragma once
+
+#include "device_common.h"
+
+namespace dsv {
+namespace {
+
+extern "C" __device__ void llvm_amdgcn_raw_buffer_load_lds_t(i32x4 rsrc, lds_u32* lds, int size, int voffset,
+                                                             int soffset, int offset,
+                                                             int aux) __asm("llvm.amdgcn.raw.buffer.load.lds");
+
+constexpr int kTileStage = 2 * 256 * 64 * 2;  // bytes of one buffer (FM 8)
+
+// Descriptor over `bytes` bytes (at most 2^31) from base.
+__device__ __forceinline__ i32x4 tile_rsrc(const void* base, int64_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  i32x4 r;
+  r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+  r.y = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+  r.z = __builtin_amdgcn_readfirstlane((int)(bytes > 0 ? bytes : 0));
+  r.w = 0x00020000;
+  return r;
+}
+
+// Consecutive workgroup ids go round the 8 XCDs: each gets a contiguous range of tiles.
+__device__ __forceinline__ int tile_of(int bid, int n) {
+  const int per = n >> 3, rem = n & 7, xcd = bid & 7;
+  return xcd * per + min(xcd, rem) + (bid >> 3);
+}
+
+// Tile -> (row tile, column tile): groups of 4 row tiles, column by column.
+__device__ __forceinline__ void tile_at(int lin, int n_m, int n_n, int& mt, int& nt) {
+  const int span = 4 * n_n, grp = lin / span, first = grp * 4, size = min(n_m - first, 4);
+  mt = first + (lin % span) % size;
+  nt = (lin % span) / size;
+}
+
+// P: the tile's first row; p_rows, q_cols: rows and columns that exist; C: contraction length.
+// Returns the buffer that the last step did not use.
+template <bool NN, int FM>
+__device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, int p_rows, const uint16_t* Q, int64_t ldq_,
+                                              int q_cols, int C, char* smem0, char* smem1, f32x4 (&acc)[FM][8]) {
+  constexpr int WM = 16 * FM, TM = 2 * WM, TN = 256, TK = 64, FN = 8, ROWB = TK * 2;
+  constexpr int A_BYTES = TM * ROWB, LOADS = 8, LOADS_A = FM;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, lr = lane >> 3;
+  const int ld = (int)ldp, ldq = (int)ldq_, nk = (C + TK - 1) / TK;
+  auto buf = [&](int stage) { return stage ? smem1 : smem0; };
+  auto rswz = [](int row) { return (row ^ (row >> 3)) & 7; };
+  const i32x4 ra = tile_rsrc(P, (int64_t)min(TM, p_rows) * ld * 2);
+  const i32x4 rb = NN ? tile_rsrc(Q, ((int64_t)C * ldq - (ldq - q_cols)) * 2) : tile_rsrc(Q, (int64_t)min(TN, q_cols) * ldq * 2);
+  int voff_a[LOADS_A], voff_b[NN ? 2 : LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS_A; ++i) voff_a[i] = ((((lane & 7) ^ lr ^ ((LOADS_A * wave + i) & 7)) << 4)) + lr * ld * 2;
+  if constexpr (NN) {
+#pragma unroll
+    for (int par = 0; par < 2; ++par)
+      voff_b[par] = ((lane >> 5) * ldq + 8 * ((lane & 31) ^ 2 * ((2 * par + (lane >> 5)) & 3))) * 2;
+  } else {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) voff_b[i] = (((lane & 7) ^ lr ^ i) << 4) + lr * ldq * 2;
+  }
+  auto load_a = [&](int kt, char* st, int i) {
+    const int q = wave * LOADS_A + i;
+    llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16, voff_a[i],
+                                      __builtin_amdgcn_readfirstlane(q * 16 * ld + kt * TK * 2), 0, 0);
+  };
+  auto load_b = [&](int kt, char* st, int i) {
+    const int q = wave * LOADS + i;
+    if constexpr (NN)
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i & 1],
+                                        __builtin_amdgcn_readfirstlane((kt * TK + 2 * q) * ldq * 2), 0, 0);
+    else
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i],
+                                        __builtin_amdgcn_readfirstlane(q * 16 * ldq + kt * TK * 2), 0, 0);
+  };
+  // any step: chunks past the contraction read zeros (C is a multiple of 8)
+  auto issue = [&](int kt, int stage) {
+    const int k0 = kt * TK;
+    char* st = buf(stage);
+    const bool whole = k0 + TK <= C;
+#pragma unroll
+    for (int i = 0; i < LOADS_A; ++i) {
+      if (whole) {
+        load_a(kt, st, i);
+        continue;
+      }
+      const int q = wave * LOADS_A + i, row = 8 * q + lr, c = (lane & 7) ^ rswz(row);
+      const int vo = k0 + 8 * c < C ? (row * ld + k0 + 8 * c) * 2 : (int)0x7FFFFFF0;
+      llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16, vo, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      if (whole || NN) {  // NN: rows past the contraction lie past the descriptor
+        load_b(kt, st, i);
+        continue;
+      }
+      const int q = wave * LOADS + i, row = 8 * q + lr, c = (lane & 7) ^ rswz(row);
+      const int vo = k0 + 8 * c < C ? (row * ldq + k0 + 8 * c) * 2 : (int)0x7FFFFFF0;
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, vo, 0, 0, 0);
+    }
+  };
+  issue(0, 0);
+  if (nk > 1) issue(1, 1);
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Fragment addresses: a lane part picked by the step and block (the chunk swizzle), plus an immediate.
+  const int lanepart = (lane >> 4) ^ (l15 & 7) ^ (l15 >> 3);
+  int off_a[4], off_b[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    off_a[c] = (wm * WM + l15) * ROWB + 16 * (lanepart ^ (2 * c));
+    off_b[c] = NN ? A_BYTES + (8 * (lane >> 4) + (l15 >> 2)) * (TN * 2) + 256 * wn + 32 * (c ^ (l15 >> 2)) +
+                        16 * ((l15 & 3) >> 1) + 8 * (l15 & 1)
+                  : A_BYTES + (wn * 128 + l15) * ROWB + 16 * (lanepart ^ (2 * c));
+  }
+  auto rd_a = [&](const char* st, int s, int i) {
+    return as_bf(*reinterpret_cast<const u32x4*>(st + off_a[((2 * s) ^ i) & 3] + 16 * i * ROWB));
+  };
+  auto rd_b = [&](const char* st, int s, int j) {
+    if constexpr (NN) {
+      typedef uint32_t u32x2t __attribute__((ext_vector_type(2)));
+      const char* p = st + off_b[j & 3] + 128 * (j >> 2) + s * 32 * (TN * 2);
+      const u32x2t a0 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+      const u32x2t a1 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * (TN * 2))));
+      return as_bf(u32x4{a0[0], a0[1], a1[0], a1[1]});
+    } else {
+      return as_bf(*reinterpret_cast<const u32x4*>(st + off_b[((2 * s) ^ j) & 3] + 16 * j * ROWB));
+    }
+  };
+  bf16x8 fa0[FM], fa1[FM], fb[FN];
+  if (nk >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS_A + LOADS));  // the first step has landed
+  else vmem_wait_all();
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < FN; ++j) fb[j] = rd_b(smem0, 0, j);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) fa0[i] = rd_a(smem0, 0, i);
+  // 32 contraction values with fragments (cur, fb), a column block at a time; per block two of the loads of
+  // step kl into buffer ls, and the reads that replace the fragments it is done with.
+  auto half = [&](bf16x8 (&cur)[FM], bf16x8 (&nxt)[FM], const char* st_next, int s_next, bool load, int kl, int ls) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], cur[i], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int e = 2 * j; e < 2 * j + 2; ++e)
+        if (load && e < LOADS_A + LOADS) {
+          if (e < LOADS_A) load_a(kl, buf(ls), e < LOADS_A ? e : 0);
+          else load_b(kl, buf(ls), e - LOADS_A);
+        }
+      if (j < FM / 2) {
+        nxt[2 * j] = rd_a(st_next, s_next, 2 * j);
+        nxt[2 * j + 1] = rd_a(st_next, s_next, 2 * j + 1);
+      }
+      fb[j] = rd_b(st_next, s_next, j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Step kt in buffer `stage`, another one to follow: the barrier between its halves publishes kt + 1 and
+  // frees the buffer, which kt + 2 is loaded into.
+  auto kstep = [&](int kt, int stage, bool load) {
+    half(fa0, fa1, buf(stage), 1, false, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    vmem_wait_all();
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    if (!load && kt + 2 < nk) issue(kt + 2, stage);  // a partial last step
+    half(fa1, fa0, buf(stage ^ 1), 0, load, kt + 2, stage);
+  };
+  int kt = 0, stage = 0;
+  const int main_end = C / TK - 2;  // kt < main_end: step kt + 2 is whole
+  if constexpr (NN) {
+    for (; kt + 1 < main_end; kt += 2) {  // pairs: the buffers are constants at every use
+      kstep(kt, 0, true);
+      kstep(kt + 1, 1, true);
+    }
+    if (kt < main_end) {
+      kstep(kt, 0, true);
+      ++kt;
+      stage = 1;
+    }
+  } else {
+    for (; kt < main_end; ++kt, stage ^= 1) kstep(kt, stage, true);
+  }
+  for (; kt + 1 < nk; ++kt, stage ^= 1) kstep(kt, stage, false);
+  half(fa0, fa1, buf(stage), 1, false, 0, 0);
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa1[i], acc[i][j], 0, 0, 0);
+  return buf(stage ^ 1);
+}
+
+}  // namespace
+}  // namespace dsv

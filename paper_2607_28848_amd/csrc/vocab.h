@@ -1,0 +1,47 @@
+// vocab.h -- arguments and host launchers of the vocabulary loss's kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace dsv {
+
+// One piece of the vocabulary: columns [v0, v0 + vn) of the logits, in column tiles of `tw`.
+struct VocabArgs {
+  int32_t T, K, V;
+  const void* X;
+  const void* W;
+  const void* Wt;         // nullptr: the second product reads W
+  int64_t ldx, ldw, ldwt, lddx;
+  const int32_t* target;
+  const float* weight;    // nullptr: ones
+  float* loss;            // nullptr: not written
+  void* dX;
+  int32_t v0, vn;
+  int32_t tw, n_ct;       // width and number of the piece's column tiles
+  int32_t first, last;    // the piece is the first / the last
+  int32_t grad;
+  // Exponents are base 2: a row's reference r stands for 2^r.
+  void* P;                // [T][ldp] 2^(z log2 e - reference) of the piece, the target's left out (grad)
+  int64_t ldp;
+  float2* stats;          // [T][ld_stats] per column tile: reference, sum of its P
+  int64_t ld_stats;
+  float* ref;             // [T] the row's reference
+  float* others;          // [T] sum of the terms that are not the target's, at the reference
+  float* zt;              // [T] the target's logit
+  float* alpha;           // [T] what the sums so far are multiplied by (the reference moved)
+  // second product: contraction in `split` ranges of split_len columns, each with its own sums
+  float* O;               // [split][T][K]
+  int32_t split, split_len;
+};
+
+// A tile whose largest logit (base 2) exceeds the row's reference by more than this takes its own
+// maximum as reference: terms stay below 2^kVocabSlack, and all but a row's first pieces keep the
+// reference they find, so their terms need no second look.
+constexpr float kVocabSlack = 24.f;
+
+hipError_t launch_vocab_f32_logits(const VocabArgs& a, hipStream_t s);
+hipError_t launch_vocab_f32_grad(const VocabArgs& a, hipStream_t s);
+
+}  // namespace dsv
