@@ -43,12 +43,12 @@ struct Seq {
 // (ids go round the 8 XCDs) when the key heads are 8, and share K and V in its L2.
 __device__ __forceinline__ int head_of(const AttnArgs& a, int x) { return (x % a.hkv) * a.group + x / a.hkv; }
 
-// LDS image of staged rows (D bf16 each): 16-byte chunk c of row r sits in slot c ^ swz(r).  Eight
-// consecutive rows put one chunk in eight different bank groups (fragment reads), four consecutive rows
-// put a pair of chunks in four (transposing reads).
+// LDS image of staged rows (D bf16 each): 16-byte chunk c of row r sits in slot c ^ swz(r).  Of the 64 banks'
+// 256 bytes, 16 consecutive rows put one chunk in 16 different 16-byte groups (fragment reads), and four
+// consecutive rows put four neighbouring chunks in four different 64-byte groups (transposing reads).
 template <int D>
-__device__ __forceinline__ int swz(int r) {
-  return ((r & 3) << 1) | ((r >> 2) & 1) | (D == 128 ? r & 8 : 0);
+__device__ __forceinline__ constexpr int swz(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
 // Descriptor over rows [r0, r_end) of a head (reads past them return zeros); rows are at most 64 at a
@@ -66,11 +66,10 @@ __device__ __forceinline__ i32x4 rows_rsrc(const AttnView& t, int64_t row, int h
 
 // Rows [0, ROWS) of the descriptor into LDS, the work shared by NW waves.
 template <int D, int ROWS, int NW>
-__device__ __forceinline__ void stage(const i32x4& rs, int row_bytes, char* lds, int wave) {
+__device__ __forceinline__ void stage(const i32x4& rs, int row_bytes, char* lds, int wave, int lane = threadIdx.x & 63) {
   constexpr int RB = 2 * D, RPL = 1024 / RB, CH = RB / 16;  // row bytes, rows a load, chunks a row
   constexpr int N = ROWS / RPL / NW;
   static_assert(N * RPL * NW == ROWS, "rows");
-  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int q = wave * N + i;
@@ -80,23 +79,31 @@ __device__ __forceinline__ void stage(const i32x4& rs, int row_bytes, char* lds,
   }
 }
 
-// Fragment of rows 32 u ..: lane's row 32 u + l % 32, its 8 values of step s.
+// The lane's number, read afresh: what is derived from it cannot be kept in registers across uses.
+__device__ __forceinline__ int fresh_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
+// Fragment of rows 32 u ..: lane's row 32 u + l % 32, its 8 values of step s.  Steps and blocks of columns
+// change single bits of the lane's slot, so an address is the lane's own part xor a constant.
 template <int D>
-__device__ __forceinline__ bf16x8 frag(const char* lds, int u, int s) {
-  const int lane = threadIdx.x & 63, r = 32 * u + (lane & 31);
-  return as_bf(*reinterpret_cast<const u32x4*>(lds + r * 2 * D + 16 * ((2 * s + (lane >> 5)) ^ swz<D>(r))));
+__device__ __forceinline__ bf16x8 frag(const char* lds, int u, int s, int lane = threadIdx.x & 63) {
+  const int r = lane & 31, own = r * 2 * D + 16 * ((lane >> 5) ^ swz<D>(r));
+  return as_bf(*reinterpret_cast<const u32x4*>(lds + (own ^ (32 * s)) + u * 64 * D));
 }
 
 // Transposed fragment: lane's column 32 t + l % 32 of rows 16 w + 4 (l / 32) + {0..3} and 8 further on.
 template <int D>
-__device__ __forceinline__ bf16x8 frag_t(const char* lds, int w, int t) {
-  const int lane = threadIdx.x & 63, lam = lane & 15;
-  const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lam & 3) >> 1);
+__device__ __forceinline__ bf16x8 frag_t(const char* lds, int w, int t, int lane = threadIdx.x & 63) {
+  const int lam = lane & 15, r = 4 * (lane >> 5) + (lam >> 2);
+  const int own = r * 2 * D + 16 * ((2 * ((lane >> 4) & 1) + ((lam & 3) >> 1)) ^ swz<D>(r)) + 8 * (lam & 1);
+  static_assert(swz<D>(8) == 2 && swz<D>(16) == 0, "row 8 on: slot bit 1");
   u32x4 v;
 #pragma unroll
   for (int hh = 0; hh < 2; ++hh) {
-    const int r = 16 * w + 8 * hh + 4 * (lane >> 5) + (lam >> 2);
-    const char* p = lds + r * 2 * D + 16 * (c ^ swz<D>(r)) + 8 * (lam & 1);
+    const char* p = lds + (own ^ (64 * t + 32 * hh)) + (16 * w + 8 * hh) * 2 * D;
     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
     v[2 * hh] = (uint32_t)(uint16_t)x[0] | ((uint32_t)(uint16_t)x[1] << 16);
     v[2 * hh + 1] = (uint32_t)(uint16_t)x[2] | ((uint32_t)(uint16_t)x[3] << 16);
@@ -110,6 +117,20 @@ __device__ __forceinline__ void row_frags(const AttnView& t, int64_t row, int h,
   const uint16_t* p = static_cast<const uint16_t*>(t.ptr) + row * t.row + h * t.head + 8 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) f[s] = as_bf(in ? ld16(p + 16 * s) : zero4());
+}
+
+// Scheduling of a run of N matrix instructions that consume DS LDS reads each: the reads of the first `ahead`
+// of them, then one instruction and the reads of a later one by turns, so that no instruction waits for
+// the read before it.
+template <int N, int DS, int AHEAD>
+__device__ __forceinline__ void feed() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * DS, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, DS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
 // The larger / the sum of the two lanes that share a column.
@@ -145,11 +166,10 @@ struct Running {
   float ref = -INFINITY, sum = 0.f;
 };
 
-// Scores x (16 N per lane, masked ones -inf) to exp2(c x - ref), with the sums and acc moved to a new
-// reference where a score exceeds the old one by more than 2^8: what leaves the reference alone is bounded
-// by that, and all but the first blocks of a row do.
+// Moves the reference (and with it the sums and acc) where a score c x exceeds it by more than 2^8: terms are
+// bounded by that, and all but the first blocks of a row leave the reference as it is.
 template <int N, int NA>
-__device__ __forceinline__ void softmax_step(f32x16 (&x)[N], float c, Running& r, f32x16 (&acc)[NA]) {
+__device__ __forceinline__ void softmax_ref(const f32x16 (&x)[N], float c, Running& r, f32x16 (&acc)[NA]) {
   float mx = x[0][0];
 #pragma unroll
   for (int u = 0; u < N; ++u)
@@ -164,14 +184,18 @@ __device__ __forceinline__ void softmax_step(f32x16 (&x)[N], float c, Running& r
 #pragma unroll
     for (int t = 0; t < NA; ++t) acc[t] *= f;
   }
-  const float ref = r.ref == -INFINITY ? 0.f : r.ref;  // no key seen so far: every term is exp2(-inf) = 0
+}
+
+// Values 8 w .. of a block's scores to terms exp2(c x - ref), into the sum and, as bf16, the second product's
+// operand.  base: the reference, 0 where no key was seen so far (every term is exp2(-inf) = 0 then).
+__device__ __forceinline__ bf16x8 softmax_terms(const f32x16& x, int w, float c, float base, float& sum) {
+  f32x16 e;
 #pragma unroll
-  for (int u = 0; u < N; ++u)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      x[u][v] = __builtin_amdgcn_exp2f(x[u][v] * c - ref);
-      r.sum += x[u][v];
-    }
+  for (int v = 0; v < 8; ++v) {
+    e[v] = __builtin_amdgcn_exp2f(x[8 * w + v] * c - base);
+    sum += e[v];
+  }
+  return pack8(e, 0);
 }
 
 __device__ __forceinline__ float lse_of(float ref, float sum) {
@@ -193,7 +217,7 @@ __device__ __forceinline__ void store_cols(const AttnView& t, int64_t row, int h
 
 // ---------------------------------------------------------------------------------------------------
 template <int D>
-__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
   __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
@@ -226,26 +250,41 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
     if (kt + TK < k_end) load(kt + TK, nxt);
     if (kt >= wave_end) return;
     f32x16 x[2];
+    x[0] = x[1] = zero16();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      x[u] = zero16();
+    for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x[u], 0, 0, 0);
-    }
+      for (int u = 0; u < 2; ++u) x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x[u], 0, 0, 0);
+    feed<D / 8, 1, 4>();
+    __builtin_amdgcn_sched_barrier(0);
     if (kt + TK - 1 > wave_all) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[u][v] = kt + 32 * u + tile_row(v) <= seen ? x[u][v] : -INFINITY;
     }
-    softmax_step(x, c, run, acc);
+    softmax_ref(x, c, run, acc);
+    const float base = run.ref == -INFINITY ? 0.f : run.ref;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const bf16x8 p = pack8(x[w >> 1], w & 1);
+      const bf16x8 p = softmax_terms(x[w >> 1], w & 1, c, base, run.sum);
 #pragma unroll
       for (int t = 0; t < D / 32; ++t)
         acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, acc[t], 0, 0, 0);
     }
+    // the terms of 16 keys are formed between the products of the 16 before
+    __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, 28, 0);
+#pragma unroll
+    for (int i = 0; i < 3 * D / 32; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 28 * 32 / D, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, D / 32, 0);
+    __builtin_amdgcn_sched_barrier(0);
   };
   for (int kt = 0; kt < k_end; kt += 2 * TK) {
     step(kt, b0, b1);
@@ -313,10 +352,11 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
       for (int v = 0; v < 16; ++v)
         x[0][v] = kt + tile_row(v) <= seen && kt + tile_row(v) < k_last ? x[0][v] : -INFINITY;
     }
-    softmax_step(x, c, run, acc);
+    softmax_ref(x, c, run, acc);
+    const float base = run.ref == -INFINITY ? 0.f : run.ref;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const bf16x8 p = pack8(x[0], w);
+      const bf16x8 p = softmax_terms(x[0], w, c, base, run.sum);
 #pragma unroll
       for (int t = 0; t < D / 32; ++t)
         acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, acc[t], 0, 0, 0);
@@ -417,7 +457,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // ---------------------------------------------------------------------------------------------------
 template <int D>
-__global__ __launch_bounds__(256) void attn_dq_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
   __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
@@ -493,88 +533,140 @@ __global__ __launch_bounds__(256) void attn_dq_kernel(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------
-// dK and dV of 128 keys of one key head, 32 a wave, over 32 queries at a time, the key head's query
-// heads one after the other: the sums over them stay in registers.
+// dK and dV of 128 keys of one key head over 64 queries at a time, the key head's query heads one after
+// the other: the sums over them stay in registers.
+//
+// Two waves share 32 keys, each with the sums of one output (32 x D, as many registers as one wave can
+// keep beside another one on its SIMD): wave w forms p and dV, wave w + 4 do . v and dK. p goes from one to
+// the other through LDS, lane to lane, in bf16 (as dV's product takes it), a step late: in step n the
+// second wave multiplies dO(n) with V and closes ds(n - 1), for which Q is kept for one step more.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dk_kernel(AttnArgs a) {
-  constexpr int TQ = 32, TILE = TQ * 2 * D;
-  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
-  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
-  __shared__ __attribute__((aligned(16))) float st[2][2][TQ];  // [buffer][lse (base 2), delta]
+__global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
+  constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ;  // PB: p of 4 x 32 keys
+  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE + PB];
+  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE + PB];
+  __shared__ __attribute__((aligned(1024))) char b2[2 * TILE + PB];
+  __shared__ __attribute__((aligned(16))) float st[3][2][TQ];  // [buffer][lse (base 2), delta]
   const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool second = wave >= 4;
+  const int blk = wave & 3;
   const int off = s.kl - s.ql;
-  const int k = k0 + 32 * wave + (lane & 31);
+  const int k = k0 + 32 * blk + (lane & 31);
   const bool in = k < s.kl;
   const int qrow = (int)a.Q.row * 2, drow = (int)a.dO.row * 2;
   const int q_first = max(0, k0 - off);
   const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, steps = per_head * a.group;
+  // The last queries first, one query head after the other: the workgroups of a sequence's key tiles run
+  // through the same rows at the same time, whatever their first query, and share them in L2 (heads
+  // outside and queries upwards missed more than half of its lines and took ...).
+  auto q_of = [&](int n) { return q_first + (per_head - 1 - n / a.group) * TQ; };
   float st_next = 0.f;  // of the next step: lse (threads 0 ..), delta (threads TQ ..)
-  auto load = [&](int n, char* b) {
-    const int h = hk * a.group + n / per_head, qt = q_first + n % per_head * TQ;
-    stage<D, TQ, 4>(rows_rsrc(a.Q, (int64_t)s.q0 + qt, h, min(TQ, s.ql - qt), D), qrow, b, wave);
-    stage<D, TQ, 4>(rows_rsrc(a.dO, (int64_t)s.cq + qt, h, min(TQ, s.ql - qt), D), drow, b + TILE, wave);
-    // queries past the last one: lse of +infinity makes their p and ds zero
+  auto load = [&](int n, char* b, int ln) {
+    const int h = hk * a.group + n % a.group, qt = q_of(n);
+    stage<D, TQ, 8>(rows_rsrc(a.Q, (int64_t)s.q0 + qt, h, min(TQ, s.ql - qt), D), qrow, b, wave, ln);
+    stage<D, TQ, 8>(rows_rsrc(a.dO, (int64_t)s.cq + qt, h, min(TQ, s.ql - qt), D), drow, b + TILE, wave, ln);
+    // queries past the last one: lse of +infinity makes their p zero
     if (threadIdx.x < 2 * TQ) {
       const int r = threadIdx.x & (TQ - 1), q = qt + r;
       if (threadIdx.x < TQ) st_next = q < s.ql ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : INFINITY;
       else st_next = q < s.ql ? a.delta[h * a.train_q + s.cq + q] : 0.f;
     }
   };
-  if (steps > 0) load(0, b0);
-  bf16x8 kf[D / 16], vf[D / 16];
-  row_frags<D>(a.K, (int64_t)s.k0 + k, hk, in, kf);
-  row_frags<D>(a.V, (int64_t)s.k0 + k, hk, in, vf);
-  f32x16 dk[D / 32], dv[D / 32];
+  if (steps > 0) load(0, b0, lane);
+  bf16x8 kv[D / 16];  // the lane's key: K (first wave) or V
+  row_frags<D>(second ? a.V : a.K, (int64_t)s.k0 + k, hk, in, kv);
+  f32x16 acc[D / 32];  // dV or dK
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zero16();
+  for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
+  f32x16 dp[2];  // second wave: do . v of the step before
+  dp[0] = dp[1] = zero16();
   const float c = a.scale * kLog2e;
-  auto step = [&](int n, int b, const char* cur, char* nxt) {
+  // step n in buffer `cur` (index b), the step before in `old`
+  auto step = [&](int n, int b, char* cur, const char* old, char* nxt) {
     vmem_wait_all();
     if (threadIdx.x < 2 * TQ) st[b][threadIdx.x / TQ][threadIdx.x & (TQ - 1)] = st_next;
     __syncthreads();
-    if (n + 1 < steps) load(n + 1, nxt);
-    const int qt = q_first + n % per_head * TQ;
-    f32x16 x = zero16(), dp = zero16();
+    // the three buffers lie further apart than an LDS offset reaches: kept in registers, three sets of
+    // addresses spill
+    const int ln = fresh_lane();
+    if (n + 1 < steps) load(n + 1, nxt, ln);
+    if (!second) {
+      if (n == steps) return;
+      const int qt = q_of(n);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, 0, i), kf[i], x, 0, 0, 0);
+      for (int u = 0; u < 2; ++u) {
+        f32x16 x = zero16();
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, 0, i), vf[i], dp, 0, 0, 0);
-    const bool cut = k0 + 32 * wave + 31 > qt + off;
+        for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i, ln), kv[i], x, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 8 * i + 4 * (lane >> 5);
-      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st[b][0][r]), d4 = *reinterpret_cast<const f32x4*>(&st[b][1][r]);
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st[b][0][32 * u + 8 * i + 4 * (ln >> 5)]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v = 4 * i + e;
-        float p = __builtin_amdgcn_exp2f(x[v] * c - l4[e]);
-        if (cut) p = k <= qt + r + e + off ? p : 0.f;
-        x[v] = p;
-        dp[v] = cut && k > qt + r + e + off ? 0.f : p * (dp[v] - d4[e]);
+          for (int e = 0; e < 4; ++e) x[4 * i + e] = __builtin_amdgcn_exp2f(x[4 * i + e] * c - l4[e]);
+        }
+        if (k0 + 32 * blk + 31 > qt + 32 * u + off) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = k <= qt + 32 * u + tile_row(v) + off ? x[v] : 0.f;
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const bf16x8 p = pack8(x, w);
+          *reinterpret_cast<u32x4*>(cur + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16) = __builtin_bit_cast(u32x4, p);
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t)
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, 2 * u + w, t, ln), p, acc[t], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return;
+    }
+    if (n > 0) {
+      const int ob = b == 0 ? 2 : b - 1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const u32x4 p = *reinterpret_cast<const u32x4*>(old + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const f32x4 d4 = *reinterpret_cast<const f32x4*>(&st[ob][1][32 * u + 16 * w + 8 * i + 4 * (ln >> 5)]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t pw = p[2 * i + e / 2];
+              const float pf = __uint_as_float(e & 1 ? pw & 0xffff0000u : pw << 16);
+              dp[u][8 * w + 4 * i + e] = pf * (dp[u][8 * w + 4 * i + e] - d4[e]);
+            }
+          }
+          const bf16x8 ds = pack8(dp[u], w);
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t)
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(old, 2 * u + w, t, ln), ds, acc[t], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if (n < steps) {
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const bf16x8 p = pack8(x, w), ds = pack8(dp, w);
+      for (int u = 0; u < 2; ++u) {
+        dp[u] = zero16();
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t)
-        dv[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, dv[t], 0, 0, 0);
-#pragma unroll
-      for (int t = 0; t < D / 32; ++t)
-        dk[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur, w, t), ds, dk[t], 0, 0, 0);
+        for (int i = 0; i < D / 16; ++i)
+          dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, u, i, ln), kv[i], dp[u], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
-  for (int n = 0; n < steps; n += 2) {
-    step(n, 0, b0, b1);
-    if (n + 1 < steps) step(n + 1, 1, b1, b0);
+  for (int n = 0; n <= steps; n += 3) {
+    step(n, 0, b0, b2, b1);
+    if (n + 1 <= steps) step(n + 1, 1, b1, b0, b2);
+    if (n + 2 <= steps) step(n + 2, 2, b2, b1, b0);
   }
   if (!in) return;
-  store_cols<D>(a.dK, (int64_t)s.ck + k, hk, dk, a.scale);
-  store_cols<D>(a.dV, (int64_t)s.ck + k, hk, dv, 1.f);
+  if (second) store_cols<D>(a.dK, (int64_t)s.ck + k, hk, acc, a.scale);
+  else store_cols<D>(a.dV, (int64_t)s.ck + k, hk, acc, 1.f);
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -641,9 +733,9 @@ AttnArgs common(const dsv_attn_plan& p, double scale) {
 int status(hipError_t e) { return e == hipSuccess ? DSV_OK : DSV_ERR_DEVICE; }
 
 template <typename K>
-hipError_t launch(K k64, K k128, const AttnArgs& a, int64_t groups, hipStream_t s) {
+hipError_t launch(K k64, K k128, const AttnArgs& a, int64_t groups, hipStream_t s, int threads = 256) {
   if (groups <= 0) return hipSuccess;
-  hipLaunchKernelGGL(a.d == 64 ? k64 : k128, dim3((unsigned)groups), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(a.d == 64 ? k64 : k128, dim3((unsigned)groups), dim3((unsigned)threads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -726,5 +818,5 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   a.items = p->dptr(f32 ? p->lay.f32_dk_items : p->lay.dk_items);
   a.n_items = f32 ? p->n_f32_dk : p->n_dk;
   return status(f32 ? launch_attn_f32_dk(a, s)
-                    : launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, (int64_t)a.n_items * p->hkv, s));
+                    : launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, (int64_t)a.n_items * p->hkv, s, 512));
 }
