@@ -23,7 +23,8 @@ struct AttnArgs {
   float scale;           // of the scores
   AttnView Q, K, V, O, dO, dQ, dK, dV;
   float* lse;            // nullptr: not written (forward)
-  float* delta;          // do . o of the compact rows
+  float* delta;          // do . o of the compact rows, [hq][train_q]
+  float* lse2;           // bf16: lse of the compact rows, base 2
   // split form
   const int32_t* split_keys;
   const int32_t* join_items;

@@ -64,18 +64,29 @@ __device__ __forceinline__ i32x4 rows_rsrc(const AttnView& t, int64_t row, int h
   return r;
 }
 
-// Rows [0, ROWS) of the descriptor into LDS, the work shared by NW waves.
+__device__ __forceinline__ i32x4 flat_rsrc(const void* base, int bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  i32x4 r;
+  r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+  r.y = __builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+  r.z = __builtin_amdgcn_readfirstlane(bytes);
+  r.w = 0x00020000;
+  return r;
+}
+
+// Rows [0, ROWS) of the descriptor into LDS, the work shared by NW waves.  A load fills 1 KiB of the image: RPL
+// rows; row blocks go in the scalar offset and change the lane's slot by a constant xor.
 template <int D, int ROWS, int NW>
 __device__ __forceinline__ void stage(const i32x4& rs, int row_bytes, char* lds, int wave, int lane = threadIdx.x & 63) {
   constexpr int RB = 2 * D, RPL = 1024 / RB, CH = RB / 16;  // row bytes, rows a load, chunks a row
   constexpr int N = ROWS / RPL / NW;
-  static_assert(N * RPL * NW == ROWS, "rows");
+  static_assert(N > 0 && N * RPL * NW == ROWS, "rows");
+  const int own = 16 * ((lane % CH) ^ swz<D>(lane / CH)), row = lane / CH * row_bytes;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int q = wave * N + i;
-    const int r = q * RPL + lane / CH;
-    const int c = (lane % CH) ^ swz<D>(r);
-    llvm_amdgcn_raw_buffer_load_lds_a(rs, (lds_u32*)(lds + q * 1024), 16, r * row_bytes + 16 * c, 0, 0, 0);
+    llvm_amdgcn_raw_buffer_load_lds_a(rs, (lds_u32*)(lds + q * 1024), 16, (own ^ (16 * swz<D>(q * RPL % 16))) + row,
+                                      __builtin_amdgcn_readfirstlane(q * RPL * row_bytes), 0, 0);
   }
 }
 
@@ -132,6 +143,23 @@ __device__ __forceinline__ void feed() {
   }
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
+
+// The same with V vector instructions (of other values) after each matrix instruction.
+template <int N, int DS, int AHEAD, int V>
+__device__ __forceinline__ void feed_beside() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * DS, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i < N - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, DS, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, V, 0);
+  }
+}
+
+template <bool B>
+struct bool_c {  // a compile-time flag passed as a value
+  static constexpr bool value = B;
+};
 
 // The larger / the sum of the two lanes that share a column.
 __device__ __forceinline__ float pair_max(float x) {
@@ -471,8 +499,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   const int k_end = min(s.kl, min(qt + kAttnBwdRows, s.ql) + off);
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
   auto load = [&](int kt, char* b) {
-    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave);
-    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave);
+    const int ln = fresh_lane();  // the loads' addresses kept in registers would spill others
+    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave, ln);
+    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave, ln);
   };
   if (k_end > 0) load(0, b0);
   bf16x8 qf[D / 16], df[D / 16];
@@ -488,42 +517,69 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
       for (int e = 0; e < 8; ++e) dot += (float)df[i][e] * (float)of[i][e];
   }
   const float delta = pair_sum(dot);
-  if (in && lane < 32) a.delta[h * a.train_q + s.cq + q] = delta;
   const float lse2 = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : 0.f;
+  if (in && lane < 32) {
+    a.delta[h * a.train_q + s.cq + q] = delta;
+    a.lse2[h * a.train_q + s.cq + q] = lse2;
+  }
   f32x16 acc[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   const float c = a.scale * kLog2e;
   const int seen = q + off, wave_all = qt + 32 * wave + off, wave_end = min(s.kl, wave_all + 32);
+  // 64 keys as two blocks: the terms of one are formed beside the products of the other.  CUT: some query of
+  // the wave does not see all of them.
+  auto block = [&](auto cut, int kt, const char* cur) {
+    constexpr bool CUT = decltype(cut)::value;
+    constexpr int V = (CUT ? 104 : 72) * 8 / D + 1;
+    f32x16 x[2], dp[2];
+    auto scores = [&](int u) {
+      x[u] = dp[u] = zero16();
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x[u], 0, 0, 0);
+        dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, u, i), df[i], dp[u], 0, 0, 0);
+      }
+    };
+    bf16x8 ds[2][2];
+    auto terms = [&](int u) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float t = __builtin_amdgcn_exp2f(x[u][v] * c - lse2) * (dp[u][v] - delta);
+        x[u][v] = !CUT || kt + 32 * u + tile_row(v) <= seen ? t : 0.f;
+      }
+      ds[u][0] = pack8(x[u], 0), ds[u][1] = pack8(x[u], 1);
+    };
+    auto product = [&](int u) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur, 2 * u + w, t), ds[u][w], acc[t], 0, 0, 0);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    scores(0);
+    feed<D / 8, 1, 4>();
+    __builtin_amdgcn_sched_barrier(0);
+    scores(1);
+    terms(0);
+    feed_beside<D / 8, 1, 4, V>();
+    __builtin_amdgcn_sched_barrier(0);
+    product(0);
+    terms(1);
+    feed_beside<D / 16, 2, 2, 2 * V>();
+    __builtin_amdgcn_sched_barrier(0);
+    product(1);
+    feed<D / 16, 2, 2>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
   auto step = [&](int kt, const char* cur, char* nxt) {
     vmem_wait_all();
     __syncthreads();
     if (kt + TK < k_end) load(kt + TK, nxt);
     if (kt >= wave_end) return;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x16 x = zero16(), dp = zero16();
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, u, i), df[i], dp, 0, 0, 0);
-      if (kt + 32 * u + 31 > wave_all) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          x[v] = kt + 32 * u + tile_row(v) <= seen ? __builtin_amdgcn_exp2f(x[v] * c - lse2) * (dp[v] - delta) : 0.f;
-      } else {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] * c - lse2) * (dp[v] - delta);
-      }
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const bf16x8 p = pack8(x, w);
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur, 2 * u + w, t), p, acc[t], 0, 0, 0);
-      }
-    }
+    if (kt + TK - 1 > wave_all) block(bool_c<true>{}, kt, cur);
+    else block(bool_c<false>{}, kt, cur);
   };
   for (int kt = 0; kt < k_end; kt += 2 * TK) {
     step(kt, b0, b1);
@@ -542,11 +598,11 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // second wave multiplies dO(n) with V and closes ds(n - 1), for which Q is kept for one step more.
 template <int D>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
-  constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ;  // PB: p of 4 x 32 keys
-  __shared__ __attribute__((aligned(1024))) char b0[2 * TILE + PB];
-  __shared__ __attribute__((aligned(1024))) char b1[2 * TILE + PB];
-  __shared__ __attribute__((aligned(1024))) char b2[2 * TILE + PB];
-  __shared__ __attribute__((aligned(16))) float st[3][2][TQ];  // [buffer][lse (base 2), delta]
+  constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;
+  // Q, dO, p of 4 x 32 keys, lse (base 2) and delta
+  __shared__ __attribute__((aligned(1024))) char b0[ST + 8 * TQ];
+  __shared__ __attribute__((aligned(1024))) char b1[ST + 8 * TQ];
+  __shared__ __attribute__((aligned(1024))) char b2[ST + 8 * TQ];
   const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
@@ -563,16 +619,15 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   // through the same rows at the same time, whatever their first query, and share them in L2 (heads
   // outside and queries upwards missed more than half of its lines and took ...).
   auto q_of = [&](int n) { return q_first + (per_head - 1 - n / a.group) * TQ; };
-  float st_next = 0.f;  // of the next step: lse (threads 0 ..), delta (threads TQ ..)
   auto load = [&](int n, char* b, int ln) {
     const int h = hk * a.group + n % a.group, qt = q_of(n);
     stage<D, TQ, 8>(rows_rsrc(a.Q, (int64_t)s.q0 + qt, h, min(TQ, s.ql - qt), D), qrow, b, wave, ln);
     stage<D, TQ, 8>(rows_rsrc(a.dO, (int64_t)s.cq + qt, h, min(TQ, s.ql - qt), D), drow, b + TILE, wave, ln);
-    // queries past the last one: lse of +infinity makes their p zero
-    if (threadIdx.x < 2 * TQ) {
-      const int r = threadIdx.x & (TQ - 1), q = qt + r;
-      if (threadIdx.x < TQ) st_next = q < s.ql ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : INFINITY;
-      else st_next = q < s.ql ? a.delta[h * a.train_q + s.cq + q] : 0.f;
+    // one load each: a value a lane (zeros past the last query, whose dO is zeros)
+    if (blk == 0) {
+      const float* v = (second ? a.delta : a.lse2) + h * a.train_q + s.cq + qt;
+      llvm_amdgcn_raw_buffer_load_lds_a(flat_rsrc(v, 4 * min(TQ, s.ql - qt)), (lds_u32*)(b + ST + (second ? 4 * TQ : 0)), 4,
+                                        4 * ln, 0, 0, 0);
     }
   };
   if (steps > 0) load(0, b0, lane);
@@ -581,88 +636,146 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   f32x16 acc[D / 32];  // dV or dK
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
-  f32x16 dp[2];  // second wave: do . v of the step before
-  dp[0] = dp[1] = zero16();
   const float c = a.scale * kLog2e;
-  // step n in buffer `cur` (index b), the step before in `old`
-  auto step = [&](int n, int b, char* cur, const char* old, char* nxt) {
-    vmem_wait_all();
-    if (threadIdx.x < 2 * TQ) st[b][threadIdx.x / TQ][threadIdx.x & (TQ - 1)] = st_next;
-    __syncthreads();
-    // the three buffers lie further apart than an LDS offset reaches: kept in registers, three sets of
-    // addresses spill
-    const int ln = fresh_lane();
-    if (n + 1 < steps) load(n + 1, nxt, ln);
-    if (!second) {
-      if (n == steps) return;
-      const int qt = q_of(n);
+  // First wave: p of 64 queries as two blocks, the terms of one beside the products of the other.  CUT: some
+  // key lies behind a query's last one.
+  auto form_p = [&](auto cut, char* cur, int qt, int ln) {
+    constexpr bool CUT = decltype(cut)::value;
+    constexpr int V = (CUT ? 72 : 40) * 16 / D + 1;
+    f32x16 x[2];
+    f32x4 l4[2][4];
+    bf16x8 p[2][2];
+    auto scores = [&](int u) {
+      x[u] = zero16();
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x16 x = zero16();
+      for (int i = 0; i < 4; ++i) l4[u][i] = *reinterpret_cast<const f32x4*>(cur + ST + 4 * (32 * u + 8 * i + 4 * (ln >> 5)));
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i, ln), kv[i], x, 0, 0, 0);
+      for (int i = 0; i < D / 16; ++i)
+        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i, ln), kv[i], x[u], 0, 0, 0);
+    };
+    auto terms = [&](int u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st[b][0][32 * u + 8 * i + 4 * (ln >> 5)]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * i + e] = __builtin_amdgcn_exp2f(x[4 * i + e] * c - l4[e]);
-        }
-        if (k0 + 32 * blk + 31 > qt + 32 * u + off) {
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] = k <= qt + 32 * u + tile_row(v) + off ? x[v] : 0.f;
-        }
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const bf16x8 p = pack8(x, w);
-          *reinterpret_cast<u32x4*>(cur + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16) = __builtin_bit_cast(u32x4, p);
-#pragma unroll
-          for (int t = 0; t < D / 32; ++t)
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, 2 * u + w, t, ln), p, acc[t], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+      for (int v = 0; v < 16; ++v) {
+        const float e = __builtin_amdgcn_exp2f(x[u][v] * c - l4[u][v >> 2][v & 3]);
+        x[u][v] = !CUT || k <= qt + 32 * u + tile_row(v) + off ? e : 0.f;
       }
-      return;
-    }
-    if (n > 0) {
-      const int ob = b == 0 ? 2 : b - 1;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int w = 0; w < 2; ++w) {
+        p[u][w] = pack8(x[u], w);
+        *reinterpret_cast<u32x4*>(cur + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16) = __builtin_bit_cast(u32x4, p[u][w]);
+      }
+    };
+    auto product = [&](int u) {
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const u32x4 p = *reinterpret_cast<const u32x4*>(old + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16);
+      for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const f32x4 d4 = *reinterpret_cast<const f32x4*>(&st[ob][1][32 * u + 16 * w + 8 * i + 4 * (ln >> 5)]);
+        for (int t = 0; t < D / 32; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, 2 * u + w, t, ln), p[u][w], acc[t], 0, 0, 0);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    scores(0);
+    feed<D / 16, 1, 4>();
+    __builtin_amdgcn_sched_barrier(0);
+    scores(1);
+    terms(0);
+    feed_beside<D / 16, 1, 4, V>();
+    __builtin_amdgcn_sched_barrier(0);
+    product(0);
+    terms(1);
+    feed_beside<D / 16, 2, 2, V>();
+    __builtin_amdgcn_sched_barrier(0);
+    product(1);
+    feed<D / 16, 2, 2>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Second wave: do . v of step n (NOW), and ds of the step before (PAST) with its product, a block of 32
+  // queries after the other.
+  auto form_ds = [&](auto now_c, auto past_c, f32x16 (&dp)[2], const char* cur, const char* old, int ln) {
+    constexpr bool NOW = decltype(now_c)::value, PAST = decltype(past_c)::value;
+    constexpr int V = 56 * 16 / D;
+    bf16x8 ds[2];
+    auto terms = [&](int u) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t pw = p[2 * i + e / 2];
-              const float pf = __uint_as_float(e & 1 ? pw & 0xffff0000u : pw << 16);
-              dp[u][8 * w + 4 * i + e] = pf * (dp[u][8 * w + 4 * i + e] - d4[e]);
-            }
+      for (int w = 0; w < 2; ++w) {
+        const u32x4 p = *reinterpret_cast<const u32x4*>(old + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(old + ST + 4 * (TQ + 32 * u + 16 * w + 8 * i + 4 * (ln >> 5)));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t pw = p[2 * i + e / 2];
+            const float pf = __uint_as_float(e & 1 ? pw & 0xffff0000u : pw << 16);
+            dp[u][8 * w + 4 * i + e] = pf * (dp[u][8 * w + 4 * i + e] - d4[e]);
           }
-          const bf16x8 ds = pack8(dp[u], w);
-#pragma unroll
-          for (int t = 0; t < D / 32; ++t)
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(old, 2 * u + w, t, ln), ds, acc[t], 0, 0, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        ds[w] = pack8(dp[u], w);
       }
+    };
+    auto product = [&](int u, const bf16x8 (&d)[2]) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(old, 2 * u + w, t, ln), d[w], acc[t], 0, 0, 0);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PAST) {
+      terms(0);
+      const bf16x8 d0[2] = {ds[0], ds[1]};
+      __builtin_amdgcn_sched_barrier(0);
+      product(0, d0);
+      terms(1);
+      feed_beside<D / 16, 2, 2, V>();
+      __builtin_amdgcn_sched_barrier(0);
+      product(1, ds);
+      feed<D / 16, 2, 2>();
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (n < steps) {
+    if constexpr (NOW) {
+      dp[0] = dp[1] = zero16();
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        dp[u] = zero16();
+      for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
+        for (int u = 0; u < 2; ++u)
           dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur + TILE, u, i, ln), kv[i], dp[u], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      feed<D / 8, 1, 4>();
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  for (int n = 0; n <= steps; n += 3) {
-    step(n, 0, b0, b2, b1);
-    if (n + 1 <= steps) step(n + 1, 1, b1, b0, b2);
-    if (n + 2 <= steps) step(n + 2, 2, b2, b1, b0);
+  // Step n, 0 to steps: its rows have landed, the next ones are under way.  (The three buffers lie further apart
+  // than an LDS offset reaches: kept in registers, three sets of addresses spill.)
+  auto begin = [&](int n, char* nxt) {
+    vmem_wait_all();
+    __syncthreads();
+    const int ln = fresh_lane();
+    if (n + 1 < steps) load(n + 1, nxt, ln);
+    return ln;
+  };
+  if (!second) {
+    auto step = [&](int n, char* cur, char* nxt) {
+      const int ln = begin(n, nxt);
+      if (n == steps) return;
+      const int qt = q_of(n);
+      if (k0 + 32 * blk + 31 > qt + off) form_p(bool_c<true>{}, cur, qt, ln);
+      else form_p(bool_c<false>{}, cur, qt, ln);
+    };
+    for (int n = 0; n <= steps; n += 3) {
+      step(n, b0, b1);
+      if (n + 1 <= steps) step(n + 1, b1, b2);
+      if (n + 2 <= steps) step(n + 2, b2, b0);
+    }
+  } else {
+    f32x16 dp[2];  // do . v of the step before
+    auto step = [&](int n, const char* cur, const char* old, char* nxt) {
+      const int ln = begin(n, nxt);
+      if (n > 0) form_ds(bool_c<false>{}, bool_c<true>{}, dp, cur, old, ln);
+      if (n < steps) form_ds(bool_c<true>{}, bool_c<false>{}, dp, cur, old, ln);
+    };
+    for (int n = 0; n <= steps; n += 3) {
+      step(n, b0, b2, b1);
+      if (n + 1 <= steps) step(n + 1, b1, b0, b2);
+      if (n + 2 <= steps) step(n + 2, b2, b1, b0);
+    }
   }
   if (!in) return;
   if (second) store_cols<D>(a.dK, (int64_t)s.ck + k, hk, acc, a.scale);
@@ -673,7 +786,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Workspace {
-  size_t part_o, part_ml, delta, total;
+  size_t part_o, part_ml, delta, lse2, total;
 };
 
 Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
@@ -687,9 +800,10 @@ Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   at += align256(slots * kAttnPackRows * p.d * sizeof(float));
   w.part_ml = at;
   at += align256(slots * 2 * kAttnPackRows * sizeof(float));
-  // the two directions do not overlap on a stream: delta shares the room
+  // the two directions do not overlap on a stream: the backward's values share the room
   w.delta = 0;
-  w.total = std::max<size_t>(256, std::max(at, align256((size_t)p.train_q * p.hq * sizeof(float))));
+  w.lse2 = align256((size_t)p.train_q * p.hq * sizeof(float));
+  w.total = std::max<size_t>(256, std::max(at, (dt == DSV_BF16 ? 2 : 1) * w.lse2));
   return w;
 }
 
@@ -809,6 +923,7 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   if (ws_bytes < w.total) return DSV_ERR_SIZE;
   a.lse = const_cast<float*>(lse);
   a.delta = reinterpret_cast<float*>(static_cast<char*>(ws) + w.delta);
+  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(ws) + w.lse2);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const bool f32 = dt == DSV_F32;
   a.items = p->dptr(f32 ? p->lay.f32_dq_items : p->lay.dq_items);
