@@ -16,7 +16,7 @@ struct AttnView {
 struct AttnArgs {
   const int32_t* seqs;   // sequence descriptors (attn_plan.h)
   const int32_t* items;  // the launch's work items
-  int32_t n_items;
+  int32_t n_items;       // fp32 launches
   int32_t hq, hkv, group, d;
   int32_t n_q;           // row length of lse ([hq][n_q])
   int64_t train_q;       // row length of delta ([hq][train_q])
@@ -27,10 +27,11 @@ struct AttnArgs {
   float* lse2;           // bf16: lse of the compact rows, base 2
   // split form
   const int32_t* split_keys;
-  const int32_t* join_items;
-  int32_t n_join;
-  float* part_o;         // [piece][hkv][kAttnPackRows][D], sums of exp(s - m) v
-  float* part_ml;        // [piece][hkv][2][kAttnPackRows]: m, sum of exp(s - m)
+  // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
+  // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
+  // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].
+  float* part_o;
+  float* part_ml;
 };
 
 // fp32 mode: tiles of kAttnF32Rows.

@@ -250,18 +250,20 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
   __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
   const int item = blockIdx.x / a.hq, h = head_of(a, blockIdx.x % a.hq);
-  const Seq s(a, a.items[2 * item]);
-  const int qt = a.items[2 * item + 1];
+  const int32_t* it = a.items + (int64_t)item * kAttnTileWords;
+  const Seq s(a, it[0]);
+  const int qt = it[1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int off = s.kl - s.ql, hk = h / a.group;
   const int q = qt + 32 * wave + (lane & 31);
-  const int k_end = min(s.kl, min(qt + kAttnFwdRows, s.ql) + off);
+  // the tile's keys, or a piece of them
+  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnFwdRows, s.ql) + off), TK * it[3]);
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
   auto load = [&](int kt, char* b) {
     stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave);
     stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave);
   };
-  if (k_end > 0) load(0, b0);
+  if (k_first < k_end) load(k_first, b0);
   bf16x8 qf[D / 16];
   row_frags<D>(a.Q, (int64_t)s.q0 + q, h, q < s.ql, qf);
   f32x16 acc[D / 32];
@@ -314,12 +316,28 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     __builtin_amdgcn_sched_group_barrier(0x008, D / 32, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  for (int kt = 0; kt < k_end; kt += 2 * TK) {
+  for (int kt = k_first; kt < k_end; kt += 2 * TK) {
     step(kt, b0, b1);
     if (kt + TK < k_end) step(kt + TK, b1, b0);
   }
   const float sum = pair_sum(run.sum);
   if (q >= s.ql) return;
+  if (it[5] > 1) {
+    const int64_t slot = (int64_t)it[4] * a.hq + h;
+    const int row = 32 * wave + (lane & 31);
+    float* p = a.part_o + (slot * kAttnFwdRows + row) * D + 4 * (lane >> 5);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(p + 32 * t + 8 * i) =
+            f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+    if (lane < 32) {
+      a.part_ml[slot * 2 * kAttnFwdRows + row] = run.ref;
+      a.part_ml[(slot * 2 + 1) * kAttnFwdRows + row] = sum;
+    }
+    return;
+  }
   store_cols<D>(a.O, (int64_t)s.q0 + q, h, acc, sum == 0.f ? 0.f : 1.f / sum);
   if (a.lse && lane < 32) a.lse[(int64_t)h * a.n_q + s.q0 + q] = lse_of(run.ref, sum);
 }
@@ -449,38 +467,56 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   }
 }
 
-// The pieces of a tile of the split form, added in order: row tid / 8, D / 8 columns each.
+// Pieces of a row added in order: columns c0 .. c0 + D / 8 of row `row` of `rows`, slots first, first + step, ..
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
-  const int32_t* it = a.join_items + 4 * (int64_t)item;
-  const int n = it[3];
-  if (n == 1) return;  // written by its only piece
-  const Seq s(a, it[0]);
-  const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8), r = it[1] + row;
-  if (r >= s.ql * a.group) return;
+__device__ __forceinline__ void join_row(const AttnArgs& a, int64_t first, int64_t step, int n, int rows, int row, int c0,
+                                         int64_t out_row, int h) {
   float ref = -INFINITY, total = 0.f;
-  for (int k = 0; k < n; ++k)
-    ref = fmaxf(ref, a.part_ml[((int64_t)(it[2] + k) * a.hkv + hk) * 2 * kAttnPackRows + row]);
+  for (int k = 0; k < n; ++k) ref = fmaxf(ref, a.part_ml[(first + k * step) * 2 * rows + row]);
   f32x4 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < n; ++k) {
-    const int64_t slot = (int64_t)(it[2] + k) * a.hkv + hk;
-    const float m = a.part_ml[slot * 2 * kAttnPackRows + row];
+    const int64_t slot = first + k * step;
+    const float m = a.part_ml[slot * 2 * rows + row];
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-    total += f * a.part_ml[(slot * 2 + 1) * kAttnPackRows + row];
-    const float* p = a.part_o + (slot * kAttnPackRows + row) * D + c0;
+    total += f * a.part_ml[(slot * 2 + 1) * rows + row];
+    const float* p = a.part_o + (slot * rows + row) * D + c0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + 4 * i) * f;
   }
   const float g = total == 0.f ? 0.f : 1.f / total;
-  const int q = r / a.group, h = hk * a.group + r % a.group;
-  uint16_t* p = static_cast<uint16_t*>(a.O.ptr) + ((int64_t)s.q0 + q) * a.O.row + h * a.O.head + c0;
+  uint16_t* p = static_cast<uint16_t*>(a.O.ptr) + out_row * a.O.row + h * a.O.head + c0;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
     *reinterpret_cast<uint2*>(p + 4 * i) = make_uint2(f2bf2(o[i][0] * g, o[i][1] * g), f2bf2(o[i][2] * g, o[i][3] * g));
-  if (a.lse && (threadIdx.x & 7) == 0) a.lse[(int64_t)h * a.n_q + s.q0 + q] = lse_of(ref, total);
+  if (a.lse && c0 == 0) a.lse[(int64_t)h * a.n_q + out_row] = lse_of(ref, total);
+}
+
+// Tiles of the split form: row tid / 8, D / 8 columns each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
+  const int32_t* it = a.items + 4 * (int64_t)item;
+  if (it[3] == 1) return;  // written by its only piece
+  const Seq s(a, it[0]);
+  const int row = threadIdx.x >> 3, r = it[1] + row;
+  if (r >= s.ql * a.group) return;
+  join_row<D>(a, (int64_t)it[2] * a.hkv + hk, a.hkv, it[3], kAttnPackRows, row, (threadIdx.x & 7) * (D / 8),
+              (int64_t)s.q0 + r / a.group, hk * a.group + r % a.group);
+}
+
+// Forward tiles: 32 rows a workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void attn_fwd_join_kernel(AttnArgs a) {
+  constexpr int BL = kAttnFwdRows / 32;
+  const int item = blockIdx.x / (BL * a.hq), h = blockIdx.x / BL % a.hq;
+  const int32_t* it = a.items + 4 * (int64_t)item;
+  const Seq s(a, it[0]);
+  const int row = 32 * (blockIdx.x % BL) + (threadIdx.x >> 3), q = it[1] + row;
+  if (q >= s.ql) return;
+  join_row<D>(a, (int64_t)it[2] * a.hq + h, a.hq, it[3], kAttnFwdRows, row, (threadIdx.x & 7) * (D / 8), (int64_t)s.q0 + q,
+              h);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -604,8 +640,9 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char b1[ST + 8 * TQ];
   __shared__ __attribute__((aligned(1024))) char b2[ST + 8 * TQ];
   const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
-  const Seq s(a, a.items[2 * item]);
-  const int k0 = a.items[2 * item + 1];
+  const int32_t* it = a.items + (int64_t)item * kAttnTileWords;
+  const Seq s(a, it[0]);
+  const int k0 = it[1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wave >= 4;
   const int blk = wave & 3;
@@ -614,13 +651,14 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   const bool in = k < s.kl;
   const int qrow = (int)a.Q.row * 2, drow = (int)a.dO.row * 2;
   const int q_first = max(0, k0 - off);
-  const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, steps = per_head * a.group;
+  // the tile's steps, or a piece of them
+  const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, n0 = it[2], steps = it[3] - n0;
   // The last queries first, one query head after the other: the workgroups of a sequence's key tiles run
   // through the same rows at the same time, whatever their first query, and share them in L2 (heads
   // outside and queries upwards missed more than half of its lines and took ...).
-  auto q_of = [&](int n) { return q_first + (per_head - 1 - n / a.group) * TQ; };
+  auto q_of = [&](int n) { return q_first + (per_head - 1 - (n0 + n) / a.group) * TQ; };
   auto load = [&](int n, char* b, int ln) {
-    const int h = hk * a.group + n % a.group, qt = q_of(n);
+    const int h = hk * a.group + (n0 + n) % a.group, qt = q_of(n);
     stage<D, TQ, 8>(rows_rsrc(a.Q, (int64_t)s.q0 + qt, h, min(TQ, s.ql - qt), D), qrow, b, wave, ln);
     stage<D, TQ, 8>(rows_rsrc(a.dO, (int64_t)s.cq + qt, h, min(TQ, s.ql - qt), D), drow, b + TILE, wave, ln);
     // one load each: a value a lane (zeros past the last query, whose dO is zeros)
@@ -778,33 +816,82 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
     }
   }
   if (!in) return;
+  if (it[5] > 1) {
+    float* p = a.part_o + ((((int64_t)it[4] * a.hkv + hk) * 2 + (second ? 0 : 1)) * kAttnBwdRows + 32 * blk + (lane & 31)) * D +
+               4 * (lane >> 5);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(p + 32 * t + 8 * i) =
+            f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+    return;
+  }
   if (second) store_cols<D>(a.dK, (int64_t)s.ck + k, hk, acc, a.scale);
   else store_cols<D>(a.dV, (int64_t)s.ck + k, hk, acc, 1.f);
+}
+
+// dK (half 0) and dV of key tiles in pieces, added in order: 32 rows a workgroup, row tid / 8, D / 8 columns each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dk_join_kernel(AttnArgs a) {
+  constexpr int BL = kAttnBwdRows / 32;
+  const int half = blockIdx.x & 1, blk = blockIdx.x / 2 % BL, hk = blockIdx.x / (2 * BL) % a.hkv;
+  const int32_t* it = a.items + 4 * (int64_t)(blockIdx.x / (2 * BL * a.hkv));
+  const Seq s(a, it[0]);
+  const int row = 32 * blk + (threadIdx.x >> 3), k = it[1] + row, c0 = (threadIdx.x & 7) * (D / 8);
+  if (k >= s.kl) return;
+  f32x4 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < it[3]; ++n) {
+    const float* p = a.part_o + ((((int64_t)(it[2] + n) * a.hkv + hk) * 2 + half) * kAttnBwdRows + row) * D + c0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + 4 * i);
+  }
+  const AttnView& t = half ? a.dV : a.dK;
+  const float f = half ? 1.f : a.scale;
+  uint16_t* p = static_cast<uint16_t*>(t.ptr) + ((int64_t)s.ck + k) * t.row + hk * t.head + c0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+    *reinterpret_cast<uint2*>(p + 4 * i) = make_uint2(f2bf2(o[i][0] * f, o[i][1] * f), f2bf2(o[i][2] * f, o[i][3] * f));
 }
 
 // ---- host -------------------------------------------------------------------------------------------
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Workspace {
-  size_t part_o, part_ml, delta, lse2, total;
+  size_t split_o, split_ml, fwd_o, fwd_ml;  // forward
+  size_t delta, lse2, dk;                   // backward (the two do not overlap on a stream: one room)
+  size_t total;
 };
 
 Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   Workspace w{};
   size_t at = 0;
-  bool joined = false;  // some tile has more than one piece
-  const int32_t* join = p.meta.data() + p.lay.join_items;
-  for (int32_t i = 0; i < p.n_join; ++i) joined |= join[4 * i + 3] > 1;
-  const size_t slots = dt == DSV_BF16 && joined ? (size_t)p.n_split * p.hkv : 0;
-  w.part_o = at;
-  at += align256(slots * kAttnPackRows * p.d * sizeof(float));
-  w.part_ml = at;
-  at += align256(slots * 2 * kAttnPackRows * sizeof(float));
-  // the two directions do not overlap on a stream: the backward's values share the room
-  w.delta = 0;
-  w.lse2 = align256((size_t)p.train_q * p.hq * sizeof(float));
-  w.total = std::max<size_t>(256, std::max(at, (dt == DSV_BF16 ? 2 : 1) * w.lse2));
+  auto room = [&](size_t floats) {
+    const size_t o = at;
+    at += align256(floats * sizeof(float));
+    return o;
+  };
+  const bool bf = dt == DSV_BF16;
+  const size_t split = bf && p.n_split > p.n_join ? (size_t)p.n_split * p.hkv : 0;  // some tile has several pieces
+  const size_t tiles = bf ? (size_t)p.fwd_slots * p.hq : 0;
+  w.split_o = room(split * kAttnPackRows * p.d);
+  w.split_ml = room(split * 2 * kAttnPackRows);
+  w.fwd_o = room(tiles * kAttnFwdRows * p.d);
+  w.fwd_ml = room(tiles * 2 * kAttnFwdRows);
+  const size_t fwd = at;
+  at = 0;
+  w.delta = room((size_t)p.train_q * p.hq);
+  w.lse2 = room(bf ? (size_t)p.train_q * p.hq : 0);
+  w.dk = room(bf ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d : 0);
+  w.total = std::max<size_t>(256, std::max(at, fwd));
   return w;
+}
+
+template <typename T>
+T* at(void* ws, size_t off) {
+  return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
 }
 
 constexpr int64_t kMaxRowStride = 1 << 23, kMaxHeadStride = (int64_t)1 << 40;
@@ -886,20 +973,23 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
     a.n_items = p->n_f32;
     return status(launch_attn_f32_fwd(a, s));
   }
+  const int64_t hq = p->hq, hkv = p->hkv;
   a.items = p->dptr(p->lay.fwd_items);
-  a.n_items = p->n_fwd;
-  hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, (int64_t)p->n_fwd * p->hq, s);
-  if (e != hipSuccess || p->n_split == 0) return status(e);
+  a.part_o = at<float>(ws, w.fwd_o);
+  a.part_ml = at<float>(ws, w.fwd_ml);
+  hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, p->n_fwd * hq, s);
+  if (e != hipSuccess) return status(e);
+  a.items = p->dptr(p->lay.fwd_join);
+  e = launch(attn_fwd_join_kernel<64>, attn_fwd_join_kernel<128>, a, p->n_fwd_join * hq * (kAttnFwdRows / 32), s);
+  if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.split_items);
-  a.n_items = p->n_split;
   a.split_keys = p->dptr(p->lay.split_keys);
-  a.join_items = p->dptr(p->lay.join_items);
-  a.n_join = p->n_join;
-  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_o);
-  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_ml);
-  e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, (int64_t)p->n_split * p->hkv, s);
+  a.part_o = at<float>(ws, w.split_o);
+  a.part_ml = at<float>(ws, w.split_ml);
+  e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, p->n_split * hkv, s);
   if (e != hipSuccess || p->n_split == p->n_join) return status(e);  // one piece each: nothing to join
-  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, (int64_t)p->n_join * p->hkv, s));
+  a.items = p->dptr(p->lay.join_items);
+  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, p->n_join * hkv, s));
 }
 
 extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, const dsv_attn_view* Q,
@@ -922,16 +1012,26 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   const Workspace w = carve(*p, dt);
   if (ws_bytes < w.total) return DSV_ERR_SIZE;
   a.lse = const_cast<float*>(lse);
-  a.delta = reinterpret_cast<float*>(static_cast<char*>(ws) + w.delta);
-  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(ws) + w.lse2);
+  a.delta = at<float>(ws, w.delta);
+  a.lse2 = at<float>(ws, w.lse2);
+  a.part_o = at<float>(ws, w.dk);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const bool f32 = dt == DSV_F32;
-  a.items = p->dptr(f32 ? p->lay.f32_dq_items : p->lay.dq_items);
-  a.n_items = f32 ? p->n_f32_dq : p->n_dq;
-  hipError_t e = f32 ? launch_attn_f32_dq(a, s) : launch(attn_dq_kernel<64>, attn_dq_kernel<128>, a, (int64_t)a.n_items * p->hq, s);
+  const int64_t hq = p->hq, hkv = p->hkv;
+  if (dt == DSV_F32) {
+    a.items = p->dptr(p->lay.f32_dq_items);
+    a.n_items = p->n_f32_dq;
+    const hipError_t e = launch_attn_f32_dq(a, s);
+    if (e != hipSuccess) return status(e);
+    a.items = p->dptr(p->lay.f32_dk_items);
+    a.n_items = p->n_f32_dk;
+    return status(launch_attn_f32_dk(a, s));
+  }
+  a.items = p->dptr(p->lay.dq_items);
+  hipError_t e = launch(attn_dq_kernel<64>, attn_dq_kernel<128>, a, p->n_dq * hq, s);
   if (e != hipSuccess) return status(e);
-  a.items = p->dptr(f32 ? p->lay.f32_dk_items : p->lay.dk_items);
-  a.n_items = f32 ? p->n_f32_dk : p->n_dk;
-  return status(f32 ? launch_attn_f32_dk(a, s)
-                    : launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, (int64_t)a.n_items * p->hkv, s, 512));
+  a.items = p->dptr(p->lay.dk_items);
+  e = launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, p->n_dk * hkv, s, 512);
+  if (e != hipSuccess) return status(e);
+  a.items = p->dptr(p->lay.dk_join);
+  return status(launch(attn_dk_join_kernel<64>, attn_dk_join_kernel<128>, a, p->n_dk_join * hkv * 2 * (kAttnBwdRows / 32), s));
 }

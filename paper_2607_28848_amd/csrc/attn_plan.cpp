@@ -7,8 +7,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <functional>
 #include <new>
 #include <numeric>
+#include <queue>
 
 #include "attn_plan.h"
 
@@ -29,6 +31,79 @@ struct Tiles {
     return w;
   }
 };
+
+// Tiles in steps of equal cost, `copies` (heads) of each, on `slots` workgroups at a time: every tile whole, or cut
+// into pieces of at most `piece` steps.
+struct Cut {
+  std::vector<int32_t> items, join;
+  int32_t n_items = 0, n_join = 0, n_slots = 0;
+};
+
+// The time, in steps, that the tiles take in pieces of at most `piece` steps, longest first, each on the slot
+// that is free first.  join: steps that a piece's own sums cost.
+int64_t makespan(const std::vector<int64_t>& steps, int64_t copies, int64_t piece, int slots, int64_t join) {
+  std::vector<int64_t> len;
+  for (int64_t s : steps) {
+    const int64_t n = std::max<int64_t>(1, (s + piece - 1) / piece);
+    for (int64_t k = 0; k < n * copies; ++k) len.push_back((s + n - 1) / n + (n > 1 ? join : 0));
+  }
+  std::sort(len.begin(), len.end(), std::greater<int64_t>());
+  std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> free_at;
+  for (int i = 0; i < slots; ++i) free_at.push(0);
+  int64_t end = 0;
+  for (int64_t l : len) {
+    const int64_t t = free_at.top() + l;
+    free_at.pop();
+    free_at.push(t);
+    end = std::max(end, t);
+  }
+  return end;
+}
+
+// tiles: {-steps, {sequence, first row}}
+Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t copies, int slots) {
+  std::stable_sort(t.begin(), t.end(), [](const auto& a, const auto& b) { return a.first < b.first; });
+  std::vector<int64_t> steps;
+  int64_t all = 0, most = 0;
+  for (const auto& e : t) {
+    steps.push_back(-e.first);
+    all += -e.first;
+    most = std::max(most, -e.first);
+  }
+  int64_t piece = std::max<int64_t>(most, 1);
+  const int64_t share = all * copies / slots;
+  // With several rounds of tiles the short ones fill what the long ones leave.
+  if ((int64_t)t.size() * copies < 4 * slots && most > share + share / 4 && most > kAttnPieceSteps) {
+    int64_t best = makespan(steps, copies, piece, slots, 0);
+    for (int64_t d = 2; d <= 8; ++d) {  // shares of eighths
+      const int64_t p = std::max<int64_t>(kAttnPieceSteps, share * d / 4);
+      const int64_t m = makespan(steps, copies, p, slots, 2);
+      if (m < best) best = m, piece = p;
+    }
+  }
+  Cut c;
+  struct Piece {
+    int64_t steps;
+    int32_t w[kAttnTileWords];
+  };
+  std::vector<Piece> all_pieces;
+  for (const auto& e : t) {
+    const int64_t s = -e.first, n = std::max<int64_t>(1, (s + piece - 1) / piece), len = (s + n - 1) / n;
+    if (n > 1) {
+      c.join.insert(c.join.end(), {e.second.first, e.second.second, c.n_slots, (int32_t)n});
+      ++c.n_join;
+    }
+    for (int64_t k = 0; k < n; ++k) {
+      const int64_t b = std::min(k * len, s), l = std::min((k + 1) * len, s);
+      all_pieces.push_back({l - b, {e.second.first, e.second.second, (int32_t)b, (int32_t)l, n > 1 ? c.n_slots++ : 0,
+                                    (int32_t)n, 0, 0}});
+    }
+  }
+  std::stable_sort(all_pieces.begin(), all_pieces.end(), [](const Piece& a, const Piece& b) { return a.steps > b.steps; });
+  for (const Piece& p : all_pieces) c.items.insert(c.items.end(), p.w, p.w + kAttnTileWords);
+  c.n_items = (int32_t)all_pieces.size();
+  return c;
+}
 
 // Keys that queries [.., last] of a sequence see.
 int64_t keys_seen(const dsv_attn_seq& s, int64_t last) {
@@ -61,7 +136,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     tiles_q += ((int64_t)seqs[i].q_len + kAttnF32Rows - 1) / kAttnF32Rows;
     tiles_k += ((int64_t)seqs[i].k_len + kAttnF32Rows - 1) / kAttnF32Rows;
   }
-  if (tiles_q * hq > INT32_MAX || tiles_k * hkv > INT32_MAX) return DSV_ERR_SIZE;
+  if (8 * tiles_q * hq > INT32_MAX || 8 * tiles_k * hkv > INT32_MAX) return DSV_ERR_SIZE;
 
   p.n_seqs = n;
   p.n_q = n_q;
@@ -102,7 +177,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
       split_keys_all += tiles * s.k_len;
     } else {
       for (int64_t q = 0; q < s.q_len; q += kAttnFwdRows)
-        fwd.add(keys_seen(s, std::min<int64_t>(q + kAttnFwdRows, s.q_len) - 1), i, q);
+        fwd.add((keys_seen(s, std::min<int64_t>(q + kAttnFwdRows, s.q_len) - 1) + 63) / 64, i, q);
     }
   }
   for (int32_t i = 0; i < n; ++i) {
@@ -114,7 +189,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
       f32_dq.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
     // queries that see key k: from max(0, k - (k_len - q_len)) on
     auto seen_by = [&](int64_t k) { return s.q_len - std::max<int64_t>(0, k - ((int64_t)s.k_len - s.q_len)); };
-    for (int64_t k = 0; k < s.k_len; k += kAttnBwdRows) dk.add(seen_by(k), i, k);
+    for (int64_t k = 0; k < s.k_len; k += kAttnBwdRows) dk.add(std::max<int64_t>(0, (seen_by(k) + 63) / 64) * group, i, k);
     for (int64_t k = 0; k < s.k_len; k += kAttnF32Rows) f32_dk.add(seen_by(k), i, k);
   }
 
@@ -154,26 +229,29 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     *out = (int32_t)c;
     return c;
   };
-  const std::vector<int32_t> wf = fwd.words(), w3 = f32.words(), wq = dq.words(), wk = dk.words(), w3q = f32_dq.words(),
+  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots), ck = cut(std::move(dk.t), hkv, kAttnDkSlots);
+  p.n_fwd = cf.n_items, p.n_fwd_join = cf.n_join, p.fwd_slots = cf.n_slots;
+  p.n_dk = ck.n_items, p.n_dk_join = ck.n_join, p.dk_slots = ck.n_slots;
+  const std::vector<int32_t> w3 = f32.words(), wq = dq.words(), w3q = f32_dq.words(),
                              w3k = f32_dk.words();
-  int64_t most = 0;
-  most = std::max(most, count(wf, 2, &p.n_fwd));
+  int64_t most = std::max(p.n_fwd, p.n_dk);
   most = std::max(most, count(w3, 2, &p.n_f32));
   most = std::max(most, count(split_items, 4, &p.n_split));
   most = std::max(most, count(join_items, 4, &p.n_join));
   most = std::max(most, count(wq, 2, &p.n_dq));
-  most = std::max(most, count(wk, 2, &p.n_dk));
   most = std::max(most, count(w3q, 2, &p.n_f32_dq));
   most = std::max(most, count(w3k, 2, &p.n_f32_dk));
-  if (most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
+  if (4 * most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
   L.seqs = put(desc);
-  L.fwd_items = put(wf);
+  L.fwd_items = put(cf.items);
+  L.fwd_join = put(cf.join);
   L.f32_items = put(w3);
   L.split_items = put(split_items);
   L.split_keys = put(split_keys);
   L.join_items = put(join_items);
   L.dq_items = put(wq);
-  L.dk_items = put(wk);
+  L.dk_items = put(ck.items);
+  L.dk_join = put(ck.join);
   L.f32_dq_items = put(w3q);
   L.f32_dk_items = put(w3k);
   m.resize(std::max<size_t>(64, (m.size() + 63) & ~size_t(63)), 0);
