@@ -36,10 +36,15 @@ struct VocabArgs {
   int32_t split, split_len;
 };
 
-// A tile whose largest logit (base 2) exceeds the row's reference by more than this takes its own
-// maximum as reference: terms stay below 2^kVocabSlack, and all but a row's first pieces keep the
-// reference they find, so their terms need no second look.
-constexpr float kVocabSlack = 24.f;
+// References.  A row starts at 0, and a tile of the first piece takes its own maximum (m, base 2) where it lies
+// further than kVocabSlack from that on either side; in later pieces where it exceeds the row's reference by
+// more.  So terms stay below 2^kVocabSlack and the row's largest far from underflow, and for all but unusual
+// logits every tile of a row has one reference: its terms need no second look.
+constexpr float kVocabSlack = 60.f;
+
+__device__ __forceinline__ bool own_reference(float m, float have, bool first) {
+  return m > have + kVocabSlack || (first && m < have - kVocabSlack);
+}
 
 hipError_t launch_vocab_f32_logits(const VocabArgs& a, hipStream_t s);
 hipError_t launch_vocab_f32_grad(const VocabArgs& a, hipStream_t s);

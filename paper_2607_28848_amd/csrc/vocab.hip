@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   constexpr int WM = 16 * FM, TM = 2 * WM;
   __shared__ __attribute__((aligned(1024))) char smem0[kTileStage];
   __shared__ __attribute__((aligned(1024))) char smem1[kTileStage];
-  __shared__ float red[2][2][TM];  // [maximum, sum][column half][row]
+  __shared__ float red[3][2][TM];  // [maximum, sum, reference][column half][row]
   const int n_m = (a.T + TM - 1) / TM;
   int mt, nt;
   tile_at(tile_of(blockIdx.x, gridDim.x), n_m, a.n_ct, mt, nt);
@@ -49,77 +49,65 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                                              static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols,
                                              a.K, smem0, smem1, acc);
   const int c0 = wn * 128 + 4 * g4;  // column of acc[.][j][v]: c0 + 16 j + v
-  if (cols < 256) {
+  // The sums are read twice and never written: in registers of the matrix core from the first to the last.
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < FM; ++i) {
+    float m = -INFINITY;
+    if (cols == 256) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (c0 + 16 * j + v >= cols) acc[i][j][v] = -INFINITY;
-  }
-  float top[FM];
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, acc[i][j][v]);
+    } else {
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    float m = acc[i][0][0];
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) m = fmaxf(m, acc[i][j][v]);
-    top[i] = quad_max(m);
-    if (lane < 16) red[0][wn][wm * WM + 16 * i + l15] = top[i];
-  }
-  __syncthreads();
-  float ref[FM], sum[FM];
-#pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int r = wm * WM + 16 * i + l15, row = m0 + r;
-    const bool in = row < a.T;
-    const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
-    const float have = GRAD && !a.first && in ? a.ref[row] : -INFINITY;
-    ref[i] = m > have + kVocabSlack ? m : have;
-    const float base = ref[i] == -INFINITY ? 0.f : ref[i];
-    const int t = in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
-    sum[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float z = acc[i][j][v];
-        float e = __builtin_amdgcn_exp2f(z * kLog2e - base);
-        if (t == 16 * j + v) {
-          a.zt[row] = z;
-          e = 0.f;
-        }
-        sum[i] += e;
-        acc[i][j][v] = e;
-      }
-    sum[i] = quad_sum(sum[i]);
-    if (lane < 16) red[1][wn][r] = sum[i];
-  }
-  __syncthreads();
-  if (wn == 0 && lane < 16) {
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int r = wm * WM + 16 * i + l15;
-      if (m0 + r < a.T) a.stats[(int64_t)(m0 + r) * a.ld_stats + nt] = make_float2(ref[i], red[1][0][r] + red[1][1][r]);
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, c0 + 16 * j + v < cols ? acc[i][j][v] : -INFINITY);
     }
+    m = quad_max(m);
+    if (lane < 16) red[0][wn][wm * WM + 16 * i + l15] = m;
   }
-  if constexpr (GRAD) {
-    // P through the idle buffer, 32 rows of 128 columns per wave at a time, for 16-byte stores
-    constexpr int SRS = 128 * 2 + 16;
-    char* const slice = idle + wave * 32 * SRS;
-    uint16_t* const P = static_cast<uint16_t*>(a.P) + (int64_t)(m0 + wm * WM) * a.ldp + n0 + wn * 128;
+  __syncthreads();
+  // Terms: 32 rows of 128 columns per wave at a time, whose P goes through the idle buffer for 16-byte stores.
+  constexpr int SRS = 128 * 2 + 16;
+  char* const slice = idle + wave * 32 * SRS;
+  uint16_t* const P = static_cast<uint16_t*>(a.P) + (int64_t)(m0 + wm * WM) * a.ldp + n0 + wn * 128;
 #pragma unroll
-    for (int t = 0; t < FM / 2; ++t) {
+  for (int t = 0; t < FM / 2; ++t) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      const int i = 2 * t + h, r = wm * WM + 16 * i + l15, row = m0 + r;
+      const bool in = row < a.T;
+      const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
+      const float have = !a.first && in ? a.ref[row] : 0.f;
+      const float ref = own_reference(m, have, a.first) ? m : have, base = ref == -INFINITY ? 0.f : ref;
+      const int tc = in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
+      float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const f32x4 x = acc[2 * t + h][j];
-          *reinterpret_cast<uint2*>(slice + (16 * h + l15) * SRS + 2 * (16 * j + 4 * g4)) =
-              make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
+      for (int j = 0; j < 8; ++j) {
+        f32x4 e;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float z = acc[i][j][v];
+          e[v] = __builtin_amdgcn_exp2f(z * kLog2e - base);
+          if (tc == 16 * j + v) {
+            a.zt[row] = z;
+            e[v] = 0.f;
+          }
+          if (cols < 256 && c0 + 16 * j + v >= cols) e[v] = 0.f;
+          sum += e[v];
         }
+        if constexpr (GRAD)
+          *reinterpret_cast<uint2*>(slice + (16 * h + l15) * SRS + 2 * (16 * j + 4 * g4)) =
+              make_uint2(f2bf2(e[0], e[1]), f2bf2(e[2], e[3]));
+      }
+      sum = quad_sum(sum);
+      if (lane < 16) {
+        red[1][wn][r] = sum;
+        if (wn == 0) red[2][0][r] = ref;
+      }
+    }
+    if constexpr (GRAD) {
       asm volatile("" ::: "memory");  // a wave's LDS accesses run in order
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
@@ -130,6 +118,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
       asm volatile("" ::: "memory");
     }
   }
+  __syncthreads();
+  for (int r = threadIdx.x; r < TM; r += 256)
+    if (m0 + r < a.T) a.stats[(int64_t)(m0 + r) * a.ld_stats + nt] = make_float2(red[2][0][r], red[1][0][r] + red[1][1][r]);
 }
 
 // ---- second product -------------------------------------------------------------------------------------
@@ -148,33 +139,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   const int c0 = part * a.split_len, C = min(a.vn - c0, a.split_len);
   const uint16_t* W = static_cast<const uint16_t*>(NN ? a.W : a.Wt);
   W += NN ? (int64_t)(a.v0 + c0) * a.ldw + n0 : (int64_t)n0 * a.ldwt + a.v0 + c0;
-  f32x4 acc[FM][8];
-  if (C > 0) {
-    tile_product<NN, FM>(static_cast<const uint16_t*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0, W,
-                         NN ? a.ldw : a.ldwt, a.K - n0, C, smem0, smem1, acc);
-  } else {  // a short last piece ends before this range
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
+  auto put = [&](auto value) {
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int row = m0 + wm * WM + 16 * i + (lane & 15);
-    if (row >= a.T) continue;
-    const float f = a.first ? 0.f : a.alpha[row];
-    float* o = a.O + ((int64_t)part * a.T + row) * a.K;
+    for (int i = 0; i < FM; ++i) {
+      const int row = m0 + wm * WM + 16 * i + (lane & 15);
+      if (row >= a.T) continue;
+      const float f = a.first ? 0.f : a.alpha[row];
+      float* o = a.O + ((int64_t)part * a.T + row) * a.K;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int col = n0 + wn * 128 + 16 * j + 4 * (lane >> 4);
-      if (col >= a.K) continue;
-      f32x4 x = acc[i][j];
-      if (!a.first) x += *reinterpret_cast<const f32x4*>(o + col) * f;
-      *reinterpret_cast<f32x4*>(o + col) = x;
+      for (int j = 0; j < 8; ++j) {
+        const int col = n0 + wn * 128 + 16 * j + 4 * (lane >> 4);
+        if (col >= a.K) continue;
+        f32x4 x = value(i, j);
+        if (!a.first) x += *reinterpret_cast<const f32x4*>(o + col) * f;
+        *reinterpret_cast<f32x4*>(o + col) = x;
+      }
     }
+  };
+  if (C <= 0) {  // a short last piece ends before this range
+    put([](int, int) { return f32x4{0.f, 0.f, 0.f, 0.f}; });
+    return;
   }
+  f32x4 acc[FM][8];
+  tile_product<NN, FM>(static_cast<const uint16_t*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0, W, NN ? a.ldw : a.ldwt,
+                       a.K - n0, C, smem0, smem1, acc);
+  put([&](int i, int j) { return acc[i][j]; });
 }
 
 // ---- rows -------------------------------------------------------------------------------------------------
@@ -277,7 +268,9 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(VocabArgs a) {
   const T* w = static_cast<const T*>(a.W) + (int64_t)(has ? t : 0) * a.ldw;
   const float others = a.others[row], et = has ? exp2f(a.zt[row] * kLog2e - a.ref[row]) : 1.f;
   const float f = (a.weight ? a.weight[row] : 1.f) / (others + et);
-  for (int c = 4 * threadIdx.x; c < a.K; c += 1024) {
+  // 1024 columns a workgroup
+  const int c = 1024 * blockIdx.y + 4 * threadIdx.x;
+  if (c < a.K) {
     f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
     if (has) {
       for (int s = 0; s < a.split; ++s) x += *reinterpret_cast<const f32x4*>(a.O + ((int64_t)s * a.T + row) * a.K + c);
@@ -432,8 +425,8 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     if (e != hipSuccess) return DSV_ERR_DEVICE;
   }
   if (!a.grad) return DSV_OK;
-  if (bf) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(vocab_finish_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
+  if (bf) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, dim3((unsigned)a.T, (a.K + 1023) / 1024), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(vocab_finish_kernel<float>, dim3((unsigned)a.T, (a.K + 1023) / 1024), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? DSV_OK : DSV_ERR_DEVICE;
 }
 
