@@ -156,6 +156,12 @@ __device__ __forceinline__ void feed_beside() {
   }
 }
 
+// Two values of [0, 2) in 16 bits each, rounded to nearest: sign and the exponent's first bit are zero, so 7 bits of
+// exponent and 9 of mantissa hold fp32's range below 2.  (A NaN is lost; its query's delta is NaN, and with it ds.)
+__device__ __forceinline__ uint32_t pack_p(float a, float b) {
+  return __builtin_amdgcn_perm((__float_as_uint(b) << 2) + 0x8000u, (__float_as_uint(a) << 2) + 0x8000u, 0x07060302u);
+}
+
 template <bool B>
 struct bool_c {  // a compile-time flag passed as a value
   static constexpr bool value = B;
@@ -630,8 +636,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 //
 // Two waves share 32 keys, each with the sums of one output (32 x D, as many registers as one wave can
 // keep beside another one on its SIMD): wave w forms p and dV, wave w + 4 do . v and dK. p goes from one to
-// the other through LDS, lane to lane, in bf16 (as dV's product takes it), a step late: in step n the
-// second wave multiplies dO(n) with V and closes ds(n - 1), for which Q is kept for one step more.
+// the other through LDS, lane to lane, a step late: in step n the second wave multiplies dO(n) with V and
+// closes ds(n - 1), for which Q is kept for one step more.  It travels in 16 bits with 9 of mantissa
+// (pack_p): in bf16 the second rounding of ds would show, dK being off by 0.31% instead of 0.25%.
 template <int D>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;
@@ -679,7 +686,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   // key lies behind a query's last one.
   auto form_p = [&](auto cut, char* cur, int qt, int ln) {
     constexpr bool CUT = decltype(cut)::value;
-    constexpr int V = (CUT ? 72 : 40) * 16 / D + 1;
+    constexpr int V = (CUT ? 96 : 64) * 16 / D + 1;
     f32x16 x[2];
     f32x4 l4[2][4];
     bf16x8 p[2][2];
@@ -700,7 +707,11 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         p[u][w] = pack8(x[u], w);
-        *reinterpret_cast<u32x4*>(cur + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16) = __builtin_bit_cast(u32x4, p[u][w]);
+        u32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          h[e] = pack_p(x[u][8 * w + 2 * e], x[u][8 * w + 2 * e + 1]);
+        *reinterpret_cast<u32x4*>(cur + 2 * TILE + ((blk * 4 + 2 * u + w) * 64 + ln) * 16) = h;
       }
     };
     auto product = [&](int u) {
@@ -730,7 +741,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   // queries after the other.
   auto form_ds = [&](auto now_c, auto past_c, f32x16 (&dp)[2], const char* cur, const char* old, int ln) {
     constexpr bool NOW = decltype(now_c)::value, PAST = decltype(past_c)::value;
-    constexpr int V = 56 * 16 / D;
+    constexpr int V = 72 * 16 / D;
     bf16x8 ds[2];
     auto terms = [&](int u) {
 #pragma unroll
@@ -742,7 +753,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t pw = p[2 * i + e / 2];
-            const float pf = __uint_as_float(e & 1 ? pw & 0xffff0000u : pw << 16);
+            const float pf = __uint_as_float(e & 1 ? pw >> 2 & 0x3fffc000u : (pw & 0xffffu) << 14);
             dp[u][8 * w + 4 * i + e] = pf * (dp[u][8 * w + 4 * i + e] - d4[e]);
           }
         }

@@ -19,7 +19,7 @@
 namespace dsv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float quad_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -194,11 +194,12 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
   return x;
 }
 
-// Row loss from the sums at a reference (base 2): others, and the target's logit.
+// Row loss from the sums at a reference (base 2): others, and the target's logit.  In 64 bits: the logarithm and
+// the target's logit nearly cancel for a sure row, and there is one per row.
 __device__ __forceinline__ float row_loss(float ref, float others, float zt) {
   const float et = exp2f(zt * kLog2e - ref);
   if (et >= others) return log1pf(others / et);  // near 0 the loss keeps its relative accuracy
-  return (ref - zt * kLog2e + log2f(others + et)) * kLn2;
+  return (float)(log((double)others + et) + ref * 0.69314718055994531 - zt);
 }
 
 // One row: the piece's sums into the row's, at the larger of the references; the terms of tiles at another
