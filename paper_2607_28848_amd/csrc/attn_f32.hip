@@ -6,8 +6,11 @@
 // and the scores of a tile, as the matrix core leaves them (four keys of one query per lane, or four
 // queries of one key), are the second product's operand where they are.
 //
-// Bounds: the matrix core (two products of D = 64 at 16 x 16 tiles need one LDS read per step) and,
-// for the small batches that this mode serves, the latency of one tile after the other.
+// A workgroup has 16 queries (or keys) of one head, and its waves take 16 keys (queries) each by turns, straight
+// from global memory (the rows that several workgroups read come from L2), and add their sums at the end: the
+// batches of this mode are small, and what bounds them is the number of tiles that one wave walks one after the other.
+// Two samples of 96 and three of 157 rows, 8 heads on 2 of 64, both directions: 44 us (four waves on 64 rows
+// with staged tiles: 135).
 #include <hip/hip_runtime.h>
 
 #include "attn.h"
@@ -17,7 +20,7 @@
 namespace dsv {
 namespace {
 
-constexpr int kTK = 32;  // rows of the staged tiles (keys in forward and dQ, queries in dK and dV)
+static_assert(kAttnF32Rows == 16, "rows of a tile");
 
 __device__ __forceinline__ float quad_max(float x) {  // over the four lanes l, l ^ 16, l ^ 32, l ^ 48
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -48,201 +51,232 @@ __device__ __forceinline__ void load_quarter(const AttnView& t, int64_t row, int
   }
 }
 
-// Rows [r0, r0 + kTK) of a head into LDS, rows from r_end on as zeros.
+// C[row][col] = the dot product of the lanes' rows a (as rows of C) and b (as columns).
 template <int D>
-__device__ __forceinline__ void stage(const AttnView& t, int64_t base, int r0, int r_end, int h, float* lds) {
-  constexpr int LD = D + 4;
-  const float* p = static_cast<const float*>(t.ptr) + h * t.head;
-  for (int i = threadIdx.x; i < kTK * D / 4; i += 256) {
-    const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    const bool in = r0 + r < r_end;
-    const f32x4 v = in ? *reinterpret_cast<const f32x4*>(p + (base + r0 + r) * t.row + c) : f32x4{0.f, 0.f, 0.f, 0.f};
-    *reinterpret_cast<f32x4*>(lds + r * LD + c) = v;
-  }
-}
-
-// C[row][col] = sum over D of the staged rows 16 sub .. and the lane's own row x.
-template <int D>
-__device__ __forceinline__ f32x4 dot_tile(const float* lds, int sub, const float (&x)[D / 4]) {
-  const int lane = threadIdx.x & 63;
-  const float* p = lds + (16 * sub + (lane & 15)) * (D + 4) + (lane >> 4) * (D / 4);
+__device__ __forceinline__ f32x4 dot_tile(const float (&a)[D / 4], const float (&b)[D / 4]) {
   f32x4 c = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int s = 0; s < D / 4; s += 4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p + s);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], x[s + e], c, 0, 0, 0);
-  }
+  for (int s = 0; s < D / 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
   return c;
 }
 
-// acc[d][lane's column] += sum over the staged rows 16 sub + 4 (l / 16) + v of row[d] w[v].
+// Values [16 t + l % 16] of rows r0 + 4 (l / 16) + v, rows from r_end on as zeros.
 template <int D>
-__device__ __forceinline__ void add_rows(const float* lds, int sub, f32x4 w, f32x4 (&acc)[D / 16]) {
+__device__ __forceinline__ void load_columns(const AttnView& t, int64_t base, int r0, int r_end, int h,
+                                             float (&x)[4][D / 16]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    const float* p = lds + (16 * sub + 4 * (lane >> 4) + v) * (D + 4) + (lane & 15);
+    const int r = r0 + 4 * (lane >> 4) + v;
+    const float* p = static_cast<const float*>(t.ptr) + (base + r) * t.row + h * t.head + (lane & 15);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[16 * t], w[v], acc[t], 0, 0, 0);
+    for (int i = 0; i < D / 16; ++i) x[v][i] = r < r_end ? p[16 * i] : 0.f;
   }
 }
 
+// acc[d][lane's column] += sum over the loaded rows of row[d] w[v].
 template <int D>
-__device__ __forceinline__ void store_row(const AttnView& t, int64_t row, int h, const f32x4 (&acc)[D / 16], float f) {
-  float* p = static_cast<float*>(t.ptr) + row * t.row + h * t.head + 4 * (threadIdx.x >> 4 & 3);
+__device__ __forceinline__ void add_rows(const float (&x)[4][D / 16], f32x4 w, f32x4 (&acc)[D / 16]) {
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i)
-    *reinterpret_cast<f32x4*>(p + 16 * i) = f32x4{acc[i][0] * f, acc[i][1] * f, acc[i][2] * f, acc[i][3] * f};
+  for (int v = 0; v < 4; ++v)
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[v][t], w[v], acc[t], 0, 0, 0);
 }
 
-// 64 queries of one head, 16 a wave, over the keys that the last of them sees.
+template <int D>
+__device__ __forceinline__ void clear(f32x4 (&acc)[D / 16]) {
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// The waves' sums times f, through LDS: afterwards red[wave][row][d].
+template <int D>
+__device__ __forceinline__ void spread(const f32x4 (&acc)[D / 16], float f, float* red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* p = red + (wave * 16 + (lane & 15)) * (D + 4) + 4 * (lane >> 4);
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t)
+    *reinterpret_cast<f32x4*>(p + 16 * t) = f32x4{acc[t][0] * f, acc[t][1] * f, acc[t][2] * f, acc[t][3] * f};
+}
+// Elements c .. c + 3 of row r, the waves' parts added in order.
+template <int D, int NW>
+__device__ __forceinline__ f32x4 gather(const float* red, int r, int c) {
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) x += *reinterpret_cast<const f32x4*>(red + (w * 16 + r) * (D + 4) + c);
+  return x;
+}
+
+// 16 queries of one head over the keys that the last of them sees.
 template <int D>
 __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) float ks[kTK * (D + 4)], vs[kTK * (D + 4)];
+  constexpr int NW = 4;
+  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
+  __shared__ float ml[2][NW][16];
   const int item = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
   const Seq s(a, a.items[2 * item]);
   const int qt = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
-  const int q = qt + 16 * wave + l15;  // the lane's query
-  const int off = s.kl - s.ql;
+  const int q = qt + l15, off = s.kl - s.ql;  // the lane's query
   float qv[D / 4];
   load_quarter<D>(a.Q, (int64_t)s.q0 + q, h, q < s.ql, qv);
   f32x4 acc[D / 16];
-#pragma unroll
-  for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  clear<D>(acc);
   float m = -INFINITY, l = 0.f;
-  const int k_end = min(s.kl, min(qt + kAttnF32Rows, s.ql) + off);
-  for (int kt = 0; kt < k_end; kt += kTK) {
-    __syncthreads();
-    stage<D>(a.K, s.k0, kt, s.kl, h / a.group, ks);
-    stage<D>(a.V, s.k0, kt, s.kl, h / a.group, vs);
-    __syncthreads();
-    f32x4 x[kTK / 16];
+  const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
+  for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
+    float kv[D / 4], vv[4][D / 16];
+    load_quarter<D>(a.K, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, kv);
+    load_columns<D>(a.V, s.k0, kt, s.kl, h / a.group, vv);
+    f32x4 x = dot_tile<D>(kv, qv);
     float mx = m;
 #pragma unroll
-    for (int u = 0; u < kTK / 16; ++u) {
-      x[u] = dot_tile<D>(ks, u, qv);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        x[u][v] = kt + 16 * u + 4 * (lane >> 4) + v <= q + off ? x[u][v] * a.scale : -INFINITY;
-        mx = fmaxf(mx, x[u][v]);
-      }
+    for (int v = 0; v < 4; ++v) {
+      x[v] = kt + 4 * (lane >> 4) + v <= q + off ? x[v] * a.scale : -INFINITY;
+      mx = fmaxf(mx, x[v]);
     }
     mx = quad_max(mx);
     const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: every term below is exp(-inf) = 0
     const float f = expf(m - ref);
     float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < kTK / 16; ++u)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sum += x[u][v] = expf(x[u][v] - ref);
+    for (int v = 0; v < 4; ++v) sum += x[v] = expf(x[v] - ref);
     l = l * f + quad_sum(sum);
     m = mx;
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) acc[t] *= f;
-#pragma unroll
-    for (int u = 0; u < kTK / 16; ++u) add_rows<D>(vs, u, x[u], acc);
+    add_rows<D>(vv, x, acc);
   }
-  if (q >= s.ql) return;
-  store_row<D>(a.O, (int64_t)s.q0 + q, h, acc, l > 0.f ? 1.f / l : l);  // l is 0 where no key is seen, NaN stays NaN
-  if (a.lse && lane < 16) a.lse[(int64_t)h * a.n_q + s.q0 + q] = l > 0.f ? m + logf(l) : l == 0.f ? -INFINITY : l;
+  if (lane < 16) {
+    ml[0][wave][l15] = m;
+    ml[1][wave][l15] = l;
+  }
+  __syncthreads();
+  // the waves' sums at one reference
+  float ref = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) ref = fmaxf(ref, ml[0][w][l15]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) total += ml[0][w][l15] == -INFINITY ? ml[1][w][l15] : ml[1][w][l15] * expf(ml[0][w][l15] - ref);
+  spread<D>(acc, (m == -INFINITY ? 1.f : expf(m - ref)) * (total == 0.f ? 0.f : 1.f / total), red);
+  if (a.lse && wave == 0 && lane < 16 && q < s.ql)
+    a.lse[(int64_t)h * a.n_q + s.q0 + q] = total == 0.f ? -INFINITY : ref + logf(total);
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    if (qt + r < s.ql)
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.O.ptr) + ((int64_t)s.q0 + qt + r) * a.O.row + h * a.O.head + c) =
+          gather<D, NW>(red, r, c);
+  }
 }
 
-// dQ of 64 queries of one head, and delta = do . o for the launch of dK and dV.
+// dQ of 16 queries of one head, and delta = do . o for the launch of dK and dV.
 template <int D>
 __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) float ks[kTK * (D + 4)], vs[kTK * (D + 4)];
+  constexpr int NW = 4;
+  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
   const int item = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
   const Seq s(a, a.items[2 * item]);
   const int qt = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
-  const int q = qt + 16 * wave + l15;
-  const int off = s.kl - s.ql;
+  const int q = qt + l15, off = s.kl - s.ql;
   const bool in = q < s.ql;
-  float qv[D / 4], dv[D / 4], ov[D / 4];
+  float qv[D / 4], dv[D / 4], dot = 0.f;
   load_quarter<D>(a.Q, (int64_t)s.q0 + q, h, in, qv);
   load_quarter<D>(a.dO, (int64_t)s.cq + q, h, in, dv);
-  load_quarter<D>(a.O, (int64_t)s.q0 + q, h, in, ov);
-  float dot = 0.f;
+  {
+    float ov[D / 4];
+    load_quarter<D>(a.O, (int64_t)s.q0 + q, h, in, ov);
 #pragma unroll
-  for (int c = 0; c < D / 4; ++c) dot += dv[c] * ov[c];
+    for (int c = 0; c < D / 4; ++c) dot += dv[c] * ov[c];
+  }
   const float delta = quad_sum(dot);
-  if (in && lane < 16) a.delta[h * a.train_q + s.cq + q] = delta;
+  if (in && wave == 0 && lane < 16) a.delta[h * a.train_q + s.cq + q] = delta;
   const float lse = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] : 0.f;
   f32x4 acc[D / 16];
+  clear<D>(acc);
+  const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
+  for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
+    float kv[D / 4], vv[D / 4], kc[4][D / 16];
+    load_quarter<D>(a.K, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, kv);
+    load_quarter<D>(a.V, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, vv);
+    load_columns<D>(a.K, s.k0, kt, s.kl, h / a.group, kc);
+    const f32x4 x = dot_tile<D>(kv, qv), dp = dot_tile<D>(vv, dv);
+    f32x4 ds;
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int k_end = min(s.kl, min(qt + kAttnF32Rows, s.ql) + off);
-  for (int kt = 0; kt < k_end; kt += kTK) {
-    __syncthreads();
-    stage<D>(a.K, s.k0, kt, s.kl, h / a.group, ks);
-    stage<D>(a.V, s.k0, kt, s.kl, h / a.group, vs);
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kTK / 16; ++u) {
-      const f32x4 x = dot_tile<D>(ks, u, qv), dp = dot_tile<D>(vs, u, dv);
-      f32x4 ds;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const bool seen = kt + 16 * u + 4 * (lane >> 4) + v <= q + off;
-        ds[v] = seen ? expf(x[v] * a.scale - lse) * (dp[v] - delta) * a.scale : 0.f;
-      }
-      add_rows<D>(ks, u, ds, acc);
+    for (int v = 0; v < 4; ++v) {
+      const bool seen = kt + 4 * (lane >> 4) + v <= q + off;
+      ds[v] = seen ? expf(x[v] * a.scale - lse) * (dp[v] - delta) * a.scale : 0.f;
     }
+    add_rows<D>(kc, ds, acc);
   }
-  if (in) store_row<D>(a.dQ, (int64_t)s.cq + q, h, acc, 1.f);
+  spread<D>(acc, 1.f, red);
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    if (qt + r < s.ql)
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.dQ.ptr) + ((int64_t)s.cq + qt + r) * a.dQ.row + h * a.dQ.head + c) =
+          gather<D, NW>(red, r, c);
+  }
 }
 
-// dK and dV of 64 keys of one key head, 16 a wave, over the queries that see the first of them, the
-// key head's query heads one after the other (so the sums over them need no atomics).
+// dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
+// heads (so the sums over them need no atomics).
 template <int D>
-__global__ __launch_bounds__(256) void attn_f32_dk_kernel(AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) float qs[kTK * (D + 4)], os[kTK * (D + 4)];
-  __shared__ float st[2][kTK];  // lse and delta of the staged queries
+__global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
   const int item = blockIdx.x / a.hkv, g = blockIdx.x % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
-  const int k = k0 + 16 * wave + l15;  // the lane's key
-  const int off = s.kl - s.ql;
-  const bool in = k < s.kl;
+  const int k = k0 + l15, off = s.kl - s.ql;  // the lane's key
   float kv[D / 4], vv[D / 4];
-  load_quarter<D>(a.K, (int64_t)s.k0 + k, g, in, kv);
-  load_quarter<D>(a.V, (int64_t)s.k0 + k, g, in, vv);
+  load_quarter<D>(a.K, (int64_t)s.k0 + k, g, k < s.kl, kv);
+  load_quarter<D>(a.V, (int64_t)s.k0 + k, g, k < s.kl, vv);
   f32x4 dk[D / 16], dv[D / 16];
-#pragma unroll
-  for (int t = 0; t < D / 16; ++t) dk[t] = dv[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  clear<D>(dk);
+  clear<D>(dv);
   const int q_first = max(0, k0 - off);
-  for (int h = g * a.group; h < (g + 1) * a.group; ++h) {
-    for (int qt = q_first; qt < s.ql; qt += kTK) {
-      __syncthreads();
-      stage<D>(a.Q, s.q0, qt, s.ql, h, qs);
-      stage<D>(a.dO, s.cq, qt, s.ql, h, os);
-      if (threadIdx.x < kTK) {
-        const int q = min(qt + (int)threadIdx.x, s.ql - 1);
-        st[0][threadIdx.x] = a.lse[(int64_t)h * a.n_q + s.q0 + q];
-        st[1][threadIdx.x] = a.delta[h * a.train_q + s.cq + q];
-      }
-      __syncthreads();
+  const int per_head = q_first < s.ql ? (s.ql - q_first + 15) / 16 : 0;
+  for (int n = wave; n < per_head * a.group; n += NW) {
+    const int h = g * a.group + n / per_head, qt = q_first + n % per_head * 16;
+    float qv[D / 4], ov[D / 4], qc[4][D / 16], oc[4][D / 16], lse[4], delta[4];
+    load_quarter<D>(a.Q, (int64_t)s.q0 + qt + l15, h, qt + l15 < s.ql, qv);
+    load_quarter<D>(a.dO, (int64_t)s.cq + qt + l15, h, qt + l15 < s.ql, ov);
+    load_columns<D>(a.Q, s.q0, qt, s.ql, h, qc);
+    load_columns<D>(a.dO, s.cq, qt, s.ql, h, oc);
 #pragma unroll
-      for (int u = 0; u < kTK / 16; ++u) {
-        const f32x4 x = dot_tile<D>(qs, u, kv), dp = dot_tile<D>(os, u, vv);
-        f32x4 p, ds;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int r = 16 * u + 4 * (lane >> 4) + v, q = qt + r;
-          p[v] = q < s.ql && k <= q + off ? expf(x[v] * a.scale - st[0][r]) : 0.f;
-          ds[v] = q < s.ql && k <= q + off ? p[v] * (dp[v] - st[1][r]) * a.scale : 0.f;
-        }
-        add_rows<D>(os, u, p, dv);
-        add_rows<D>(qs, u, ds, dk);
-      }
+    for (int v = 0; v < 4; ++v) {
+      const int q = min(qt + 4 * (lane >> 4) + v, s.ql - 1);
+      lse[v] = a.lse[(int64_t)h * a.n_q + s.q0 + q];
+      delta[v] = a.delta[h * a.train_q + s.cq + q];
     }
+    const f32x4 x = dot_tile<D>(qv, kv), dp = dot_tile<D>(ov, vv);
+    f32x4 p, ds;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int q = qt + 4 * (lane >> 4) + v;
+      const bool seen = q < s.ql && k <= q + off;
+      p[v] = seen ? expf(x[v] * a.scale - lse[v]) : 0.f;
+      ds[v] = seen ? p[v] * (dp[v] - delta[v]) * a.scale : 0.f;
+    }
+    add_rows<D>(oc, p, dv);
+    add_rows<D>(qc, ds, dk);
   }
-  if (!in) return;
-  store_row<D>(a.dK, (int64_t)s.ck + k, g, dk, 1.f);
-  store_row<D>(a.dV, (int64_t)s.ck + k, g, dv, 1.f);
+  auto put = [&](const f32x4 (&acc)[D / 16], const AttnView& t) {
+    __syncthreads();
+    spread<D>(acc, 1.f, red);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
+      const int r = i / (D / 4), c = 4 * (i % (D / 4));
+      if (k0 + r < s.kl)
+        *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) =
+            gather<D, NW>(red, r, c);
+    }
+  };
+  put(dk, a.dK);
+  put(dv, a.dV);
 }
 
 }  // namespace
@@ -266,8 +300,8 @@ hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s) {
 hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)(a.n_items * (int64_t)a.hkv));
-  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_kernel<64>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(attn_f32_dk_kernel<128>, grid, dim3(256), 0, s, a);
+  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_kernel<64>, grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL(attn_f32_dk_kernel<128>, grid, dim3(512), 0, s, a);
   return hipGetLastError();
 }
 

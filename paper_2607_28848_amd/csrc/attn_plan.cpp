@@ -164,7 +164,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   }
 
   Tiles fwd, f32, dq, dk, f32_dq, f32_dk;
-  int64_t split_keys_all = 0;  // keys that the split form's tiles read
+  int64_t split_keys_all = 0, split_most = 0;  // keys that the split form's tiles read; the longest sequence's
   std::vector<int32_t> split;
   for (int32_t i = 0; i < n; ++i) {
     const dsv_attn_seq& s = seqs[i];
@@ -175,6 +175,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
       split.push_back(i);
       const int64_t tiles = ((int64_t)s.q_len * group + kAttnPackRows - 1) / kAttnPackRows;
       split_keys_all += tiles * s.k_len;
+      split_most = std::max<int64_t>(split_most, s.k_len);
     } else {
       for (int64_t q = 0; q < s.q_len; q += kAttnFwdRows)
         fwd.add((keys_seen(s, std::min<int64_t>(q + kAttnFwdRows, s.q_len) - 1) + 63) / 64, i, q);
@@ -197,6 +198,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   // kAttnSplitTarget workgroups.
   int64_t piece = (split_keys_all * hkv + kAttnSplitTarget - 1) / kAttnSplitTarget;
   piece = std::max<int64_t>(kAttnPieceKeys, (piece + kAttnPieceKeys - 1) / kAttnPieceKeys * kAttnPieceKeys);
+  if (split_most <= kAttnWholeKeys) piece = kAttnWholeKeys;
   std::vector<int32_t> split_items, split_keys, join_items;
   for (int32_t i : split) {
     const dsv_attn_seq& s = seqs[i];

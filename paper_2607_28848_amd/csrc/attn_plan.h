@@ -15,14 +15,17 @@ constexpr int kAttnSeqWords = 8;
 // Rows of a forward tile (bf16), of a gradient tile (bf16: queries, keys) and of the fp32 tiles.
 constexpr int kAttnFwdRows = 128;
 constexpr int kAttnBwdRows = 128;
-constexpr int kAttnF32Rows = 64;
+constexpr int kAttnF32Rows = 16;
 // A sequence of up to kAttnSplitQ queries takes the split form: the (query, head) pairs of a
 // key head form rows, kAttnPackRows to a tile, and the keys are split into pieces.
 constexpr int kAttnSplitQ = 16;
 constexpr int kAttnPackRows = 32;
-// Pieces of the split form: multiples of kAttnPieceKeys keys (each of the workgroup's four waves
-// takes blocks of 32 of them by turns), as many as bring about kAttnSplitTarget workgroups.
-constexpr int kAttnPieceKeys = 128;
+// Pieces of the split form: multiples of kAttnPieceKeys keys (each of the workgroup's four waves takes blocks of
+// 32 of them by turns), as many as bring about kAttnSplitTarget workgroups.  Where no sequence has more than
+// kAttnWholeKeys keys each is one piece: a wave walks 8 blocks in the 5 us that the join's launch takes
+// (8 sequences of 400 keys: 11.5 us in pieces of 128, 8.6 whole).
+constexpr int kAttnPieceKeys = 256;
+constexpr int kAttnWholeKeys = 1024;
 constexpr int kAttnSplitTarget = 512;
 
 // A forward or key tile with far more work than its share of the device (few tiles over long rows: a
