@@ -25,8 +25,6 @@ struct AttnArgs {
   float* lse;            // nullptr: not written (forward)
   float* delta;          // do . o of the compact rows, [hq][train_q]
   float* lse2;           // bf16: lse of the compact rows, base 2
-  // split form
-  const int32_t* split_keys;
   // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
   // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
   // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].

@@ -360,10 +360,9 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char b1[kBuf];
   __shared__ float ml[2][4][32];
   const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
-  const int32_t* it = a.items + 4 * (int64_t)item;
-  const Seq s(a, it[0]);
-  const int r0 = it[1], n_pieces = it[3];
-  const int k_first = a.split_keys[2 * (int64_t)item], k_last = a.split_keys[2 * (int64_t)item + 1];
+  const int32_t* it = a.items + kAttnSplitWords * (int64_t)item;
+  const struct { int q0, ql, k0, kl; } s = {it[0], it[1], it[2], it[3]};
+  const int r0 = it[4], n_pieces = it[5], k_first = it[7], k_last = it[8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int off = s.kl - s.ql, rows = s.ql * a.group;
   const int r = r0 + (lane & 31), q = min(r, rows - 1) / a.group, h = hk * a.group + min(r, rows - 1) % a.group;
@@ -376,10 +375,10 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   };
   constexpr int LOADS = 2 * TILE / 1024;
   const int kb = k_first + TK * wave;
+  if (kb < k_last) load(kb, w0);
   bf16x8 qf[D / 16];
   row_frags<D>(a.Q, (int64_t)s.q0 + q, h, r < rows, qf);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the counts below are the staged loads alone
-  if (kb < k_last) load(kb, w0);
+  asm volatile("" ::: "memory");  // before the next block's loads: what step() waits for covers them
   f32x16 acc[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
@@ -397,8 +396,11 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
     asm volatile("" ::: "memory");
     f32x16 x[1];
     x[0] = zero16();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) x[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, 0, i), qf[i], x[0], 0, 0, 0);
+    feed<D / 16, 1, D / 16>();
+    __builtin_amdgcn_sched_barrier(0);
     if (kt + TK - 1 > all || kt + TK > k_last) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -406,6 +408,7 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
     }
     softmax_ref(x, c, run, acc);
     const float base = run.ref == -INFINITY ? 0.f : run.ref;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const bf16x8 p = softmax_terms(x[0], w, c, base, run.sum);
@@ -413,6 +416,8 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
       for (int t = 0; t < D / 32; ++t)
         acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_t<D>(cur + TILE, w, t), p, acc[t], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x100, D / 8, 0);
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // `cur` is read before it is loaded again
   };
   for (int kt = kb; kt < k_last; kt += 8 * TK) {
@@ -448,7 +453,7 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   const bool whole = n_pieces == 1;
   const float g = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
   const int qr = (r0 + row) / a.group, hr = hk * a.group + (r0 + row) % a.group;
-  const int64_t slot = (int64_t)item * a.hkv + hk;
+  const int64_t slot = (int64_t)it[6] * a.hkv + hk;
 #pragma unroll
   for (int i = 0; i < D / 8; i += 4) {
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -503,13 +508,12 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int64_t first, int64
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
-  const int32_t* it = a.items + 4 * (int64_t)item;
-  if (it[3] == 1) return;  // written by its only piece
-  const Seq s(a, it[0]);
-  const int row = threadIdx.x >> 3, r = it[1] + row;
-  if (r >= s.ql * a.group) return;
-  join_row<D>(a, (int64_t)it[2] * a.hkv + hk, a.hkv, it[3], kAttnPackRows, row, (threadIdx.x & 7) * (D / 8),
-              (int64_t)s.q0 + r / a.group, hk * a.group + r % a.group);
+  const int32_t* it = a.items + kAttnSplitWords * (int64_t)item;
+  if (it[5] == 1) return;  // written by its only piece
+  const int row = threadIdx.x >> 3, r = it[4] + row;
+  if (r >= it[1] * a.group) return;
+  join_row<D>(a, (int64_t)it[6] * a.hkv + hk, a.hkv, it[5], kAttnPackRows, row, (threadIdx.x & 7) * (D / 8),
+              (int64_t)it[0] + r / a.group, hk * a.group + r % a.group);
 }
 
 // Forward tiles: 32 rows a workgroup.
@@ -994,7 +998,6 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   e = launch(attn_fwd_join_kernel<64>, attn_fwd_join_kernel<128>, a, p->n_fwd_join * hq * (kAttnFwdRows / 32), s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.split_items);
-  a.split_keys = p->dptr(p->lay.split_keys);
   a.part_o = at<float>(ws, w.split_o);
   a.part_ml = at<float>(ws, w.split_ml);
   e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, p->n_split * hkv, s);

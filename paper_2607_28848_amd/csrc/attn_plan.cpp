@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <functional>
 #include <new>
 #include <numeric>
@@ -194,12 +195,13 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     for (int64_t k = 0; k < s.k_len; k += kAttnF32Rows) f32_dk.add(seen_by(k), i, k);
   }
 
-  // Pieces: one length for the whole call, such that all tiles' pieces are about
-  // kAttnSplitTarget workgroups.
-  int64_t piece = (split_keys_all * hkv + kAttnSplitTarget - 1) / kAttnSplitTarget;
+  // Pieces: one length for the whole call
+  const int64_t target = d == 128 ? kAttnSplitTarget : 2 * kAttnSplitTarget;
+  int64_t piece = (split_keys_all * hkv + target - 1) / target;
   piece = std::max<int64_t>(kAttnPieceKeys, (piece + kAttnPieceKeys - 1) / kAttnPieceKeys * kAttnPieceKeys);
   if (split_most <= kAttnWholeKeys) piece = kAttnWholeKeys;
-  std::vector<int32_t> split_items, split_keys, join_items;
+  std::vector<std::array<int32_t, kAttnSplitWords>> pieces;
+  std::vector<int32_t> split_items, join_items;
   for (int32_t i : split) {
     const dsv_attn_seq& s = seqs[i];
     const int64_t rows = (int64_t)s.q_len * group;
@@ -207,16 +209,18 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     const int64_t np = std::max<int64_t>(1, (s.k_len + piece - 1) / piece);
     const int64_t len = std::max<int64_t>(32, ((s.k_len + np - 1) / np + 31) / 32 * 32);
     for (int64_t r = 0; r < rows; r += kAttnPackRows) {
-      const int64_t first = (int64_t)split_items.size() / 4;
-      if (first + np > INT32_MAX) return DSV_ERR_SIZE;
-      join_items.insert(join_items.end(), {i, (int32_t)r, (int32_t)first, (int32_t)np});
-      for (int64_t k = 0; k < np; ++k) {
-        split_items.insert(split_items.end(), {i, (int32_t)r, (int32_t)k, (int32_t)np});
-        split_keys.insert(split_keys.end(), {(int32_t)std::min<int64_t>(k * len, s.k_len),
-                                             (int32_t)std::min<int64_t>((k + 1) * len, s.k_len)});
-      }
+      const int64_t first = (int64_t)pieces.size();
+      if (first + np > INT32_MAX / kAttnSplitWords) return DSV_ERR_SIZE;
+      join_items.insert(join_items.end(), {s.q_start, s.q_len, s.k_start, s.k_len, (int32_t)r, (int32_t)np, (int32_t)first, 0,
+                                           s.k_len, 0, 0, 0});
+      for (int64_t k = 0; k < np; ++k)
+        pieces.push_back({s.q_start, s.q_len, s.k_start, s.k_len, (int32_t)r, (int32_t)np, (int32_t)(first + k),
+                          (int32_t)std::min<int64_t>(k * len, s.k_len), (int32_t)std::min<int64_t>((k + 1) * len, s.k_len), 0,
+                          0, 0});
     }
   }
+  std::stable_sort(pieces.begin(), pieces.end(), [](const auto& a, const auto& b) { return a[8] - a[7] > b[8] - b[7]; });
+  for (const auto& w : pieces) split_items.insert(split_items.end(), w.begin(), w.end());
 
   std::vector<int32_t>& m = p.meta;
   auto put = [&](const std::vector<int32_t>& w) {
@@ -238,8 +242,8 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
                              w3k = f32_dk.words();
   int64_t most = std::max(p.n_fwd, p.n_dk);
   most = std::max(most, count(w3, 2, &p.n_f32));
-  most = std::max(most, count(split_items, 4, &p.n_split));
-  most = std::max(most, count(join_items, 4, &p.n_join));
+  most = std::max(most, count(split_items, kAttnSplitWords, &p.n_split));
+  most = std::max(most, count(join_items, kAttnSplitWords, &p.n_join));
   most = std::max(most, count(wq, 2, &p.n_dq));
   most = std::max(most, count(w3q, 2, &p.n_f32_dq));
   most = std::max(most, count(w3k, 2, &p.n_f32_dk));
@@ -249,7 +253,6 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   L.fwd_join = put(cf.join);
   L.f32_items = put(w3);
   L.split_items = put(split_items);
-  L.split_keys = put(split_keys);
   L.join_items = put(join_items);
   L.dq_items = put(wq);
   L.dk_items = put(ck.items);

@@ -21,12 +21,13 @@ constexpr int kAttnF32Rows = 16;
 constexpr int kAttnSplitQ = 16;
 constexpr int kAttnPackRows = 32;
 // Pieces of the split form: multiples of kAttnPieceKeys keys (each of the workgroup's four waves takes blocks of
-// 32 of them by turns), as many as bring about kAttnSplitTarget workgroups.  Where no sequence has more than
-// kAttnWholeKeys keys each is one piece: a wave walks 8 blocks in the 5 us that the join's launch takes
-// (8 sequences of 400 keys: 11.5 us in pieces of 128, 8.6 whole).
+// 32 of them by turns), of a length that makes about as many as run at a time (one workgroup per CU with heads of
+// 128, two with 64; 64 sequences of 2600 keys: 104 us in 536 pieces, 114 in 1144).  Where no sequence has more than
+// kAttnWholeKeys keys each is one piece: the join's launch costs more than the shorter walk saves
+// (8 sequences of 400 keys: 12.4 us in pieces of 128, 10.9 whole).
 constexpr int kAttnPieceKeys = 256;
 constexpr int kAttnWholeKeys = 1024;
-constexpr int kAttnSplitTarget = 512;
+constexpr int kAttnSplitTarget = 256;
 
 // A forward or key tile with far more work than its share of the device (few tiles over long rows: a
 // chunk behind a long prefix, short batches' gradients) is cut along its sum into pieces, whose fp32 sums a
@@ -39,15 +40,19 @@ constexpr int kAttnPieceSteps = 8;
 // tile descriptor: {sequence, first row, first step, last step + 1, slot of its sums, pieces, 0, 0}
 constexpr int kAttnTileWords = 8;
 
+// split form descriptor: {q_start, q_len, k_start, k_len, first row, pieces, slot (join: the first one's), first key,
+// last key + 1, 0, 0, 0}.  The sequence's fields stand in the item: short calls wait for every load that
+// another one's address depends on.
+constexpr int kAttnSplitWords = 12;
+
 // Word offsets inside the packed blob (int32 words).
 struct AttnLayout {
   int64_t seqs;         // [n_seqs][kAttnSeqWords]
   int64_t fwd_items;    // [n_fwd][kAttnTileWords]: bf16 forward tiles or their pieces, steps of 64 keys
   int64_t fwd_join;     // [n_fwd_join][4] {sequence, first query, first slot, pieces}
   int64_t f32_items;    // [n_f32][2] {sequence, first query}: fp32 forward tiles of every sequence
-  int64_t split_items;  // [n_split][4] {sequence, first row, piece, n_pieces}: pieces of the split form
-  int64_t split_keys;   // [n_split][2] {first key, last key + 1}
-  int64_t join_items;   // [n_join][4] {sequence, first row, first piece (index into split_items), n_pieces}
+  int64_t split_items;  // [n_split][kAttnSplitWords]: pieces of the split form, longest first
+  int64_t join_items;   // [n_join][kAttnSplitWords]: its tiles
   int64_t dq_items;     // [n_dq][2] {sequence, first query}: fine-tuning samples, most keys first
   int64_t dk_items;     // [n_dk][kAttnTileWords]: fine-tuning samples, steps of 64 queries of one head
   int64_t dk_join;      // [n_dk_join][4]

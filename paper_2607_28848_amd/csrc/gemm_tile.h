@@ -44,10 +44,12 @@ __device__ __forceinline__ void tile_at(int lin, int n_m, int n_n, int& mt, int&
 }
 
 // P: the tile's first row; p_rows, q_cols: rows and columns that exist; C: contraction length.
+// turn: the step of 64 to begin with.  Tiles that run together and whose rows lie a power of two apart read from the
+// same memory channels when they walk the contraction in step.
 // Returns the buffer that the last step did not use.
 template <bool NN, int FM>
 __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, int p_rows, const uint16_t* Q, int64_t ldq_,
-                                              int q_cols, int C, char* smem0, char* smem1, f32x4 (&acc)[FM][8]) {
+                                              int q_cols, int C, int turn, char* smem0, char* smem1, f32x4 (&acc)[FM][8]) {
   constexpr int WM = 16 * FM, TM = 2 * WM, TN = 256, TK = 64, FN = 8, ROWB = TK * 2;
   constexpr int A_BYTES = TM * ROWB, LOADS = 8, LOADS_A = FM;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -55,8 +57,10 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
   const int ld = (int)ldp, ldq = (int)ldq_, nk = (C + TK - 1) / TK;
   auto buf = [&](int stage) { return stage ? smem1 : smem0; };
   auto rswz = [](int row) { return (row ^ (row >> 3)) & 7; };
-  const i32x4 ra = tile_rsrc(P, (int64_t)min(TM, p_rows) * ld * 2);
-  const i32x4 rb = NN ? tile_rsrc(Q, ((int64_t)C * ldq - (ldq - q_cols)) * 2) : tile_rsrc(Q, (int64_t)min(TN, q_cols) * ldq * 2);
+  // from the tile's first value to its last row's last one (P: rows are read eight values at a time)
+  const i32x4 ra = tile_rsrc(P, ((int64_t)(min(TM, p_rows) - 1) * ld + ((C + 7) & ~7)) * 2);
+  const i32x4 rb = NN ? tile_rsrc(Q, ((int64_t)(C - 1) * ldq + q_cols) * 2)
+                      : tile_rsrc(Q, ((int64_t)(min(TN, q_cols) - 1) * ldq + C) * 2);
   int voff_a[LOADS_A], voff_b[NN ? 2 : LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS_A; ++i) voff_a[i] = ((((lane & 7) ^ lr ^ ((LOADS_A * wave + i) & 7)) << 4)) + lr * ld * 2;
@@ -68,19 +72,22 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) voff_b[i] = (((lane & 7) ^ lr ^ i) << 4) + lr * ldq * 2;
   }
+  // Steps in the order turn, turn + 1, .., nk - 1, 0, .. (where all are whole).
+  const int first = C % TK == 0 ? turn % nk : 0;
+  auto at = [&](int kt) { return kt + first < nk ? kt + first : kt + first - nk; };
   auto load_a = [&](int kt, char* st, int i) {
     const int q = wave * LOADS_A + i;
     llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16, voff_a[i],
-                                      __builtin_amdgcn_readfirstlane(q * 16 * ld + kt * TK * 2), 0, 0);
+                                      __builtin_amdgcn_readfirstlane(q * 16 * ld + at(kt) * TK * 2), 0, 0);
   };
   auto load_b = [&](int kt, char* st, int i) {
     const int q = wave * LOADS + i;
     if constexpr (NN)
       llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i & 1],
-                                        __builtin_amdgcn_readfirstlane((kt * TK + 2 * q) * ldq * 2), 0, 0);
+                                        __builtin_amdgcn_readfirstlane((at(kt) * TK + 2 * q) * ldq * 2), 0, 0);
     else
       llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i],
-                                        __builtin_amdgcn_readfirstlane(q * 16 * ldq + kt * TK * 2), 0, 0);
+                                        __builtin_amdgcn_readfirstlane(q * 16 * ldq + at(kt) * TK * 2), 0, 0);
   };
   // any step: chunks past the contraction read zeros (C is a multiple of 8, or the rows hold zeros from C on)
   auto issue = [&](int kt, int stage) {

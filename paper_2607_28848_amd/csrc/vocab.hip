@@ -45,9 +45,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4;
   f32x4 acc[FM][8];
+  // with one row tile the head's rows come from memory once, and neighbouring tiles begin a step apart (one row
+  // against 128256 of 4096: 215 us in step, 185 so; with more row tiles it changes nothing)
   char* const idle = tile_product<false, FM>(static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
                                              static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols,
-                                             a.K, smem0, smem1, acc);
+                                             a.K,
+                                             n_m == 1 ? nt : 0, smem0, smem1, acc);
   const int c0 = wn * 128 + 4 * g4;  // column of acc[.][j][v]: c0 + 16 j + v
   // The sums are read twice and never written: in registers of the matrix core from the first to the last.
 #pragma unroll
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   }
   f32x4 acc[FM][8];
   tile_product<NN, FM>(static_cast<const uint16_t*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0, W, NN ? a.ldw : a.ldwt,
-                       a.K - n0, C, smem0, smem1, acc);
+                       a.K - n0, C, 0, smem0, smem1, acc);
   put([&](int i, int j) { return acc[i][j]; });
 }
 
