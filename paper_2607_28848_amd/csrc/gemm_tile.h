@@ -1,10 +1,10 @@
-// gemm_tile.h -- the contraction loop of a 256-column bf16 tile (v_mfma_f32_16x16x32_bf16) as a function
-// that leaves the fp32 sums in registers for the caller's epilogue.
+// gemm_tile.h -- the contraction loops of a 256-column bf16 tile (v_mfma_f32_16x16x32_bf16) as functions
+// that leave the fp32 sums in registers for the caller's epilogue.
 //
+//   tile_nt: out[m][n] = sum_c P[m][c] Q[n][c]      tile_nn: out[m][n] = sum_c P[m][c] Q[c][n]
 // 4 waves in a 2 x 2 grid, each FM x 8 blocks of 16 x 16 (FM 8: 256 rows, FM 4: 128).  Operand tiles go
-// from global memory straight into LDS, two buffers; one barrier per step of 64.  Rows and columns past
-// the operands, and contraction values past C, read zeros.
-//   NT: out[m][n] = sum_c P[m][c] Q[n][c]      NN: out[m][n] = sum_c P[m][c] Q[c][n]
+// from global memory straight into LDS.  Rows and columns past the operands, and contraction values past C,
+// read zeros.
 // Sums: acc[i][j][v] is row wm * 16 FM + 16 i + l % 16, column wn * 128 + 16 j + 4 (l / 16) + v.
 #pragma once
 
@@ -17,7 +17,18 @@ extern "C" __device__ void llvm_amdgcn_raw_buffer_load_lds_t(i32x4 rsrc, lds_u32
                                                              int soffset, int offset,
                                                              int aux) __asm("llvm.amdgcn.raw.buffer.load.lds");
 
-constexpr int kTileStage = 2 * 256 * 64 * 2;  // bytes of one buffer (FM 8)
+template <bool B>
+struct flag_c {  // a compile-time flag passed as a value
+  static constexpr bool value = B;
+};
+
+template <int V>
+struct num_c {
+  static constexpr int value = V;
+};
+
+constexpr int kTileStage = 2 * 256 * 64 * 2;    // bytes of one of tile_nt's two buffers (FM 8)
+constexpr int kTileStageNN = 2 * 256 * 32 * 2;  // bytes of one of tile_nn's four buffers (FM 8)
 
 // Descriptor over `bytes` bytes (at most 2^31) from base.
 __device__ __forceinline__ i32x4 tile_rsrc(const void* base, int64_t bytes) {
@@ -43,12 +54,13 @@ __device__ __forceinline__ void tile_at(int lin, int n_m, int n_n, int& mt, int&
   nt = (lin % span) / size;
 }
 
-// P: the tile's first row; p_rows, q_cols: rows and columns that exist; C: contraction length.
+// P: the tile's first row; p_rows, q_cols: rows and columns that exist; C: contraction length.  Steps of 64 through two
+// buffers, a barrier each.
 // turn: the step of 64 to begin with.  Tiles that run together and whose rows lie a power of two apart read from the
 // same memory channels when they walk the contraction in step.
 // Returns the buffer that the last step did not use.
-template <bool NN, int FM>
-__device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, int p_rows, const uint16_t* Q, int64_t ldq_,
+template <int FM>
+__device__ __forceinline__ char* tile_nt(const uint16_t* P, int64_t ldp, int p_rows, const uint16_t* Q, int64_t ldq_,
                                               int q_cols, int C, int turn, char* smem0, char* smem1, f32x4 (&acc)[FM][8]) {
   constexpr int WM = 16 * FM, TM = 2 * WM, TN = 256, TK = 64, FN = 8, ROWB = TK * 2;
   constexpr int A_BYTES = TM * ROWB, LOADS = 8, LOADS_A = FM;
@@ -59,19 +71,12 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
   auto rswz = [](int row) { return (row ^ (row >> 3)) & 7; };
   // from the tile's first value to its last row's last one (P: rows are read eight values at a time)
   const i32x4 ra = tile_rsrc(P, ((int64_t)(min(TM, p_rows) - 1) * ld + ((C + 7) & ~7)) * 2);
-  const i32x4 rb = NN ? tile_rsrc(Q, ((int64_t)(C - 1) * ldq + q_cols) * 2)
-                      : tile_rsrc(Q, ((int64_t)(min(TN, q_cols) - 1) * ldq + C) * 2);
-  int voff_a[LOADS_A], voff_b[NN ? 2 : LOADS];
+  const i32x4 rb = tile_rsrc(Q, ((int64_t)(min(TN, q_cols) - 1) * ldq + C) * 2);
+  int voff_a[LOADS_A], voff_b[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS_A; ++i) voff_a[i] = ((((lane & 7) ^ lr ^ ((LOADS_A * wave + i) & 7)) << 4)) + lr * ld * 2;
-  if constexpr (NN) {
 #pragma unroll
-    for (int par = 0; par < 2; ++par)
-      voff_b[par] = ((lane >> 5) * ldq + 8 * ((lane & 31) ^ 2 * ((2 * par + (lane >> 5)) & 3))) * 2;
-  } else {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) voff_b[i] = (((lane & 7) ^ lr ^ i) << 4) + lr * ldq * 2;
-  }
+  for (int i = 0; i < LOADS; ++i) voff_b[i] = (((lane & 7) ^ lr ^ i) << 4) + lr * ldq * 2;
   // Steps in the order turn, turn + 1, .., nk - 1, 0, .. (where all are whole).
   const int first = C % TK == 0 ? turn % nk : 0;
   auto at = [&](int kt) { return kt + first < nk ? kt + first : kt + first - nk; };
@@ -82,12 +87,8 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
   };
   auto load_b = [&](int kt, char* st, int i) {
     const int q = wave * LOADS + i;
-    if constexpr (NN)
-      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i & 1],
-                                        __builtin_amdgcn_readfirstlane((at(kt) * TK + 2 * q) * ldq * 2), 0, 0);
-    else
-      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i],
-                                        __builtin_amdgcn_readfirstlane(q * 16 * ldq + at(kt) * TK * 2), 0, 0);
+    llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[i],
+                                      __builtin_amdgcn_readfirstlane(q * 16 * ldq + at(kt) * TK * 2), 0, 0);
   };
   // any step: chunks past the contraction read zeros (C is a multiple of 8, or the rows hold zeros from C on)
   auto issue = [&](int kt, int stage) {
@@ -108,13 +109,9 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
     }
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      if constexpr (NN) {
-        load_b(kt, st, i);  // rows past the contraction lie past the descriptor
-      } else {
-        const int q = wave * LOADS + i, row = 8 * q + lr, c = (lane & 7) ^ rswz(row);
-        const int vo = k0 + 8 * c < C ? (row * ldq + k0 + 8 * c) * 2 : (int)0x7FFFFFF0;
-        llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, vo, 0, 0, 0);
-      }
+      const int q = wave * LOADS + i, row = 8 * q + lr, c = (lane & 7) ^ rswz(row);
+      const int vo = k0 + 8 * c < C ? (row * ldq + k0 + 8 * c) * 2 : (int)0x7FFFFFF0;
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, vo, 0, 0, 0);
     }
   };
   issue(0, 0);
@@ -135,23 +132,13 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     off_a[c] = (wm * WM + l15) * ROWB + 16 * (lanepart ^ (2 * c));
-    off_b[c] = NN ? A_BYTES + (8 * (lane >> 4) + (l15 >> 2)) * (TN * 2) + 256 * wn + 32 * (c ^ (l15 >> 2)) +
-                        16 * ((l15 & 3) >> 1) + 8 * (l15 & 1)
-                  : A_BYTES + (wn * 128 + l15) * ROWB + 16 * (lanepart ^ (2 * c));
+    off_b[c] = A_BYTES + (wn * 128 + l15) * ROWB + 16 * (lanepart ^ (2 * c));
   }
   auto rd_a = [&](const char* st, int s, int i) {
     return as_bf(*reinterpret_cast<const u32x4*>(st + off_a[((2 * s) ^ i) & 3] + 16 * i * ROWB));
   };
   auto rd_b = [&](const char* st, int s, int j) {
-    if constexpr (NN) {
-      typedef uint32_t u32x2t __attribute__((ext_vector_type(2)));
-      const char* p = st + off_b[j & 3] + 128 * (j >> 2) + s * 32 * (TN * 2);
-      const u32x2t a0 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-      const u32x2t a1 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * (TN * 2))));
-      return as_bf(u32x4{a0[0], a0[1], a1[0], a1[1]});
-    } else {
-      return as_bf(*reinterpret_cast<const u32x4*>(st + off_b[((2 * s) ^ j) & 3] + 16 * j * ROWB));
-    }
+    return as_bf(*reinterpret_cast<const u32x4*>(st + off_b[((2 * s) ^ j) & 3] + 16 * j * ROWB));
   };
   bf16x8 fa0[FM], fa1[FM], fb[FN];
   if (nk >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS_A + LOADS));  // the first step has landed
@@ -196,19 +183,7 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
   };
   int kt = 0, stage = 0;
   const int main_end = C / TK - 2;  // kt < main_end: step kt + 2 is whole
-  if constexpr (NN) {
-    for (; kt + 1 < main_end; kt += 2) {  // pairs: the buffers are constants at every use
-      kstep(kt, 0, true);
-      kstep(kt + 1, 1, true);
-    }
-    if (kt < main_end) {
-      kstep(kt, 0, true);
-      ++kt;
-      stage = 1;
-    }
-  } else {
-    for (; kt < main_end; ++kt, stage ^= 1) kstep(kt, stage, true);
-  }
+  for (; kt < main_end; ++kt, stage ^= 1) kstep(kt, stage, true);
   for (; kt + 1 < nk; ++kt, stage ^= 1) kstep(kt, stage, false);
   half(fa0, fa1, buf(stage), 1, false, 0, 0);
 #pragma unroll
@@ -217,6 +192,103 @@ __device__ __forceinline__ char* tile_product(const uint16_t* P, int64_t ldp, in
     for (int i = 0; i < FM; ++i)
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa1[i], acc[i][j], 0, 0, 0);
   return buf(stage ^ 1);
+}
+
+// Steps of 32 through four buffers, so that a step's loads have three steps' time to arrive: Q's rows come through
+// transposing reads, twice as many as tile_nt's, and two buffers with steps of 64 leave no room between them for the
+// loads (4096 rows, 32256 x 8192: 1.75 ms so, 1.61 in four.  tile_nt gains nothing: 1.64 ms and 1.72).
+// P's rows hold zeros from C to a multiple of 32.
+template <int FM>
+__device__ __forceinline__ void tile_nn(const uint16_t* P, int64_t ldp, int p_rows, const uint16_t* Q, int64_t ldq_,
+                                        int q_cols, int C, char* b0, char* b1, char* b2, char* b3, f32x4 (&acc)[FM][8]) {
+  constexpr int WM = 16 * FM, TM = 2 * WM, TN = 256, TK = 32, FN = 8, ROWB = 2 * TK;
+  constexpr int A_BYTES = TM * ROWB, LOADS = 4, LOADS_A = FM / 2, N = LOADS + LOADS_A;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4;
+  const int ld = (int)ldp, ldq = (int)ldq_, nk = (C + TK - 1) / TK;
+  const i32x4 ra = tile_rsrc(P, ((int64_t)(min(TM, p_rows) - 1) * ld + nk * TK) * 2);
+  const i32x4 rb = tile_rsrc(Q, ((int64_t)(C - 1) * ldq + q_cols) * 2);
+  // P's rows of 64 bytes: chunk c of row r in slot c ^ r / 4 % 4 (16 consecutive rows put a chunk in
+  // 16 different bank groups).  A load fills 16 rows.
+  const int voff_a = (lane >> 2) * ld * 2 + 16 * ((lane & 3) ^ g4);
+  int voff_b[2];
+#pragma unroll
+  for (int par = 0; par < 2; ++par)
+    voff_b[par] = ((lane >> 5) * ldq + 8 * ((lane & 31) ^ 2 * ((2 * par + (lane >> 5)) & 3))) * 2;
+  // Load e of step kt (P's first).  Past the last step the last is loaded again, for a buffer that is not read: so each
+  // step's loads are followed by the same number of others.
+  auto load = [&](int kt, char* st, int e) {
+    const int k = min(kt, nk - 1) * TK;
+    if (e < LOADS_A) {
+      const int q = wave * LOADS_A + e;
+      llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16, voff_a,
+                                        __builtin_amdgcn_readfirstlane((q * 16 * ld + k) * 2), 0, 0);
+    } else {
+      const int q = wave * LOADS + e - LOADS_A;
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16, voff_b[(e - LOADS_A) & 1],
+                                        __builtin_amdgcn_readfirstlane((k + 2 * q) * ldq * 2), 0, 0);
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < N; ++e) load(0, b0, e);
+#pragma unroll
+  for (int e = 0; e < N; ++e) load(1, b1, e);
+#pragma unroll
+  for (int e = 0; e < N; ++e) load(2, b2, e);
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      asm volatile("" : "+a"(acc[i][j]));
+    }
+  const int off_a = (wm * WM + l15) * ROWB + 16 * (g4 ^ (l15 >> 2));
+  int off_b[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    off_b[c] = A_BYTES + (8 * g4 + (l15 >> 2)) * (TN * 2) + 256 * wn + 32 * (c ^ (l15 >> 2)) + 16 * ((l15 & 3) >> 1) +
+               8 * (l15 & 1);
+  // Step kt in `st`, with the loads of step kt + 3 into `nxt`, which the step before this one has read; behind the
+  // step's own loads are those of AFTER more.
+  auto step = [&](auto with, auto after, int kt, const char* st, char* nxt) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(decltype(after)::value * N));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // not __syncthreads(), which would wait for every load
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    auto rd_b = [&](int j) {
+      typedef uint32_t u32x2t __attribute__((ext_vector_type(2)));
+      const char* p = st + off_b[j & 3] + 128 * (j >> 2);
+      const u32x2t a0 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+      const u32x2t a1 = __builtin_bit_cast(u32x2t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * (TN * 2))));
+      return as_bf(u32x4{a0[0], a0[1], a1[0], a1[1]});
+    };
+    bf16x8 fa[FM], fb[FN];
+    fb[0] = rd_b(0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fa[i] = as_bf(*reinterpret_cast<const u32x4*>(st + off_a + 16 * i * ROWB));
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      if (j + 1 < FN) fb[j + 1] = rd_b(j + 1);
+      if (decltype(with)::value && j < N) load(kt + 3, nxt, j);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  int kt = 0;
+  for (; kt + 4 <= nk; kt += 4) {
+    step(flag_c<true>{}, num_c<2>{}, kt, b0, b3);
+    step(flag_c<true>{}, num_c<2>{}, kt + 1, b1, b0);
+    step(flag_c<true>{}, num_c<2>{}, kt + 2, b2, b1);
+    step(flag_c<true>{}, num_c<2>{}, kt + 3, b3, b2);
+  }
+  if (kt < nk) step(flag_c<false>{}, num_c<2>{}, kt, b0, nullptr);
+  if (kt + 1 < nk) step(flag_c<false>{}, num_c<1>{}, kt, b1, nullptr);
+  if (kt + 2 < nk) step(flag_c<false>{}, num_c<0>{}, kt, b2, nullptr);
+  vmem_wait_all();  // nothing lands in the buffers any more
+  __syncthreads();  // the buffers are free
 }
 
 }  // namespace

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   f32x4 acc[FM][8];
   // with one row tile the head's rows come from memory once, and neighbouring tiles begin a step apart (one row
   // against 128256 of 4096: 215 us in step, 185 so; with more row tiles it changes nothing)
-  char* const idle = tile_product<false, FM>(static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
+  char* const idle = tile_nt<FM>(static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
                                              static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols,
                                              a.K,
                                              n_m == 1 ? nt : 0, smem0, smem1, acc);
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 template <bool NN, int FM>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void vocab_grad_kernel(VocabArgs a) {
   constexpr int WM = 16 * FM, TM = 2 * WM;
-  __shared__ __attribute__((aligned(1024))) char smem0[kTileStage];
-  __shared__ __attribute__((aligned(1024))) char smem1[kTileStage];
+  __shared__ __attribute__((aligned(1024))) char smem0[NN ? kTileStageNN : kTileStage];
+  __shared__ __attribute__((aligned(1024))) char smem1[NN ? kTileStageNN : kTileStage];
   const int n_m = (a.T + TM - 1) / TM, n_n = (a.K + 255) / 256, tiles = n_m * n_n;
   // ranges one after the other: those that run together read the same columns of P and W
   const int lin = tile_of(blockIdx.x, gridDim.x), part = lin / tiles;
@@ -166,8 +166,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     return;
   }
   f32x4 acc[FM][8];
-  tile_product<NN, FM>(static_cast<const uint16_t*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0, W, NN ? a.ldw : a.ldwt,
-                       a.K - n0, C, 0, smem0, smem1, acc);
+  const uint16_t* const P = static_cast<const uint16_t*>(a.P) + (int64_t)m0 * a.ldp + c0;
+  if constexpr (NN) {
+    __shared__ __attribute__((aligned(1024))) char smem2[kTileStageNN];
+    __shared__ __attribute__((aligned(1024))) char smem3[kTileStageNN];
+    tile_nn<FM>(P, a.ldp, a.T - m0, W, a.ldw, a.K - n0, C, smem0, smem1, smem2, smem3, acc);
+  } else {
+    tile_nt<FM>(P, a.ldp, a.T - m0, W, a.ldwt, a.K - n0, C, 0, smem0, smem1, acc);
+  }
   put([&](int i, int j) { return acc[i][j]; });
 }
 
