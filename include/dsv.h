@@ -578,10 +578,11 @@ int dsv_attn_train_rows(const dsv_attn_plan* plan, int64_t out[2]);
 void dsv_attn_free(dsv_attn_plan* plan);
 
 /* A tensor [rows][heads][head_dim]: element (t, h, c) at ptr[t * row + h * head + c].
- * Strides in elements, multiples of 8, at least head_dim and at most 2^40; 0 stands
- * for the dense one (row: heads * head_dim, head: head_dim).  ptr is 16-byte
- * aligned.  So q, k and v may be columns of one product's rows, and a cache may be
- * [row][head][d] or [head][row][d].  The vectors of an output must not overlap. */
+ * Strides in elements, multiples of 8 and at least head_dim, row at most 2^23, head at
+ * most 2^40; 0 stands for the dense one (row: heads * head_dim, head: head_dim).  ptr
+ * is 16-byte aligned.  So q, k and v may be columns of one product's rows, and a cache
+ * may be [row][head][d] or [head][row][d].  The vectors of an output must not overlap
+ * (DSV_ERR_SIZE), nor an output and another tensor of the call (not checked). */
 typedef struct {
   void* ptr;
   int64_t row;
@@ -595,7 +596,10 @@ int dsv_attn_workspace(const dsv_attn_plan* plan, dsv_dtype dtype, size_t* bytes
 /*
  * dsv_attn_fwd -- O, and lse [heads_q][n_q] (fp32; NULL: not written, a backward
  * needs it), of every sequence of the plan.  Q and O have n_q rows of heads_q
- * heads, K and V n_kv rows of heads_kv heads.  scale must be finite.
+ * heads, K and V n_kv rows of heads_kv heads.  scale is positive and finite in fp32.
+ * Rows and keys that no sequence holds are not read, whatever they hold.  A key that
+ * only later queries see adds 0 v to the sums of queries before it: an infinite or NaN
+ * v there can reach them, as it does in softmax(masked scores) V.
  * Errors: DSV_ERR_ARG (null or misaligned pointer, plan not on the device),
  * DSV_ERR_RANGE (dtype, scale), DSV_ERR_SIZE (strides, overlapping outputs,
  * workspace).
