@@ -17,6 +17,7 @@ struct AttnArgs {
   const int32_t* seqs;   // sequence descriptors (attn_plan.h)
   const int32_t* items;  // the launch's work items
   int32_t n_items;       // fp32 launches
+  int32_t parts;         // fp32 dK and dV: ranges of a key head's query heads
   int32_t hq, hkv, group, d;
   int32_t n_q;           // row length of lse ([hq][n_q])
   int64_t train_q;       // row length of delta ([hq][train_q])
@@ -27,7 +28,7 @@ struct AttnArgs {
   float* lse2;           // bf16: lse of the compact rows, base 2
   // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
   // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
-  // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].
+  // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].  fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
   float* part_o;
   float* part_ml;
 };

@@ -880,6 +880,13 @@ struct Workspace {
   size_t total;
 };
 
+// fp32 key tiles of short batches are fewer than the CUs: the query heads of a key head are then divided among so many
+// workgroups.
+int f32_parts(const dsv_attn_plan& p) {
+  const int64_t tiles = std::max<int64_t>(1, (int64_t)p.n_f32_dk * p.hkv);
+  return (int)std::min<int64_t>(p.hq / p.hkv, (kAttnDkSlots + tiles - 1) / tiles);
+}
+
 Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   Workspace w{};
   size_t at = 0;
@@ -899,7 +906,10 @@ Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   at = 0;
   w.delta = room((size_t)p.train_q * p.hq);
   w.lse2 = room(bf ? (size_t)p.train_q * p.hq : 0);
-  w.dk = room(bf ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d : 0);
+  const int parts = f32_parts(p);
+  w.dk = room(bf          ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d
+              : parts > 1 ? (size_t)p.n_f32_dk * p.hkv * parts * 2 * kAttnF32Rows * p.d
+                          : 0);
   w.total = std::max<size_t>(256, std::max(at, fwd));
   return w;
 }
@@ -1038,6 +1048,7 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
     if (e != hipSuccess) return status(e);
     a.items = p->dptr(p->lay.f32_dk_items);
     a.n_items = p->n_f32_dk;
+    a.parts = f32_parts(*p);
     return status(launch_attn_f32_dk(a, s));
   }
   a.items = p->dptr(p->lay.dq_items);

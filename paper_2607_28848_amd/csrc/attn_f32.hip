@@ -8,9 +8,11 @@
 //
 // A workgroup has 16 queries (or keys) of one head, and its waves take 16 keys (queries) each by turns, straight
 // from global memory (the rows that several workgroups read come from L2), and add their sums at the end: the
-// batches of this mode are small, and what bounds them is the number of tiles that one wave walks one after the other.
-// Two samples of 96 and three of 157 rows, 8 heads on 2 of 64, both directions: 44 us (four waves on 64 rows
-// with staged tiles: 135).
+// batches of this mode are small, and what bounds them is the number of tiles that one wave walks one after the other,
+// each with its loads' time in front.  Rows are read through descriptors, whose lanes need no pointers and no
+// predicates of their own (with pointers the dK kernel of heads of 128 kept 215 registers in memory: 157 us against 58).
+// Two samples of 96 and three of 157 rows, 8 heads on 2 of 64: forward 7.8 us, dQ 8.4, dK and dV 10.6, their join 3.6
+// (four waves on 64 rows with staged tiles: 135 in all).  Two of 200 and three of 300, 16 on 2 of 128: 40, 47, 58, 5.
 #include <hip/hip_runtime.h>
 
 #include "attn.h"
@@ -39,13 +41,24 @@ struct Seq {
   }
 };
 
-// A lane's D / 4 values of a row (zeros where the row does not exist).
+// Descriptor over `n` rows (none if n <= 0) of head h from `row` on: what lies past them reads zeros.
 template <int D>
-__device__ __forceinline__ void load_quarter(const AttnView& t, int64_t row, int h, bool in, float (&x)[D / 4]) {
-  const float* p = static_cast<const float*>(t.ptr) + row * t.row + h * t.head + (threadIdx.x >> 4 & 3) * (D / 4);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const AttnView& t, int64_t row, int h, int n) {
+  const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const float*>(t.ptr) + row * t.row + h * t.head);
+  const int64_t bytes = n > 0 ? ((int64_t)(min(n, 16) - 1) * t.row + D) * 4 : 0;
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p),
+                 hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0,
+                                           __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+
+// A lane's D / 4 values of row l % 16.
+template <int D>
+__device__ __forceinline__ void load_quarter(__amdgpu_buffer_rsrc_t t, int64_t stride, float (&x)[D / 4]) {
+  const int at = (int)(threadIdx.x & 15) * (int)stride * 4 + (threadIdx.x >> 4 & 3) * D;
 #pragma unroll
   for (int c = 0; c < D / 4; c += 4) {
-    const f32x4 v = in ? *reinterpret_cast<const f32x4*>(p + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(t, at + 4 * c, 0, 0));
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[c + e] = v[e];
   }
@@ -60,17 +73,15 @@ __device__ __forceinline__ f32x4 dot_tile(const float (&a)[D / 4], const float (
   return c;
 }
 
-// Values [16 t + l % 16] of rows r0 + 4 (l / 16) + v, rows from r_end on as zeros.
+// Values [16 i + l % 16] of rows 4 (l / 16) + v.
 template <int D>
-__device__ __forceinline__ void load_columns(const AttnView& t, int64_t base, int r0, int r_end, int h,
-                                             float (&x)[4][D / 16]) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void load_columns(__amdgpu_buffer_rsrc_t t, int64_t stride, float (&x)[4][D / 16]) {
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    const int r = r0 + 4 * (lane >> 4) + v;
-    const float* p = static_cast<const float*>(t.ptr) + (base + r) * t.row + h * t.head + (lane & 15);
+    const int at = (int)(4 * (threadIdx.x >> 4 & 3) + v) * (int)stride * 4 + (threadIdx.x & 15) * 4;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) x[v][i] = r < r_end ? p[16 * i] : 0.f;
+    for (int i = 0; i < D / 16; ++i)
+      x[v][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(t, at + 64 * i, 0, 0));
   }
 }
 
@@ -116,18 +127,18 @@ __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
   const int item = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
   const Seq s(a, a.items[2 * item]);
   const int qt = a.items[2 * item + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
-  const int q = qt + l15, off = s.kl - s.ql;  // the lane's query
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
+  const int hk = h / a.group, q = qt + l15, off = s.kl - s.ql;  // the lane's query
   float qv[D / 4];
-  load_quarter<D>(a.Q, (int64_t)s.q0 + q, h, q < s.ql, qv);
+  load_quarter<D>(rows_of<D>(a.Q, (int64_t)s.q0 + qt, h, s.ql - qt), a.Q.row, qv);
   f32x4 acc[D / 16];
   clear<D>(acc);
   float m = -INFINITY, l = 0.f;
   const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
   for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
     float kv[D / 4], vv[4][D / 16];
-    load_quarter<D>(a.K, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, kv);
-    load_columns<D>(a.V, s.k0, kt, s.kl, h / a.group, vv);
+    load_quarter<D>(rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, s.kl - kt), a.K.row, kv);
+    load_columns<D>(rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, s.kl - kt), a.V.row, vv);
     f32x4 x = dot_tile<D>(kv, qv);
     float mx = m;
 #pragma unroll
@@ -157,7 +168,8 @@ __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
 #pragma unroll
   for (int w = 0; w < NW; ++w) ref = fmaxf(ref, ml[0][w][l15]);
 #pragma unroll
-  for (int w = 0; w < NW; ++w) total += ml[0][w][l15] == -INFINITY ? ml[1][w][l15] : ml[1][w][l15] * expf(ml[0][w][l15] - ref);
+  for (int w = 0; w < NW; ++w)
+    total += ml[0][w][l15] == -INFINITY ? ml[1][w][l15] : ml[1][w][l15] * expf(ml[0][w][l15] - ref);
   spread<D>(acc, (m == -INFINITY ? 1.f : expf(m - ref)) * (total == 0.f ? 0.f : 1.f / total), red);
   if (a.lse && wave == 0 && lane < 16 && q < s.ql)
     a.lse[(int64_t)h * a.n_q + s.q0 + q] = total == 0.f ? -INFINITY : ref + logf(total);
@@ -178,15 +190,15 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   const int item = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
   const Seq s(a, a.items[2 * item]);
   const int qt = a.items[2 * item + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
-  const int q = qt + l15, off = s.kl - s.ql;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
+  const int hk = h / a.group, q = qt + l15, off = s.kl - s.ql;
   const bool in = q < s.ql;
   float qv[D / 4], dv[D / 4], dot = 0.f;
-  load_quarter<D>(a.Q, (int64_t)s.q0 + q, h, in, qv);
-  load_quarter<D>(a.dO, (int64_t)s.cq + q, h, in, dv);
+  load_quarter<D>(rows_of<D>(a.Q, (int64_t)s.q0 + qt, h, s.ql - qt), a.Q.row, qv);
+  load_quarter<D>(rows_of<D>(a.dO, (int64_t)s.cq + qt, h, s.ql - qt), a.dO.row, dv);
   {
     float ov[D / 4];
-    load_quarter<D>(a.O, (int64_t)s.q0 + q, h, in, ov);
+    load_quarter<D>(rows_of<D>(a.O, (int64_t)s.q0 + qt, h, s.ql - qt), a.O.row, ov);
 #pragma unroll
     for (int c = 0; c < D / 4; ++c) dot += dv[c] * ov[c];
   }
@@ -198,9 +210,11 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
   for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
     float kv[D / 4], vv[D / 4], kc[4][D / 16];
-    load_quarter<D>(a.K, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, kv);
-    load_quarter<D>(a.V, (int64_t)s.k0 + kt + l15, h / a.group, kt + l15 < s.kl, vv);
-    load_columns<D>(a.K, s.k0, kt, s.kl, h / a.group, kc);
+    const auto kr = rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, s.kl - kt);
+    const auto vr = rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, s.kl - kt);
+    load_quarter<D>(kr, a.K.row, kv);
+    load_quarter<D>(vr, a.V.row, vv);
+    load_columns<D>(kr, a.K.row, kc);
     const f32x4 x = dot_tile<D>(kv, qv), dp = dot_tile<D>(vv, dv);
     f32x4 ds;
 #pragma unroll
@@ -221,38 +235,44 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
 }
 
 // dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
-// heads (so the sums over them need no atomics).
+// heads (so the sums over them need no atomics), or of one of a.parts ranges of them, whose sums go to the workspace
+// (32 us whole, 10.6 and 3.6 for the join in four parts: the first batch above).
 template <int D>
 __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
   constexpr int NW = 8;
   __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
-  const int item = blockIdx.x / a.hkv, g = blockIdx.x % a.hkv;
+  const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts, item = tile / a.hkv, g = tile % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
   const int k = k0 + l15, off = s.kl - s.ql;  // the lane's key
   float kv[D / 4], vv[D / 4];
-  load_quarter<D>(a.K, (int64_t)s.k0 + k, g, k < s.kl, kv);
-  load_quarter<D>(a.V, (int64_t)s.k0 + k, g, k < s.kl, vv);
+  load_quarter<D>(rows_of<D>(a.K, (int64_t)s.k0 + k0, g, s.kl - k0), a.K.row, kv);
+  load_quarter<D>(rows_of<D>(a.V, (int64_t)s.k0 + k0, g, s.kl - k0), a.V.row, vv);
   f32x4 dk[D / 16], dv[D / 16];
   clear<D>(dk);
   clear<D>(dv);
   const int q_first = max(0, k0 - off);
   const int per_head = q_first < s.ql ? (s.ql - q_first + 15) / 16 : 0;
-  for (int n = wave; n < per_head * a.group; n += NW) {
-    const int h = g * a.group + n / per_head, qt = q_first + n % per_head * 16;
+  const int h0 = part * a.group / a.parts, h1 = (part + 1) * a.group / a.parts;
+  for (int n = wave; n < per_head * (h1 - h0); n += NW) {
+    const int h = g * a.group + h0 + n / per_head, qt = q_first + n % per_head * 16;
     float qv[D / 4], ov[D / 4], qc[4][D / 16], oc[4][D / 16], lse[4], delta[4];
-    load_quarter<D>(a.Q, (int64_t)s.q0 + qt + l15, h, qt + l15 < s.ql, qv);
-    load_quarter<D>(a.dO, (int64_t)s.cq + qt + l15, h, qt + l15 < s.ql, ov);
-    load_columns<D>(a.Q, s.q0, qt, s.ql, h, qc);
-    load_columns<D>(a.dO, s.cq, qt, s.ql, h, oc);
+    const auto qr = rows_of<D>(a.Q, (int64_t)s.q0 + qt, h, s.ql - qt);
+    const auto dr = rows_of<D>(a.dO, (int64_t)s.cq + qt, h, s.ql - qt);
+    load_quarter<D>(qr, a.Q.row, qv);
+    load_quarter<D>(dr, a.dO.row, ov);
+    load_columns<D>(dr, a.dO.row, oc);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int q = min(qt + 4 * (lane >> 4) + v, s.ql - 1);
       lse[v] = a.lse[(int64_t)h * a.n_q + s.q0 + q];
       delta[v] = a.delta[h * a.train_q + s.cq + q];
     }
-    const f32x4 x = dot_tile<D>(qv, kv), dp = dot_tile<D>(ov, vv);
+    const f32x4 x = dot_tile<D>(qv, kv);
+    __builtin_amdgcn_sched_barrier(0);  // Q's columns take the registers of its rows (with heads of 128 both do not fit)
+    load_columns<D>(qr, a.Q.row, qc);
+    const f32x4 dp = dot_tile<D>(ov, vv);
     f32x4 p, ds;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
@@ -264,19 +284,38 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
     add_rows<D>(oc, p, dv);
     add_rows<D>(qc, ds, dk);
   }
-  auto put = [&](const f32x4 (&acc)[D / 16], const AttnView& t) {
+  auto put = [&](const f32x4 (&acc)[D / 16], const AttnView& t, int half) {
     __syncthreads();
     spread<D>(acc, 1.f, red);
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
       const int r = i / (D / 4), c = 4 * (i % (D / 4));
-      if (k0 + r < s.kl)
-        *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) =
-            gather<D, NW>(red, r, c);
+      const f32x4 x = gather<D, NW>(red, r, c);
+      if (a.parts > 1)
+        *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)blockIdx.x * 2 + half) * 16 + r) * D + c) = x;
+      else if (k0 + r < s.kl)
+        *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) = x;
     }
   };
-  put(dk, a.dK);
-  put(dv, a.dV);
+  put(dk, a.dK, 0);
+  put(dv, a.dV, 1);
+}
+
+// dK and dV of 16 keys from the parts' sums, in order: one workgroup a tile and gradient.
+template <int D>
+__global__ __launch_bounds__(256) void attn_f32_dk_join_kernel(AttnArgs a) {
+  const int half = blockIdx.x & 1, tile = blockIdx.x >> 1, item = tile / a.hkv, g = tile % a.hkv;
+  const Seq s(a, a.items[2 * item]);
+  const int k0 = a.items[2 * item + 1];
+  const AttnView& t = half ? a.dV : a.dK;
+  for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    if (k0 + r >= s.kl) break;
+    const float* p = a.part_o + (((int64_t)tile * a.parts * 2 + half) * 16 + r) * D + c;
+    f32x4 x = *reinterpret_cast<const f32x4*>(p);
+    for (int n = 1; n < a.parts; ++n) x += *reinterpret_cast<const f32x4*>(p + (int64_t)n * 32 * D);
+    *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) = x;
+  }
 }
 
 }  // namespace
@@ -299,9 +338,14 @@ hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s) {
 
 hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
-  const dim3 grid((unsigned)(a.n_items * (int64_t)a.hkv));
+  const int64_t tiles = a.n_items * (int64_t)a.hkv;
+  const dim3 grid((unsigned)(tiles * a.parts));
   if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_kernel<64>, grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL(attn_f32_dk_kernel<128>, grid, dim3(512), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_join_kernel<64>, dim3((unsigned)(2 * tiles)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(attn_f32_dk_join_kernel<128>, dim3((unsigned)(2 * tiles)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
