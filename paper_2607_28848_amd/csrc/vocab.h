@@ -29,7 +29,7 @@ struct VocabArgs {
   int64_t ld_stats;
   float* ref;             // [T] the row's reference
   float* others;          // [T] sum of the terms that are not the target's, at the reference
-  float* zt;              // [T] the target's logit
+  float* term;            // [T] the target's term at the reference (after the last piece)
   float* alpha;           // [T] what the sums so far are multiplied by (the reference moved)
   // second product: contraction in `split` ranges of split_len columns, each with its own sums
   float* O;               // [split][T][K]

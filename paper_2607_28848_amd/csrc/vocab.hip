@@ -93,10 +93,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         for (int v = 0; v < 4; ++v) {
           const float z = acc[i][j][v];
           e[v] = __builtin_amdgcn_exp2f(z * kLog2e - base);
-          if (tc == 16 * j + v) {
-            a.zt[row] = z;
-            e[v] = 0.f;
-          }
+          if (tc == 16 * j + v) e[v] = 0.f;
           if (cols < 256 && c0 + 16 * j + v >= cols) e[v] = 0.f;
           sum += e[v];
         }
@@ -203,20 +200,57 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
   return x;
 }
 
-// Row loss from the sums at a reference (base 2): others, and the target's logit.  In 64 bits: the logarithm and
-// the target's logit nearly cancel for a sure row, and there is one per row.
-__device__ __forceinline__ float row_loss(float ref, float others, float zt) {
-  const float et = exp2f(zt * kLog2e - ref);
-  if (et >= others) return log1pf(others / et);  // near 0 the loss keeps its relative accuracy
-  return (float)(log((double)others + et) + ref * 0.69314718055994531 - zt);
+template <int N>
+__device__ __forceinline__ double block_sum(double x, double* red) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = red[0];
+#pragma unroll
+  for (int w = 1; w < N; ++w) x += red[w];
+  return x;
+}
+
+// Eight values from p on.
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+  }
 }
 
 // One row: the piece's sums into the row's, at the larger of the references; the terms of tiles at another
-// reference are brought to the row's.
+// reference are brought to the row's.  After the last piece the target's logit, its term and the loss, in 64 bits: the
+// logarithm and the logit nearly cancel for a sure row, and there is one of each per row (one row against 128256 of
+// 4096: the loss is off by 8e-7 in the root mean square with the logit from the products, whose sums are fp32).
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   __shared__ float red[4];
+  __shared__ double red64[4];
   const int row = blockIdx.x;
+  const int target = a.last ? a.target[row] : -1;
+  const bool has = target >= 0 && target < a.V;
+  double zt = 0.;
+  if (has) {
+    const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+    const T* w = static_cast<const T*>(a.W) + target * a.ldw;
+    for (int c = 8 * threadIdx.x; c < a.K; c += 8 * 256) {
+      float xs[8], ws[8];
+      load8(x + c, xs);
+      load8(w + c, ws);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) zt += (double)xs[e] * ws[e];
+    }
+    zt = block_sum<4>(zt, red64);
+  }
   const float2* st = a.stats + (int64_t)row * a.ld_stats;
   const float have = a.first ? -INFINITY : a.ref[row];
   float m = have;
@@ -232,12 +266,18 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   sum = block_sum<4>(sum, red);
   if (threadIdx.x == 0) {
     const float f = have == -INFINITY ? 0.f : exp2f(have - ref);
-    a.others[row] = (a.first ? 0.f : a.others[row] * f) + sum;
+    const float others = (a.first ? 0.f : a.others[row] * f) + sum;
+    a.others[row] = others;
     a.ref[row] = ref;
-    if (a.alpha) a.alpha[row] = f;
-    if (a.last && a.loss) {
-      const int t = a.target[row];
-      a.loss[row] = t >= 0 && t < a.V ? row_loss(ref, a.others[row], a.zt[row]) : 0.f;
+    a.alpha[row] = f;
+    if (a.last) {
+      const double et = has ? exp2(zt * 1.4426950408889634 - ref) : 1.;
+      a.term[row] = (float)et;
+      // near 0 the loss keeps its relative accuracy
+      if (a.loss)
+        a.loss[row] = !has           ? 0.f
+                      : et >= others ? (float)log1p(others / et)
+                                     : (float)(log(others + et) + ref * 0.69314718055994531 - zt);
     }
   }
   if (!a.grad || !__syncthreads_or(moved)) return;
@@ -276,8 +316,7 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(VocabArgs a) {
   T* dx = static_cast<T*>(a.dX) + (int64_t)row * a.lddx;
   const bool has = t >= 0 && t < a.V;
   const T* w = static_cast<const T*>(a.W) + (int64_t)(has ? t : 0) * a.ldw;
-  const float others = a.others[row], et = has ? exp2f(a.zt[row] * kLog2e - a.ref[row]) : 1.f;
-  const float f = (a.weight ? a.weight[row] : 1.f) / (others + et);
+  const float others = a.others[row], f = (a.weight ? a.weight[row] : 1.f) / (others + a.term[row]);
   // 1024 columns a workgroup
   const int c = 1024 * blockIdx.y + 4 * threadIdx.x;
   if (c < a.K) {
@@ -413,8 +452,8 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   a.ld_stats = pc.width / pc.tw;
   a.ref = reinterpret_cast<float*>(b + pc.rows);
   a.others = a.ref + a.T;
-  a.zt = a.others + a.T;
-  a.alpha = a.zt + a.T;
+  a.term = a.others + a.T;
+  a.alpha = a.term + a.T;
   a.O = reinterpret_cast<float*>(b + pc.o);
   a.tw = pc.tw;
   a.split_len = pc.split_len;

@@ -127,10 +127,7 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
       for (int v = 0; v < 4; ++v) {
         const float z = acc[i][j][v];
         float e = exp2f(z * kLog2e - base);
-        if (t == 16 * j + v) {
-          a.zt[row] = z;
-          e = 0.f;
-        }
+        if (t == 16 * j + v) e = 0.f;
         sum += e;
         acc[i][j][v] = e;
       }
