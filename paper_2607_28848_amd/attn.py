@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import numpy as np
 
@@ -44,6 +45,14 @@ _lib.dsv_attn_fwd.argtypes = [_vp, ctypes.c_int, ctypes.c_double] + [_viewp] * 4
 _lib.dsv_attn_fwd.restype = ctypes.c_int
 _lib.dsv_attn_bwd.argtypes = [_vp, ctypes.c_int, ctypes.c_double] + [_viewp] * 4 + [_vp] + [_viewp] * 4 + [_vp, _sz, _vp]
 _lib.dsv_attn_bwd.restype = ctypes.c_int
+
+# The calls below pass their views as packed bytes, read during the call only: a decode step's attention takes the GPU
+# 10 us, and marshalling structures takes the host as long.
+_VIEW_PACK = struct.Struct("@Pqq").pack
+assert len(_VIEW_PACK(0, 0, 0)) == ctypes.sizeof(View)
+_head = (ctypes.c_int, _vp, ctypes.c_int, ctypes.c_double)
+_fwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 6, _sz, _vp)(("dsv_attn_fwd", _lib))
+_bwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 10, _sz, _vp)(("dsv_attn_bwd", _lib))
 
 
 class Plan:
@@ -93,21 +102,22 @@ def workspace_bytes(plan: Plan, dtype) -> int:
     return int(n.value)
 
 
-def _view(t, rows: int, heads: int, d: int, dtype, name: str):
-    if t.dtype != dtype:
+def _view(t, rows: int, heads: int, d: int, dtype, name: str) -> bytes:
+    if t.dtype is not dtype:
         raise TypeError("%s is %s, the call's tensors are %s" % (name, t.dtype, dtype))
-    if t.dim() == 2 and t.shape[1] == heads * d:
+    if t.shape != (rows, heads, d):
+        if t.shape != (rows, heads * d):
+            raise ValueError("%s must be [%d][%d][%d], got %s" % (name, rows, heads, d, tuple(t.shape)))
         t = t.unflatten(1, (heads, d))
-    if tuple(t.shape) != (rows, heads, d):
-        raise ValueError("%s must be [%d][%d][%d], got %s" % (name, rows, heads, d, tuple(t.shape)))
-    if t.numel() and t.stride(2) != 1:
+    row, head, one = t.stride()
+    if one != 1 and rows:
         raise ValueError("%s: the elements of a head must be contiguous" % name)
     # a stride of a dimension of one is arbitrary: the dense one then
-    return View(t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 and rows > 0 else 0)
+    return _VIEW_PACK(t.data_ptr(), row if rows > 1 else 0, head if heads > 1 and rows > 0 else 0)
 
 
 def _dense(t, shape, name: str):
-    if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != shape:
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape:
         raise ValueError("%s must be a contiguous fp32 tensor of shape %s" % (name, shape))
     return t.data_ptr()
 
@@ -127,12 +137,12 @@ def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse: bool = True
         O = torch.zeros((plan.n_q, hq, d), dtype=Q.dtype, device=Q.device)
     if lse is None and want_lse and made:
         lse = torch.full((hq, plan.n_q), -math.inf, dtype=torch.float32, device=Q.device)
-    ws = _ws(workspace, plan, Q)
-    v = [_view(t, n, h, d, Q.dtype, name) for t, n, h, name in ((Q, plan.n_q, hq, "Q"), (K, plan.n_kv, hkv, "K"),
-                                                               (V, plan.n_kv, hkv, "V"), (O, plan.n_q, hq, "O"))]
-    _check(_lib.dsv_attn_fwd(plan.handle, _code(Q.dtype), 1 / math.sqrt(d) if scale is None else scale, *v,
-                             None if lse is None else _dense(lse, (hq, plan.n_q), "lse"), _ptr(ws),
-                             ws.numel() * ws.element_size(), _stream_handle(stream)), "dsv_attn_fwd")
+    ws, dt = _ws(workspace, plan, Q), Q.dtype
+    _check(_fwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
+                _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
+                _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),
+                None if lse is None else _dense(lse, (hq, plan.n_q), "lse"), ws.data_ptr(), ws.nbytes,
+                _stream_handle(stream)), "dsv_attn_fwd")
     return O, lse
 
 
@@ -141,11 +151,11 @@ def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, 
     hq, hkv, d, nq, nk = plan.heads_q, plan.heads_kv, plan.head_dim, plan.train_q, plan.train_k
     dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)
                   for t, n, h in ((dQ, nq, hq), (dK, nk, hkv), (dV, nk, hkv)))
-    ws = _ws(workspace, plan, Q)
-    v = [_view(t, n, h, d, Q.dtype, name) for t, n, h, name in (
-        (Q, plan.n_q, hq, "Q"), (K, plan.n_kv, hkv, "K"), (V, plan.n_kv, hkv, "V"), (O, plan.n_q, hq, "O"),
-        (dO, nq, hq, "dO"), (dQ, nq, hq, "dQ"), (dK, nk, hkv, "dK"), (dV, nk, hkv, "dV"))]
-    _check(_lib.dsv_attn_bwd(plan.handle, _code(Q.dtype), 1 / math.sqrt(d) if scale is None else scale, *v[:4],
-                             _dense(lse, (hq, plan.n_q), "lse"), *v[4:], _ptr(ws), ws.numel() * ws.element_size(),
-                             _stream_handle(stream)), "dsv_attn_bwd")
+    ws, dt = _ws(workspace, plan, Q), Q.dtype
+    _check(_bwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
+                _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
+                _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),
+                _dense(lse, (hq, plan.n_q), "lse"), _view(dO, nq, hq, d, dt, "dO"), _view(dQ, nq, hq, d, dt, "dQ"),
+                _view(dK, nk, hkv, d, dt, "dK"), _view(dV, nk, hkv, d, dt, "dV"), ws.data_ptr(), ws.nbytes,
+                _stream_handle(stream)), "dsv_attn_bwd")
     return dQ, dK, dV
