@@ -31,6 +31,11 @@ struct AttnArgs {
   // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].  fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
   float* part_o;
   float* part_ml;
+  // The join of both forms: the forward tiles' own, its items and workgroups.
+  const float* fwd_o;
+  const float* fwd_ml;
+  const int32_t* fwd_join;
+  int32_t fwd_join_groups;
 };
 
 // fp32 mode: tiles of kAttnF32Rows.

@@ -480,19 +480,21 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
 
 // Pieces of a row added in order: columns c0 .. c0 + D / 8 of row `row` of `rows`, slots first, first + step, ..
 template <int D>
-__device__ __forceinline__ void join_row(const AttnArgs& a, int64_t first, int64_t step, int n, int rows, int row, int c0,
-                                         int64_t out_row, int h) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o, const float* part_ml, int64_t first, int64_t step,
+                                         int n, int rows, int row, int c0, int64_t out_row, int h) {
   float ref = -INFINITY, total = 0.f;
-  for (int k = 0; k < n; ++k) ref = fmaxf(ref, a.part_ml[(first + k * step) * 2 * rows + row]);
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) ref = fmaxf(ref, part_ml[(first + k * step) * 2 * rows + row]);
   f32x4 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int k = 0; k < n; ++k) {
     const int64_t slot = first + k * step;
-    const float m = a.part_ml[slot * 2 * rows + row];
+    const float m = part_ml[slot * 2 * rows + row];
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-    total += f * a.part_ml[(slot * 2 + 1) * rows + row];
-    const float* p = a.part_o + (slot * rows + row) * D + c0;
+    total += f * part_ml[(slot * 2 + 1) * rows + row];
+    const float* p = part_o + (slot * rows + row) * D + c0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + 4 * i) * f;
   }
@@ -504,29 +506,26 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int64_t first, int64
   if (a.lse && c0 == 0) a.lse[(int64_t)h * a.n_q + out_row] = lse_of(ref, total);
 }
 
-// Tiles of the split form: row tid / 8, D / 8 columns each.
+// Both forms' pieces in one launch: 32 rows a workgroup, row tid / 8, D / 8 columns each; forward tiles first.
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  const int item = blockIdx.x / a.hkv, hk = blockIdx.x % a.hkv;
+  const int at = blockIdx.x, row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8);
+  if (at < a.fwd_join_groups) {
+    constexpr int BL = kAttnFwdRows / 32;
+    const int item = at / (BL * a.hq), h = at / BL % a.hq;
+    const int32_t* it = a.fwd_join + 4 * (int64_t)item;
+    const Seq s(a, it[0]);
+    const int r = 32 * (at % BL) + row, q = it[1] + r;
+    if (q >= s.ql) return;
+    join_row<D>(a, a.fwd_o, a.fwd_ml, (int64_t)it[2] * a.hq + h, a.hq, it[3], kAttnFwdRows, r, c0, (int64_t)s.q0 + q, h);
+    return;
+  }
+  const int item = (at - a.fwd_join_groups) / a.hkv, hk = (at - a.fwd_join_groups) % a.hkv;
   const int32_t* it = a.items + kAttnSplitWords * (int64_t)item;
-  if (it[5] == 1) return;  // written by its only piece
-  const int row = threadIdx.x >> 3, r = it[4] + row;
-  if (r >= it[1] * a.group) return;
-  join_row<D>(a, (int64_t)it[6] * a.hkv + hk, a.hkv, it[5], kAttnPackRows, row, (threadIdx.x & 7) * (D / 8),
+  const int r = it[4] + row;
+  if (it[5] == 1 || r >= it[1] * a.group) return;  // one piece: written by it
+  join_row<D>(a, a.part_o, a.part_ml, (int64_t)it[6] * a.hkv + hk, a.hkv, it[5], kAttnPackRows, row, c0,
               (int64_t)it[0] + r / a.group, hk * a.group + r % a.group);
-}
-
-// Forward tiles: 32 rows a workgroup.
-template <int D>
-__global__ __launch_bounds__(256) void attn_fwd_join_kernel(AttnArgs a) {
-  constexpr int BL = kAttnFwdRows / 32;
-  const int item = blockIdx.x / (BL * a.hq), h = blockIdx.x / BL % a.hq;
-  const int32_t* it = a.items + 4 * (int64_t)item;
-  const Seq s(a, it[0]);
-  const int row = 32 * (blockIdx.x % BL) + (threadIdx.x >> 3), q = it[1] + row;
-  if (q >= s.ql) return;
-  join_row<D>(a, (int64_t)it[2] * a.hq + h, a.hq, it[3], kAttnFwdRows, row, (threadIdx.x & 7) * (D / 8), (int64_t)s.q0 + q,
-              h);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -1000,20 +999,20 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   }
   const int64_t hq = p->hq, hkv = p->hkv;
   a.items = p->dptr(p->lay.fwd_items);
-  a.part_o = at<float>(ws, w.fwd_o);
-  a.part_ml = at<float>(ws, w.fwd_ml);
+  a.fwd_o = a.part_o = at<float>(ws, w.fwd_o);
+  a.fwd_ml = a.part_ml = at<float>(ws, w.fwd_ml);
   hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, p->n_fwd * hq, s);
-  if (e != hipSuccess) return status(e);
-  a.items = p->dptr(p->lay.fwd_join);
-  e = launch(attn_fwd_join_kernel<64>, attn_fwd_join_kernel<128>, a, p->n_fwd_join * hq * (kAttnFwdRows / 32), s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.split_items);
   a.part_o = at<float>(ws, w.split_o);
   a.part_ml = at<float>(ws, w.split_ml);
   e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, p->n_split * hkv, s);
-  if (e != hipSuccess || p->n_split == p->n_join) return status(e);  // one piece each: nothing to join
+  if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.join_items);
-  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, p->n_join * hkv, s));
+  a.fwd_join = p->dptr(p->lay.fwd_join);
+  a.fwd_join_groups = (int32_t)(p->n_fwd_join * hq * (kAttnFwdRows / 32));
+  const int64_t split = p->n_split == p->n_join ? 0 : p->n_join * hkv;  // one piece each: nothing to join
+  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, a.fwd_join_groups + split, s));
 }
 
 extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, const dsv_attn_view* Q,

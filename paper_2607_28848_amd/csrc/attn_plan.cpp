@@ -247,7 +247,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   most = std::max(most, count(wq, 2, &p.n_dq));
   most = std::max(most, count(w3q, 2, &p.n_f32_dq));
   most = std::max(most, count(w3k, 2, &p.n_f32_dk));
-  if (4 * most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
+  if (8 * most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
   L.seqs = put(desc);
   L.fwd_items = put(cf.items);
   L.fwd_join = put(cf.join);
