@@ -3,8 +3,8 @@
     python -m paper_2607_28848_amd.build              # the library
     python -m paper_2607_28848_amd.build --host-asan  # + host-sanitized variant
 
-The host-sanitized variant compiles the host code (plan.cpp, api.cpp: segment
-table validation, plan packing, argument checks) with g++ and
+The host-sanitized variant compiles the host code (plan.cpp, attn_plan.cpp, api.cpp:
+segment table and sequence validation, plan packing, argument checks) with g++ and
 AddressSanitizer + UndefinedBehaviorSanitizer, and the device code exactly as
 the library does.  It lands in _build/host_asan/libdsv.so; the binding loads it
 when DSV_LIBRARY names it, in a process started with gcc's libasan loaded

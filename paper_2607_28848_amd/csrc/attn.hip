@@ -250,6 +250,13 @@ __device__ __forceinline__ void store_cols(const AttnView& t, int64_t row, int h
 }
 
 // ---------------------------------------------------------------------------------------------------
+// O and lse of 128 queries of one head (or the sums of a piece of their keys): 32 queries a wave, 64 keys a step.
+//
+// A wave's products read a fragment of K or V from LDS for each matrix instruction, 1 KiB in the 32 cycles that one
+// takes: all of a CU's LDS bandwidth with four waves at it, so two workgroups share a CU and one's softmax runs beside
+// the other's products.  With heads of 64 the exponentials (one for 256 operations, a quarter of the vector rate) take
+// as long as the products.  16384 queries, 32 heads of 128 on 8: 1.95 ms (1130 TFLOP/s; a large bf16 product reaches
+// 1290 on the same card).  Nine prompts of about 700, 24 heads of 64 on 4: 36 us (560 TFLOP/s).
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -351,7 +358,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 // ---------------------------------------------------------------------------------------------------
 // One piece of the keys of a sequence for 32 (query, head) pairs of a key head, row r being query
 // r / group and head r % group.  Each wave takes every fourth block of 32 keys through buffers of its
-// own (no barrier until the end), then the four waves' sums are added.
+// own (no barrier until the end), then the four waves' sums are added.  Every key is read once for all of
+// its head's queries: the stream of K and V is what bounds it where there are many keys (64 sequences of about 2600,
+// 8 heads of 128: 577 MB in 104 us, 5.5 TB/s), and the loads' latency one after the other where there are few (8 of
+// about 400: 10 us for 12 MB).
 template <int D>
 __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   constexpr int TK = 32, TILE = TK * 2 * D, LDO = D + 4;
@@ -507,6 +517,8 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
 }
 
 // Both forms' pieces in one launch: 32 rows a workgroup, row tid / 8, D / 8 columns each; forward tiles first.
+// The launch and two reads one after the other: 4.8 us for 512 tiles of the split form, 7.9 for 48 sequences' beside
+// 96 forward tiles in five pieces (two launches: 12.2).
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int at = blockIdx.x, row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8);
@@ -529,6 +541,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------
+// dQ of 128 queries of one head over the keys they see, 32 queries a wave, 64 keys a step, in three products: the scores
+// again (p = 2^(c s - lse) needs no maximum), dO V^T, and ds K.  It also leaves delta = do . o and the base-2 lse of its
+// rows for attn_dk, which runs after it.  Bound as attn_fwd is (three fragments of LDS for three matrix instructions),
+// matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.47 ms (412 GFLOP, 880 TFLOP/s).
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -642,6 +658,11 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // the other through LDS, lane to lane, a step late: in step n the second wave multiplies dO(n) with V and
 // closes ds(n - 1), for which Q is kept for one step more.  It travels in 16 bits with 9 of mantissa
 // (pack_p): in bf16 the second rounding of ds would show, dK being off by 0.31% instead of 0.25%.
+//
+// Four products of 2 D operations a score (attn_dq: three), because dQ's sums run along the other axis and would need
+// atomics here.  The matrix core is 45% busy: 64 queries against 128 keys read 272 KB of LDS, 2200 cycles beside 2048 of
+// products, and two waves a SIMD overlap them in part.  Four samples of 2048, 64 heads of 128 on
+// 8: 0.70 to 0.74 ms (550 GFLOP, 750 TFLOP/s); two of 1024, 32 heads on 8: 66 us and 8 for the join.
 template <int D>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;
@@ -665,7 +686,8 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, n0 = it[2], steps = it[3] - n0;
   // The last queries first, one query head after the other: the workgroups of a sequence's key tiles run
   // through the same rows at the same time, whatever their first query, and share them in L2 (heads
-  // outside and queries upwards missed more than half of its lines and took ...).
+  // outside and queries upwards missed 56% of its lines, this order 25%: four samples of 2048, 64 heads on 8, 1156 us
+  // and 1006 in an earlier form).
   auto q_of = [&](int n) { return q_first + (per_head - 1 - (n0 + n) / a.group) * TQ; };
   auto load = [&](int n, char* b, int ln) {
     const int h = hk * a.group + (n0 + n) % a.group, qt = q_of(n);
