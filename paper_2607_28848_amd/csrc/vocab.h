@@ -46,7 +46,10 @@ __device__ __forceinline__ bool own_reference(float m, float have, bool first) {
   return m > have + kVocabSlack || (first && m < have - kVocabSlack);
 }
 
-hipError_t launch_vocab_f32_logits(const VocabArgs& a, hipStream_t s);
+// Rows of an fp32 tile (20 rows against 20000 of 1024, with the gradient: 56 us in tiles of 32, 94 in one of 64 rows).
+inline int vocab_f32_rows(int32_t T) { return T <= 32 ? 32 : 64; }
+
+hipError_t launch_vocab_f32_logits(const VocabArgs& a, int cus, hipStream_t s);
 hipError_t launch_vocab_f32_grad(const VocabArgs& a, hipStream_t s);
 
 }  // namespace dsv

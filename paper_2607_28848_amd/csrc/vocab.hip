@@ -364,12 +364,12 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
   Pieces r{};
   const bool bf = dt == DSV_BF16;
   const int64_t size = bf ? 2 : 4;
-  r.tw = bf ? 256 : 64;
+  r.tw = bf ? 256 : 128;
   int64_t width = (V + r.tw - 1) / r.tw * r.tw;
   r.split = 1;
   if (grad) {
     // 32-bit offsets of the second product's reads of W, and P within its room
-    const int64_t most = std::min(kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 29) / ldw) / r.tw * r.tw;
+    const int64_t most = std::min(kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 30) / (size * ldw)) / r.tw * r.tw;
     const int64_t n = (V + std::max<int64_t>(most, r.tw) - 1) / std::max<int64_t>(most, r.tw);
     width = ((V + n - 1) / n + r.tw - 1) / r.tw * r.tw;
   }
@@ -378,15 +378,14 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
   r.split_len = r.width;
   if (grad && T > 0) {
     // Ranges: whole rounds of tiles against the traffic of the ranges' own sums, in microseconds.
-    const int tm = bf ? (T <= 128 ? 128 : 256) : 64, tn = bf ? 256 : 64;
+    const int tm = bf ? (T <= 128 ? 128 : 256) : vocab_f32_rows(T), tn = r.tw;
     const int64_t tiles = (int64_t)((T + tm - 1) / tm) * ((K + tn - 1) / tn);
-    const double step = bf ? (tm == 128 ? 0.8 : 1.45) : 0.6;  // of 64 contraction values
-    const int64_t slots = bf ? cus : 4 * (int64_t)cus;
+    const double step = bf ? (tm == 128 ? 0.8 : 1.45) : (tm == 32 ? 1.0 : 1.9);  // of 64 contraction values
     double best = 1e30;
     for (int s = 1; s <= 32; ++s) {
       const int64_t len = (width / 64 + s - 1) / s * 64;
       if (s > 1 && len < 512) break;
-      const double t = (double)((tiles * s + slots - 1) / slots) * (len / 64) * step + s * (double)T * K * 8 / 4.5e6;
+      const double t = (double)((tiles * s + cus - 1) / cus) * (len / 64) * step + s * (double)T * K * 8 / 4.5e6;
       if (t < best) best = t, r.split = s, r.split_len = (int32_t)len;
     }
     r.split = (int32_t)((width + r.split_len - 1) / r.split_len);
@@ -449,7 +448,8 @@ hipError_t launch_grad(const VocabArgs& a, hipStream_t s) {
 
 int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   const bool bf = dt == DSV_BF16;
-  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, device_cus());
+  const int cus = device_cus();
+  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, cus);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
   if (ws_bytes < pc.total) return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
@@ -472,7 +472,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.first = i == 0;
     a.last = i + 1 == pc.n;
     a.split = pc.split;
-    hipError_t e = !bf ? launch_vocab_f32_logits(a, s) : a.grad ? launch_logits<true>(a, s) : launch_logits<false>(a, s);
+    hipError_t e = !bf ? launch_vocab_f32_logits(a, cus, s) : a.grad ? launch_logits<true>(a, s) : launch_logits<false>(a, s);
     if (e != hipSuccess) return DSV_ERR_DEVICE;
     if (bf) hipLaunchKernelGGL(vocab_fold_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
     else hipLaunchKernelGGL(vocab_fold_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
