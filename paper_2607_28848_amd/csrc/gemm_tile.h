@@ -5,6 +5,7 @@
 // 4 waves in a 2 x 2 grid, each FM x 8 blocks of 16 x 16 (FM 8: 256 rows, FM 4: 128).  Operand tiles go
 // from global memory straight into LDS.  Rows and columns past the operands, and contraction values past C,
 // read zeros.
+// tile_ring is tile_nt's form for products of few tiles, in both types.
 // Sums: acc[i][j][v] is row wm * 16 FM + 16 i + l % 16, column wn * 128 + 16 j + 4 (l / 16) + v.
 #pragma once
 
@@ -26,6 +27,15 @@ template <int V>
 struct num_c {
   static constexpr int value = V;
 };
+
+// f(num_c<U>) for U of [U, END)
+template <int U, int END, typename F>
+__device__ __forceinline__ void ring_tail(F&& f) {
+  if constexpr (U < END) {
+    f(num_c<U>{});
+    ring_tail<U + 1, END>(f);
+  }
+}
 
 constexpr int kTileStage = 2 * 256 * 64 * 2;    // bytes of one of tile_nt's two buffers (FM 8)
 constexpr int kTileStageNN = 2 * 256 * 32 * 2;  // bytes of one of tile_nn's four buffers (FM 8)
@@ -289,6 +299,121 @@ __device__ __forceinline__ void tile_nn(const uint16_t* P, int64_t ldp, int p_ro
   if (kt + 2 < nk) step(flag_c<false>{}, num_c<0>{}, kt, b2, nullptr);
   vmem_wait_all();  // nothing lands in the buffers any more
   __syncthreads();  // the buffers are free
+}
+
+// NT tiles of 32 FM rows and 32 FN columns in either type, for products of few tiles: a step of 128 bytes of every row
+// through a ring of NB buffers, so that its loads have NB - 1 steps' time to arrive.  T: uint16_t (bf16,
+// v_mfma_f32_16x16x32_bf16, C a multiple of 8) or float (v_mfma_f32_16x16x4_f32, C a multiple of 4; slot l / 16 of
+// instruction e stands for value 16 s + 4 (l / 16) + e, so a lane's values of a row are a 16-byte chunk here too).
+// ring: NB buffers of kRingStage bytes.  Sums: acc[i][j][v] is row 16 FM wm + 16 i + l % 16, column
+// 16 FN wn + 16 j + 4 (l / 16) + v.
+template <int FM, int FN>
+constexpr int kRingStage = 32 * (FM + FN) * 128;
+
+template <typename T, int FM, int FN, int NB>
+__device__ __forceinline__ void tile_ring(const T* P, int64_t ldp, int p_rows, const T* Q, int64_t ldq_, int q_cols, int C,
+                                          int turn, char* const (&ring)[NB], f32x4 (&acc)[FM][FN]) {
+  constexpr int A_BYTES = 32 * FM * 128, N = FM + FN, E = 16 / sizeof(T), TK = 8 * E;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4, lr = lane >> 3;
+  const int nk = (C + TK - 1) / TK, lda = (int)ldp * (int)sizeof(T), ldb = (int)ldq_ * (int)sizeof(T);  // bytes
+  const i32x4 ra = tile_rsrc(P, (int64_t)(min(32 * FM, p_rows) - 1) * lda + ((C + E - 1) / E) * 16);
+  const i32x4 rb = tile_rsrc(Q, (int64_t)(min(32 * FN, q_cols) - 1) * ldb + ((C + E - 1) / E) * 16);
+  constexpr int kNone = 0x7FFFFFF0;  // past every descriptor
+  // chunk c of row r in slot c ^ r % 8 ^ r / 8 % 8: 16 rows put a chunk in 16 bank groups
+  int chunk_a[FM], chunk_b[FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) chunk_a[i] = (lane & 7) ^ lr ^ ((FM * wave + i) & 7);
+#pragma unroll
+  for (int i = 0; i < FN; ++i) chunk_b[i] = (lane & 7) ^ lr ^ ((FN * wave + i) & 7);
+  // Steps in the order turn, turn + 1, .., nk - 1, 0, .. (where all are whole).  Past the last one it is loaded again, for
+  // a buffer that is not read: so each step's loads are followed by the same number of others.
+  const int first = C % TK == 0 ? turn % nk : 0;
+  auto load = [&](int kt, char* st, int e) {
+    const int at = min(kt, nk - 1) + first, k = at < nk ? at : at - nk;
+    if (e < FM) {
+      const int q = wave * FM + e;
+      llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16,
+                                        k * TK + E * chunk_a[e] < C ? 16 * chunk_a[e] + lr * lda : kNone,
+                                        __builtin_amdgcn_readfirstlane(q * 8 * lda + k * 128), 0, 0);
+    } else {
+      const int q = wave * FN + e - FM;
+      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16,
+                                        k * TK + E * chunk_b[e - FM] < C ? 16 * chunk_b[e - FM] + lr * ldb : kNone,
+                                        __builtin_amdgcn_readfirstlane(q * 8 * ldb + k * 128), 0, 0);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < NB - 1; ++u)
+#pragma unroll
+    for (int e = 0; e < N; ++e) load(u, ring[u], e);
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      asm volatile("" : "+a"(acc[i][j]));  // as in tile_nt
+    }
+  // Fragment addresses: a lane part picked by the half step and block (the chunk swizzle), plus an immediate.
+  const int part = g4 ^ (l15 & 7) ^ (l15 >> 3);
+  int off_a[4], off_b[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    off_a[x] = (16 * FM * wm + l15) * 128 + 16 * (part ^ ((2 * FM * wm) & 7) ^ (2 * x));
+    off_b[x] = A_BYTES + (16 * FN * wn + l15) * 128 + 16 * (part ^ ((2 * FN * wn) & 7) ^ (2 * x));
+  }
+  // Step kt in `st`, with the loads of step kt + NB - 1 into `nxt`, which the step before this one has read; behind the
+  // step's own loads are those of AFTER more.
+  auto step = [&](auto with, auto after, int kt, const char* st, char* nxt) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(decltype(after)::value * N));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // not __syncthreads(), which would wait for every load
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 fa[2][FM], fb[2][FN];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[s][i] = *reinterpret_cast<const u32x4*>(st + off_a[((2 * s) ^ i) & 3] + 2048 * i);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[s][j] = *reinterpret_cast<const u32x4*>(st + off_b[((2 * s) ^ j) & 3] + 2048 * j);
+    }
+    if constexpr (decltype(with)::value) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) load(kt + NB - 1, nxt, e);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf(fb[s][j]), as_bf(fa[s][i]), acc[i][j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fb[s][j][e]), __uint_as_float(fa[s][i][e]),
+                                                               acc[i][j], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int kt = 0;
+  for (; kt + NB <= nk; kt += NB) {
+#pragma unroll
+    for (int u = 0; u < NB; ++u) step(flag_c<true>{}, num_c<NB - 2>{}, kt + u, ring[u], ring[(u + NB - 1) % NB]);
+  }
+  ring_tail<0, NB - 1>([&](auto u) {
+    constexpr int U = decltype(u)::value;
+    if (kt + U < nk) step(flag_c<false>{}, num_c<NB - 2 - U>{}, kt, ring[U], nullptr);
+  });
+  vmem_wait_all();  // nothing lands in the buffers any more
+  __syncthreads();
 }
 
 }  // namespace

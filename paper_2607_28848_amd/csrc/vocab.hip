@@ -34,41 +34,58 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 // ---- logits -------------------------------------------------------------------------------------------
-// GRAD: P is written.  FM: 16-row blocks per wave (8: 256-row tiles, 4: 128, for up to 128 rows, where the head's stream
-// is what bounds it: one row against 128256 of 4096 takes 180 us, 5.8 TB/s, 128 rows 195).  Else the matrix core:
-// 4096 rows, 32256 x 8192 a piece, 1.62 ms (1330 TFLOP/s).
-template <bool GRAD, int FM>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void vocab_logits_kernel(VocabArgs a) {
-  constexpr int WM = 16 * FM, TM = 2 * WM;
-  __shared__ __attribute__((aligned(1024))) char smem0[kTileStage];
-  __shared__ __attribute__((aligned(1024))) char smem1[kTileStage];
+// GRAD: P is written.  Tiles of 32 FM rows and 32 FN columns; NB: buffers (2: tile_nt, else tile_ring).  Up to 128 rows
+// the stream of a large head is what bounds it: one row against 128256 of 4096 takes 180 us, 5.8 TB/s, 128 rows 195.
+// Else the matrix core: 4096 rows, 32256 x 8192 a piece, 1.62 ms (1330 TFLOP/s).
+template <bool GRAD, int FM, int FN, int NB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 ? 1 : 2))) void vocab_logits_kernel(VocabArgs a) {
+  constexpr int WM = 16 * FM, TM = 2 * WM, WN = 16 * FN, TN = 2 * WN;
+  constexpr int kStage = NB == 2 ? kTileStage : kRingStage<FM, FN>;
+  __shared__ __attribute__((aligned(1024))) char smem0[kStage];
+  __shared__ __attribute__((aligned(1024))) char smem1[kStage];
   __shared__ float red[3][2][TM];  // [maximum, sum, reference][column half][row]
   const int n_m = (a.T + TM - 1) / TM;
   int mt, nt;
   tile_at(tile_of(blockIdx.x, gridDim.x), n_m, a.n_ct, mt, nt);
-  const int m0 = mt * TM, n0 = nt * 256, cols = min(256, a.vn - n0);
+  const int m0 = mt * TM, n0 = nt * TN, cols = min(TN, a.vn - n0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4;
-  f32x4 acc[FM][8];
+  f32x4 acc[FM][FN];
   // with one row tile the head's rows come from memory once, and neighbouring tiles begin a step apart (one row
   // against 128256 of 4096: 215 us in step, 185 so; with more row tiles it changes nothing)
-  char* const idle = tile_nt<FM>(static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
-                                             static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols,
-                                             a.K,
-                                             n_m == 1 ? nt : 0, smem0, smem1, acc);
-  const int c0 = wn * 128 + 4 * g4;  // column of acc[.][j][v]: c0 + 16 j + v
+  const int turn = n_m == 1 ? nt : 0;
+  const uint16_t* const X = static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx;
+  const uint16_t* const W = static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw;
+  char* idle = smem0;
+  if constexpr (NB == 2) {
+    idle = tile_nt<FM>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, smem0, smem1, acc);
+  } else {
+    __shared__ __attribute__((aligned(1024))) char smem2[kStage];
+    if constexpr (NB == 3) {
+      char* const ring[3] = {smem0, smem1, smem2};
+      tile_ring<uint16_t, FM, FN, 3>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, ring, acc);
+    } else {
+      static_assert(NB == 6, "buffers");
+      __shared__ __attribute__((aligned(1024))) char smem3[kStage];
+      __shared__ __attribute__((aligned(1024))) char smem4[kStage];
+      __shared__ __attribute__((aligned(1024))) char smem5[kStage];
+      char* const ring[6] = {smem0, smem1, smem2, smem3, smem4, smem5};
+      tile_ring<uint16_t, FM, FN, 6>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, ring, acc);
+    }
+  }
+  const int c0 = wn * WN + 4 * g4;  // column of acc[.][j][v]: c0 + 16 j + v
   // The sums are read twice and never written: in registers of the matrix core from the first to the last.
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     float m = -INFINITY;
-    if (cols == 256) {
+    if (cols == TN) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) m = fmaxf(m, acc[i][j][v]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) m = fmaxf(m, c0 + 16 * j + v < cols ? acc[i][j][v] : -INFINITY);
     }
@@ -76,10 +93,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     if (lane < 16) red[0][wn][wm * WM + 16 * i + l15] = m;
   }
   __syncthreads();
-  // Terms: 32 rows of 128 columns per wave at a time, whose P goes through the idle buffer for 16-byte stores.
-  constexpr int SRS = 128 * 2 + 16;
+  // Terms: 32 rows of 16 FN columns per wave at a time, whose P goes through the idle buffer for 16-byte stores.
+  constexpr int SRS = WN * 2 + 16, RPS = 64 / (2 * FN);  // rows a store instruction covers
+  static_assert(4 * 32 * SRS <= kStage, "slices");
   char* const slice = idle + wave * 32 * SRS;
-  uint16_t* const P = static_cast<uint16_t*>(a.P) + (int64_t)(m0 + wm * WM) * a.ldp + n0 + wn * 128;
+  uint16_t* const P = static_cast<uint16_t*>(a.P) + (int64_t)(m0 + wm * WM) * a.ldp + n0 + wn * WN;
 #pragma unroll
   for (int t = 0; t < FM / 2; ++t) {
 #pragma unroll
@@ -92,14 +110,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
       const int tc = in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < FN; ++j) {
         f32x4 e;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const float z = acc[i][j][v];
           e[v] = __builtin_amdgcn_exp2f(z * kLog2e - base);
           if (tc == 16 * j + v) e[v] = 0.f;
-          if (cols < 256 && c0 + 16 * j + v >= cols) e[v] = 0.f;
+          if (cols < TN && c0 + 16 * j + v >= cols) e[v] = 0.f;
           sum += e[v];
         }
         if constexpr (GRAD)
@@ -115,10 +133,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     if constexpr (GRAD) {
       asm volatile("" ::: "memory");  // a wave's LDS accesses run in order
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int r = 4 * q + (lane >> 4);
-        const u32x4 v = *reinterpret_cast<const u32x4*>(slice + r * SRS + 16 * l15);
-        if (m0 + wm * WM + 32 * t + r < a.T) *reinterpret_cast<u32x4*>(P + (int64_t)(32 * t + r) * a.ldp + 8 * l15) = v;
+      for (int q = 0; q < FN; ++q) {
+        const int r = RPS * q + lane / (2 * FN), c = lane % (2 * FN);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(slice + r * SRS + 16 * c);
+        if (m0 + wm * WM + 32 * t + r < a.T) *reinterpret_cast<u32x4*>(P + (int64_t)(32 * t + r) * a.ldp + 8 * c) = v;
       }
       asm volatile("" ::: "memory");
     }
@@ -358,6 +376,21 @@ struct Pieces {
   size_t p, stats, rows, o, total;
 };
 
+// Column tile of the logits: whole tiles (256, of 256 or 128 rows) where they fill the CUs, else 128 x 128 or 64 x 64 ones,
+// whichever takes the least time in rounds of one tile a CU.  Microseconds a round and 64 contraction values: 1.5 for
+// 256 x 256, 1.05 for 128 x 256, 0.62 and 0.28 for the small ones, each measured at 5000, 20000 and 50000 columns.
+// Losses of rows of 4096, in microseconds, whole / 128 / 64: 64 rows against 5000 75 / 45 / 26, against 20000 78 / 49 /
+// 51, against 50000 88 / 94 / 97; 500 rows against 5000 101 / 49 / 65, against 20000 108 / 130 / 186.
+int logits_tile(int32_t T, int64_t width, int cus) {
+  auto rounds = [&](int tm, int tn) {
+    const int64_t n = ((T + tm - 1) / tm) * ((width + tn - 1) / tn);
+    return (double)((n + cus - 1) / cus);
+  };
+  const double whole = T <= 128 ? 1.05 * rounds(128, 256) : 1.5 * rounds(256, 256);
+  const double t128 = 0.62 * rounds(128, 128), t64 = 0.28 * rounds(64, 64);
+  return whole <= std::min(t128, t64) ? 256 : t128 <= t64 ? 128 : 64;
+}
+
 constexpr int64_t kPieceBytes = 256 << 20;  // of P: the size of the last-level cache
 
 Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool grad, int cus) {
@@ -376,9 +409,10 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
   r.width = (int32_t)width;
   r.n = (int32_t)((V + width - 1) / width);
   r.split_len = r.width;
+  if (bf) r.tw = logits_tile(T, r.width, cus);
   if (grad && T > 0) {
     // Ranges: whole rounds of tiles against the traffic of the ranges' own sums, in microseconds.
-    const int tm = bf ? (T <= 128 ? 128 : 256) : vocab_f32_rows(T), tn = r.tw;
+    const int tm = bf ? (T <= 128 ? 128 : 256) : vocab_f32_rows(T), tn = bf ? 256 : 128;
     const int64_t tiles = (int64_t)((T + tm - 1) / tm) * ((K + tn - 1) / tn);
     const double step = bf ? (tm == 128 ? 0.8 : 1.45) : (tm == 32 ? 1.0 : 1.9);  // of 64 contraction values
     double best = 1e30;
@@ -425,11 +459,12 @@ int check_shape(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t ldw, int6
 
 template <bool GRAD>
 hipError_t launch_logits(const VocabArgs& a, hipStream_t s) {
-  if (a.T <= 128)
-    hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4>), dim3((unsigned)a.n_ct), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 8>), dim3((unsigned)(a.n_ct * (int64_t)((a.T + 255) / 256))), dim3(256),
-                       0, s, a);
+  const int tm = a.tw < 256 ? a.tw : a.T <= 128 ? 128 : 256;
+  const dim3 grid((unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm)));
+  if (a.tw == 64) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 6>), grid, dim3(256), 0, s, a);
+  else if (a.tw == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 4, 3>), grid, dim3(256), 0, s, a);
+  else if (tm == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 8, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 8, 8, 2>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -17,30 +17,29 @@ namespace dsv {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kStage = 64 * 128 + 128 * 128;  // bytes of a buffer (FM 2): rows of P, then Q's rows or columns
+constexpr int kStage = kRingStage<2, 4>;
 
-// Sums of a tile: acc[i][j][v] is row 16 FM wm + 16 i + l % 16, column 64 wn + 16 j + 4 (l / 16) + v.
-// NT: Q [n][C], C a multiple of 4; NN: Q [C][n], P's rows hold zeros from C to a multiple of 4.  Rows, columns and
-// contraction values that do not exist count as zeros.
-template <bool NN, int FM>
-__device__ __forceinline__ void tile_f32(const float* P, int64_t ldp, int p_rows, const float* Q, int64_t ldq_, int q_cols,
+// out[m][n] = sum_c P[m][c] Q[c][n] of a tile of 32 FM rows and 128 columns: tile_ring's loop with three buffers, and with
+// Q's rows as they lie.  P's rows hold zeros from C to a multiple of 4; rows, columns and contraction values that do not
+// exist count as zeros.
+template <int FM>
+__device__ __forceinline__ void tile_nn_f32(const float* P, int64_t ldp, int p_rows, const float* Q, int64_t ldq_, int q_cols,
                                          int C, char* b0, char* b1, char* b2, f32x4 (&acc)[FM][4]) {
   constexpr int A_BYTES = 32 * FM * 128, N = FM + 4, TK = 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4, lr = lane >> 3;
   const int ld = (int)ldp, ldq = (int)ldq_, nk = (C + TK - 1) / TK;
   const i32x4 ra = tile_rsrc(P, ((int64_t)(min(32 * FM, p_rows) - 1) * ld + ((C + 3) & ~3)) * 4);
-  const i32x4 rb = NN ? tile_rsrc(Q, ((int64_t)(C - 1) * ldq + q_cols) * 4)
-                      : tile_rsrc(Q, ((int64_t)(min(128, q_cols) - 1) * ldq + C) * 4);
-  // Rows of 128 bytes: chunk c of row r in slot c ^ r % 8 ^ r / 8 % 8 (16 rows put a chunk in 16 bank groups).  NN, rows
-  // of 512 bytes: the 64-byte block b of row c in block b ^ c / 4 % 4 (a read's four rows in different banks).
+  const i32x4 rb = tile_rsrc(Q, ((int64_t)(C - 1) * ldq + q_cols) * 4);
+  // P: chunk c of row r in slot c ^ r % 8 ^ r / 8 % 8.  Q, rows of 512 bytes: the 64-byte block b of row c in block
+  // b ^ c / 4 % 4 (a read's four rows in different banks).
   constexpr int kNone = 0x7FFFFFF0;  // past every descriptor
   int chunk_a[FM], chunk_b[4];
 #pragma unroll
   for (int i = 0; i < FM; ++i) chunk_a[i] = (lane & 7) ^ lr ^ ((FM * wave + i) & 7);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    chunk_b[i] = NN ? (lane & 31) ^ 4 * ((2 * wave + (i >> 1)) & 3) : (lane & 7) ^ lr ^ ((4 * wave + i) & 7);
+    chunk_b[i] = (lane & 31) ^ 4 * ((2 * wave + (i >> 1)) & 3);
   // Load e of step kt (P's first).  Past the last step the last is loaded again, for a buffer that is not read: so each
   // step's loads are followed by the same number of others.
   auto load = [&](int kt, char* st, int e) {
@@ -50,16 +49,11 @@ __device__ __forceinline__ void tile_f32(const float* P, int64_t ldp, int p_rows
       llvm_amdgcn_raw_buffer_load_lds_t(ra, (lds_u32*)(st + q * 1024), 16,
                                         k0 + 4 * chunk_a[e] < C ? 16 * chunk_a[e] + lr * ld * 4 : kNone,
                                         __builtin_amdgcn_readfirstlane((q * 8 * ld + k0) * 4), 0, 0);
-    } else if constexpr (NN) {
+    } else {
       const int q = wave * 4 + e - FM;
       llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16,
                                         16 * chunk_b[e - FM] + (lane >> 5) * ldq * 4,
                                         __builtin_amdgcn_readfirstlane((k0 + 2 * q) * ldq * 4), 0, 0);
-    } else {
-      const int q = wave * 4 + e - FM;
-      llvm_amdgcn_raw_buffer_load_lds_t(rb, (lds_u32*)(st + A_BYTES + q * 1024), 16,
-                                        k0 + 4 * chunk_b[e - FM] < C ? 16 * chunk_b[e - FM] + lr * ldq * 4 : kNone,
-                                        __builtin_amdgcn_readfirstlane((q * 8 * ldq + k0) * 4), 0, 0);
     }
   };
 #pragma unroll
@@ -76,8 +70,7 @@ __device__ __forceinline__ void tile_f32(const float* P, int64_t ldp, int p_rows
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
     off_a[x] = (16 * FM * wm + l15) * 128 + 16 * (part ^ (2 * FM * wm) ^ (2 * x));
-    off_b[x] = NN ? A_BYTES + 4 * g4 * 512 + 256 * wn + 64 * (x ^ g4) + 4 * l15
-                  : A_BYTES + (64 * wn + l15) * 128 + 16 * (part ^ (2 * x));
+    off_b[x] = A_BYTES + 4 * g4 * 512 + 256 * wn + 64 * (x ^ g4) + 4 * l15;
   }
   // Step kt in `st`, with the loads of step kt + 2 into `nxt`, which the step before this one has read; behind the
   // step's own loads are those of AFTER more.
@@ -94,12 +87,8 @@ __device__ __forceinline__ void tile_f32(const float* P, int64_t ldp, int p_rows
       for (int i = 0; i < FM; ++i) fa[s][i] = *reinterpret_cast<const f32x4*>(st + off_a[(2 * s) ^ i] + 2048 * i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (NN) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) fb[s][j][e] = *reinterpret_cast<const float*>(st + off_b[j] + 8192 * s + 512 * e);
-        } else {
-          fb[s][j] = *reinterpret_cast<const f32x4*>(st + off_b[(2 * s) ^ j] + 2048 * j);
-        }
+        for (int e = 0; e < 4; ++e) fb[s][j][e] = *reinterpret_cast<const float*>(st + off_b[j] + 8192 * s + 512 * e);
       }
     }
     if constexpr (decltype(with)::value) {
@@ -151,8 +140,9 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   const int m0 = TM * mt, n0 = 128 * nt, cols = min(128, a.vn - n0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l15 = lane & 15;
   f32x4 acc[FM][4];
-  tile_f32<false, FM>(static_cast<const float*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
-                      static_cast<const float*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols, a.K, b0, b1, b2, acc);
+  char* const ring[3] = {b0, b1, b2};
+  tile_ring<float, FM, 4, 3>(static_cast<const float*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
+                             static_cast<const float*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols, a.K, 0, ring, acc);
   const int c0 = 64 * wn + 4 * (lane >> 4);
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
@@ -223,9 +213,8 @@ __global__ __launch_bounds__(256) void vocab_f32_grad_kernel(VocabArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (C > 0)  // a short last piece ends before some ranges
-    tile_f32<true, FM>(static_cast<const float*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0,
-                       static_cast<const float*>(a.W) + (int64_t)(a.v0 + c0) * a.ldw + n0, a.ldw, a.K - n0, C, b0, b1, b2,
-                       acc);
+    tile_nn_f32<FM>(static_cast<const float*>(a.P) + (int64_t)m0 * a.ldp + c0, a.ldp, a.T - m0,
+                    static_cast<const float*>(a.W) + (int64_t)(a.v0 + c0) * a.ldw + n0, a.ldw, a.K - n0, C, b0, b1, b2, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
