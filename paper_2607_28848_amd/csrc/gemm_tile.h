@@ -326,9 +326,9 @@ __device__ __forceinline__ void tile_ring(const T* P, int64_t ldp, int p_rows, c
   for (int i = 0; i < FM; ++i) chunk_a[i] = (lane & 7) ^ lr ^ ((FM * wave + i) & 7);
 #pragma unroll
   for (int i = 0; i < FN; ++i) chunk_b[i] = (lane & 7) ^ lr ^ ((FN * wave + i) & 7);
-  // Steps in the order turn, turn + 1, .., nk - 1, 0, .. (where all are whole).  Past the last one it is loaded again, for
-  // a buffer that is not read: so each step's loads are followed by the same number of others.
-  const int first = C % TK == 0 ? turn % nk : 0;
+  // Steps in the order turn, turn + 1, .., nk - 1, 0, ..  Past the last one it is loaded again, for a buffer that is not
+  // read: so each step's loads are followed by the same number of others.
+  const int first = turn % nk;
   auto load = [&](int kt, char* st, int e) {
     const int at = min(kt, nk - 1) + first, k = at < nk ? at : at - nk;
     if (e < FM) {

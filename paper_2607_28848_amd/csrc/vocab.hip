@@ -64,6 +64,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
     if constexpr (NB == 3) {
       char* const ring[3] = {smem0, smem1, smem2};
       tile_ring<uint16_t, FM, FN, 3>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, ring, acc);
+    } else if constexpr (NB == 4) {
+      __shared__ __attribute__((aligned(1024))) char smem3[kStage];
+      char* const ring[4] = {smem0, smem1, smem2, smem3};
+      tile_ring<uint16_t, FM, FN, 4>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, ring, acc);
     } else {
       static_assert(NB == 6, "buffers");
       __shared__ __attribute__((aligned(1024))) char smem3[kStage];
@@ -348,6 +352,7 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(VocabArgs a) {
   if (c < a.K) {
     f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
     if (has) {
+#pragma unroll 4
       for (int s = 0; s < a.split; ++s) x += *reinterpret_cast<const f32x4*>(a.O + ((int64_t)s * a.T + row) * a.K + c);
       x = (x - load4(w + c) * others) * f;
     }
@@ -457,11 +462,15 @@ int check_shape(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t ldw, int6
   return stride(ldw, K, w);
 }
 
+// Tiles of 64 rows have six buffers where each has a CU to itself, else four, which leave room for two on a CU (one row of
+// 4096 against 5000: 22 us with six, 25 with four; 45 rows of 816 against 113000: 65 and 57).
 template <bool GRAD>
-hipError_t launch_logits(const VocabArgs& a, hipStream_t s) {
+hipError_t launch_logits(const VocabArgs& a, int cus, hipStream_t s) {
   const int tm = a.tw < 256 ? a.tw : a.T <= 128 ? 128 : 256;
   const dim3 grid((unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm)));
-  if (a.tw == 64) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 6>), grid, dim3(256), 0, s, a);
+  if (a.tw == 64 && grid.x <= (unsigned)cus)
+    hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 6>), grid, dim3(256), 0, s, a);
+  else if (a.tw == 64) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 4>), grid, dim3(256), 0, s, a);
   else if (a.tw == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 4, 3>), grid, dim3(256), 0, s, a);
   else if (tm == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 8, 2>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 8, 8, 2>), grid, dim3(256), 0, s, a);
@@ -507,7 +516,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.first = i == 0;
     a.last = i + 1 == pc.n;
     a.split = pc.split;
-    hipError_t e = !bf ? launch_vocab_f32_logits(a, cus, s) : a.grad ? launch_logits<true>(a, s) : launch_logits<false>(a, s);
+    hipError_t e = !bf ? launch_vocab_f32_logits(a, cus, s) : a.grad ? launch_logits<true>(a, cus, s) : launch_logits<false>(a, cus, s);
     if (e != hipSuccess) return DSV_ERR_DEVICE;
     if (bf) hipLaunchKernelGGL(vocab_fold_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
     else hipLaunchKernelGGL(vocab_fold_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
