@@ -28,14 +28,14 @@ struct AttnArgs {
   float* lse2;           // bf16: lse of the compact rows, base 2
   // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
   // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
-  // Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].  fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
+  // Query tiles: [slot][hq][kAttnBwdRows][D].  Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].  fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
   float* part_o;
   float* part_ml;
-  // The join of both forms: the forward tiles' own, its items and workgroups.
-  const float* fwd_o;
-  const float* fwd_ml;
-  const int32_t* fwd_join;
-  int32_t fwd_join_groups;
+  // A join's first part (forward tiles, dQ): its sums, items and workgroups; the rest is as above.
+  const float* first_o;
+  const float* first_ml;
+  const int32_t* first_join;
+  int32_t first_groups;
 };
 
 // fp32 mode: tiles of kAttnF32Rows.

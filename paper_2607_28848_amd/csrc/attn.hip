@@ -249,6 +249,18 @@ __device__ __forceinline__ void store_cols(const AttnView& t, int64_t row, int h
     }
 }
 
+// The same as they are, in fp32, to the row at p.
+template <int D>
+__device__ __forceinline__ void store_sums(float* p, const f32x16 (&acc)[D / 32]) {
+  p += 4 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(p + 32 * t + 8 * i) =
+          f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+}
+
 // ---------------------------------------------------------------------------------------------------
 // O and lse of 128 queries of one head (or the sums of a piece of their keys): 32 queries a wave, 64 keys a step.
 //
@@ -338,13 +350,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   if (it[5] > 1) {
     const int64_t slot = (int64_t)it[4] * a.hq + h;
     const int row = 32 * wave + (lane & 31);
-    float* p = a.part_o + (slot * kAttnFwdRows + row) * D + 4 * (lane >> 5);
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(p + 32 * t + 8 * i) =
-            f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+    store_sums<D>(a.part_o + (slot * kAttnFwdRows + row) * D, acc);
     if (lane < 32) {
       a.part_ml[slot * 2 * kAttnFwdRows + row] = run.ref;
       a.part_ml[(slot * 2 + 1) * kAttnFwdRows + row] = sum;
@@ -522,17 +528,17 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int at = blockIdx.x, row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (D / 8);
-  if (at < a.fwd_join_groups) {
+  if (at < a.first_groups) {
     constexpr int BL = kAttnFwdRows / 32;
     const int item = at / (BL * a.hq), h = at / BL % a.hq;
-    const int32_t* it = a.fwd_join + 4 * (int64_t)item;
+    const int32_t* it = a.first_join + 4 * (int64_t)item;
     const Seq s(a, it[0]);
     const int r = 32 * (at % BL) + row, q = it[1] + r;
     if (q >= s.ql) return;
-    join_row<D>(a, a.fwd_o, a.fwd_ml, (int64_t)it[2] * a.hq + h, a.hq, it[3], kAttnFwdRows, r, c0, (int64_t)s.q0 + q, h);
+    join_row<D>(a, a.first_o, a.first_ml, (int64_t)it[2] * a.hq + h, a.hq, it[3], kAttnFwdRows, r, c0, (int64_t)s.q0 + q, h);
     return;
   }
-  const int item = (at - a.fwd_join_groups) / a.hkv, hk = (at - a.fwd_join_groups) % a.hkv;
+  const int item = (at - a.first_groups) / a.hkv, hk = (at - a.first_groups) % a.hkv;
   const int32_t* it = a.items + kAttnSplitWords * (int64_t)item;
   const int r = it[4] + row;
   if (it[5] == 1 || r >= it[1] * a.group) return;  // one piece: written by it
@@ -551,20 +557,21 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
   __shared__ __attribute__((aligned(1024))) char b1[2 * TILE];
   const int item = blockIdx.x / a.hq, h = head_of(a, blockIdx.x % a.hq);
-  const Seq s(a, a.items[2 * item]);
-  const int qt = a.items[2 * item + 1];
+  const int32_t* it = a.items + (int64_t)item * kAttnTileWords;
+  const Seq s(a, it[0]);
+  const int qt = it[1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int off = s.kl - s.ql, hk = h / a.group;
   const int q = qt + 32 * wave + (lane & 31);
   const bool in = q < s.ql;
-  const int k_end = min(s.kl, min(qt + kAttnBwdRows, s.ql) + off);
+  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnBwdRows, s.ql) + off), TK * it[3]);
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
   auto load = [&](int kt, char* b) {
     const int ln = fresh_lane();  // the loads' addresses kept in registers would spill others
     stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave, ln);
     stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave, ln);
   };
-  if (k_end > 0) load(0, b0);
+  if (k_first < k_end) load(k_first, b0);
   bf16x8 qf[D / 16], df[D / 16];
   row_frags<D>(a.Q, (int64_t)s.q0 + q, h, in, qf);
   row_frags<D>(a.dO, (int64_t)s.cq + q, h, in, df);
@@ -579,7 +586,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   }
   const float delta = pair_sum(dot);
   const float lse2 = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : 0.f;
-  if (in && lane < 32) {
+  if (in && lane < 32 && k_first == 0) {
     a.delta[h * a.train_q + s.cq + q] = delta;
     a.lse2[h * a.train_q + s.cq + q] = lse2;
   }
@@ -642,11 +649,13 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     if (kt + TK - 1 > wave_all) block(bool_c<true>{}, kt, cur);
     else block(bool_c<false>{}, kt, cur);
   };
-  for (int kt = 0; kt < k_end; kt += 2 * TK) {
+  for (int kt = k_first; kt < k_end; kt += 2 * TK) {
     step(kt, b0, b1);
     if (kt + TK < k_end) step(kt + TK, b1, b0);
   }
-  if (in) store_cols<D>(a.dQ, (int64_t)s.cq + q, h, acc, a.scale);
+  if (!in) return;
+  if (it[5] > 1) store_sums<D>(a.part_o + (((int64_t)it[4] * a.hq + h) * kAttnBwdRows + 32 * wave + (lane & 31)) * D, acc);
+  else store_cols<D>(a.dQ, (int64_t)s.cq + q, h, acc, a.scale);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -867,29 +876,47 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   else store_cols<D>(a.dV, (int64_t)s.ck + k, hk, acc, 1.f);
 }
 
-// dK (half 0) and dV of key tiles in pieces, added in order: 32 rows a workgroup, row tid / 8, D / 8 columns each.
+// Pieces of gradients, n of them `step` rows of D apart from p on, added in order and stored times f: columns
+// c0 .. c0 + D / 8 of a row of t.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dk_join_kernel(AttnArgs a) {
-  constexpr int BL = kAttnBwdRows / 32;
-  const int half = blockIdx.x & 1, blk = blockIdx.x / 2 % BL, hk = blockIdx.x / (2 * BL) % a.hkv;
-  const int32_t* it = a.items + 4 * (int64_t)(blockIdx.x / (2 * BL * a.hkv));
-  const Seq s(a, it[0]);
-  const int row = 32 * blk + (threadIdx.x >> 3), k = it[1] + row, c0 = (threadIdx.x & 7) * (D / 8);
-  if (k >= s.kl) return;
+__device__ __forceinline__ void join_grad(const float* p, int64_t step, int n, const AttnView& t, int64_t row, int h, int c0,
+                                          float f) {
   f32x4 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < it[3]; ++n) {
-    const float* p = a.part_o + ((((int64_t)(it[2] + n) * a.hkv + hk) * 2 + half) * kAttnBwdRows + row) * D + c0;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + 4 * i);
-  }
-  const AttnView& t = half ? a.dV : a.dK;
-  const float f = half ? 1.f : a.scale;
-  uint16_t* p = static_cast<uint16_t*>(t.ptr) + ((int64_t)s.ck + k) * t.row + hk * t.head + c0;
+    for (int i = 0; i < D / 32; ++i) o[i] += *reinterpret_cast<const f32x4*>(p + k * step * D + c0 + 4 * i);
+  uint16_t* out = static_cast<uint16_t*>(t.ptr) + row * t.row + h * t.head + c0;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
-    *reinterpret_cast<uint2*>(p + 4 * i) = make_uint2(f2bf2(o[i][0] * f, o[i][1] * f), f2bf2(o[i][2] * f, o[i][3] * f));
+    *reinterpret_cast<uint2*>(out + 4 * i) = make_uint2(f2bf2(o[i][0] * f, o[i][1] * f), f2bf2(o[i][2] * f, o[i][3] * f));
+}
+
+// Gradients of tiles in pieces, dQ first, then dK (half 0) and dV: 32 rows a workgroup, row tid / 8, D / 8 columns each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_grad_join_kernel(AttnArgs a) {
+  constexpr int BL = kAttnBwdRows / 32;
+  const int c0 = (threadIdx.x & 7) * (D / 8);
+  int at = blockIdx.x;
+  if (at < a.first_groups) {
+    const int h = at / BL % a.hq, r = 32 * (at % BL) + (threadIdx.x >> 3);
+    const int32_t* it = a.first_join + 4 * (int64_t)(at / (BL * a.hq));
+    const Seq s(a, it[0]);
+    if (it[1] + r >= s.ql) return;
+    join_grad<D>(a.first_o + (((int64_t)it[2] * a.hq + h) * kAttnBwdRows + r) * D, (int64_t)a.hq * kAttnBwdRows, it[3], a.dQ,
+                 (int64_t)s.cq + it[1] + r, h, c0, a.scale);
+    return;
+  }
+  at -= a.first_groups;
+  const int half = at & 1, hk = at / (2 * BL) % a.hkv, r = 32 * (at / 2 % BL) + (threadIdx.x >> 3);
+  const int32_t* it = a.items + 4 * (int64_t)(at / (2 * BL * a.hkv));
+  const Seq s(a, it[0]);
+  if (it[1] + r >= s.kl) return;
+  join_grad<D>(a.part_o + ((((int64_t)it[2] * a.hkv + hk) * 2 + half) * kAttnBwdRows + r) * D,
+               (int64_t)a.hkv * 2 * kAttnBwdRows, it[3], half ? a.dV : a.dK, (int64_t)s.ck + it[1] + r, hk, c0,
+               half ? 1.f : a.scale);
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -897,7 +924,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Workspace {
   size_t split_o, split_ml, fwd_o, fwd_ml;  // forward
-  size_t delta, lse2, dk;                   // backward (the two do not overlap on a stream: one room)
+  size_t delta, lse2, dq, dk;               // backward (the two do not overlap on a stream: one room)
   size_t total;
 };
 
@@ -927,6 +954,7 @@ Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   at = 0;
   w.delta = room((size_t)p.train_q * p.hq);
   w.lse2 = room(bf ? (size_t)p.train_q * p.hq : 0);
+  w.dq = room(bf ? (size_t)p.dq_slots * p.hq * kAttnBwdRows * p.d : 0);
   const int parts = f32_parts(p);
   w.dk = room(bf          ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d
               : parts > 1 ? (size_t)p.n_f32_dk * p.hkv * parts * 2 * kAttnF32Rows * p.d
@@ -1021,8 +1049,8 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   }
   const int64_t hq = p->hq, hkv = p->hkv;
   a.items = p->dptr(p->lay.fwd_items);
-  a.fwd_o = a.part_o = at<float>(ws, w.fwd_o);
-  a.fwd_ml = a.part_ml = at<float>(ws, w.fwd_ml);
+  a.first_o = a.part_o = at<float>(ws, w.fwd_o);
+  a.first_ml = a.part_ml = at<float>(ws, w.fwd_ml);
   hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, p->n_fwd * hq, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.split_items);
@@ -1031,10 +1059,10 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, p->n_split * hkv, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.join_items);
-  a.fwd_join = p->dptr(p->lay.fwd_join);
-  a.fwd_join_groups = (int32_t)(p->n_fwd_join * hq * (kAttnFwdRows / 32));
+  a.first_join = p->dptr(p->lay.fwd_join);
+  a.first_groups = (int32_t)(p->n_fwd_join * hq * (kAttnFwdRows / 32));
   const int64_t split = p->n_split == p->n_join ? 0 : p->n_join * hkv;  // one piece each: nothing to join
-  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, a.fwd_join_groups + split, s));
+  return status(launch(attn_join_kernel<64>, attn_join_kernel<128>, a, a.first_groups + split, s));
 }
 
 extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, const dsv_attn_view* Q,
@@ -1073,11 +1101,17 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
     return status(launch_attn_f32_dk(a, s));
   }
   a.items = p->dptr(p->lay.dq_items);
+  a.first_o = a.part_o = at<float>(ws, w.dq);
   hipError_t e = launch(attn_dq_kernel<64>, attn_dq_kernel<128>, a, p->n_dq * hq, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.dk_items);
+  a.part_o = at<float>(ws, w.dk);
   e = launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, p->n_dk * hkv, s, 512);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.dk_join);
-  return status(launch(attn_dk_join_kernel<64>, attn_dk_join_kernel<128>, a, p->n_dk_join * hkv * 2 * (kAttnBwdRows / 32), s));
+  a.first_join = p->dptr(p->lay.dq_join);
+  constexpr int blocks = kAttnBwdRows / 32;
+  a.first_groups = (int32_t)(p->n_dq_join * hq * blocks);
+  return status(launch(attn_grad_join_kernel<64>, attn_grad_join_kernel<128>, a,
+                       a.first_groups + p->n_dk_join * hkv * 2 * blocks, s));
 }

@@ -186,7 +186,7 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     const dsv_attn_seq& s = seqs[i];
     if (!s.is_train) continue;
     for (int64_t q = 0; q < s.q_len; q += kAttnBwdRows)
-      dq.add(keys_seen(s, std::min<int64_t>(q + kAttnBwdRows, s.q_len) - 1), i, q);
+      dq.add((keys_seen(s, std::min<int64_t>(q + kAttnBwdRows, s.q_len) - 1) + 63) / 64, i, q);
     for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows)
       f32_dq.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
     // queries that see key k: from max(0, k - (k_len - q_len)) on
@@ -235,16 +235,17 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     *out = (int32_t)c;
     return c;
   };
-  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots), ck = cut(std::move(dk.t), hkv, kAttnDkSlots);
+  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots), ck = cut(std::move(dk.t), hkv, kAttnDkSlots),
+            cq = cut(std::move(dq.t), hq, kAttnFwdSlots);
   p.n_fwd = cf.n_items, p.n_fwd_join = cf.n_join, p.fwd_slots = cf.n_slots;
+  p.n_dq = cq.n_items, p.n_dq_join = cq.n_join, p.dq_slots = cq.n_slots;
   p.n_dk = ck.n_items, p.n_dk_join = ck.n_join, p.dk_slots = ck.n_slots;
-  const std::vector<int32_t> w3 = f32.words(), wq = dq.words(), w3q = f32_dq.words(),
+  const std::vector<int32_t> w3 = f32.words(), w3q = f32_dq.words(),
                              w3k = f32_dk.words();
-  int64_t most = std::max(p.n_fwd, p.n_dk);
+  int64_t most = std::max({p.n_fwd, p.n_dk, p.n_dq});
   most = std::max(most, count(w3, 2, &p.n_f32));
   most = std::max(most, count(split_items, kAttnSplitWords, &p.n_split));
   most = std::max(most, count(join_items, kAttnSplitWords, &p.n_join));
-  most = std::max(most, count(wq, 2, &p.n_dq));
   most = std::max(most, count(w3q, 2, &p.n_f32_dq));
   most = std::max(most, count(w3k, 2, &p.n_f32_dk));
   if (8 * most * hq > INT32_MAX) return DSV_ERR_SIZE;  // workgroups of a launch
@@ -254,7 +255,8 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   L.f32_items = put(w3);
   L.split_items = put(split_items);
   L.join_items = put(join_items);
-  L.dq_items = put(wq);
+  L.dq_items = put(cq.items);
+  L.dq_join = put(cq.join);
   L.dk_items = put(ck.items);
   L.dk_join = put(ck.join);
   L.f32_dq_items = put(w3q);

@@ -29,11 +29,11 @@ constexpr int kAttnPieceKeys = 256;
 constexpr int kAttnWholeKeys = 1024;
 constexpr int kAttnSplitTarget = 256;
 
-// A forward or key tile with far more work than its share of the device (few tiles over long rows: a
+// A forward, query or key tile with far more work than its share of the device (few tiles over long rows: a
 // chunk behind a long prefix, short batches' gradients) is cut along its sum into pieces, whose fp32 sums a
 // second kernel adds.  Slots: workgroups that run at a time (two of attn_fwd per CU, one of attn_dk).  A piece is
 // not shorter than kAttnPieceSteps steps of 64 rows: below that its start and the join cost more than it saves.
-constexpr int kAttnFwdSlots = 512;
+constexpr int kAttnFwdSlots = 512;  // and of attn_dq
 constexpr int kAttnDkSlots = 256;
 constexpr int kAttnPieceSteps = 8;
 
@@ -53,7 +53,8 @@ struct AttnLayout {
   int64_t f32_items;    // [n_f32][2] {sequence, first query}: fp32 forward tiles of every sequence
   int64_t split_items;  // [n_split][kAttnSplitWords]: pieces of the split form, longest first
   int64_t join_items;   // [n_join][kAttnSplitWords]: its tiles
-  int64_t dq_items;     // [n_dq][2] {sequence, first query}: fine-tuning samples, most keys first
+  int64_t dq_items;     // [n_dq][kAttnTileWords]: fine-tuning samples, steps of 64 keys
+  int64_t dq_join;      // [n_dq_join][4]
   int64_t dk_items;     // [n_dk][kAttnTileWords]: fine-tuning samples, steps of 64 queries of one head
   int64_t dk_join;      // [n_dk_join][4]
   int64_t f32_dq_items; // the same in fp32 tiles
@@ -67,6 +68,7 @@ struct dsv_attn_plan {
   int32_t n_seqs = 0, n_q = 0, n_kv = 0, hq = 0, hkv = 0, d = 0;
   int64_t train_q = 0, train_k = 0;
   int32_t n_fwd = 0, n_fwd_join = 0, fwd_slots = 0, n_dk_join = 0, dk_slots = 0;  // *_slots: pieces with sums of their own
+  int32_t n_dq_join = 0, dq_slots = 0;
   int32_t n_f32 = 0, n_split = 0, n_join = 0, n_dq = 0, n_dk = 0, n_f32_dq = 0, n_f32_dk = 0;
   std::vector<int32_t> meta;  // packed blob, host image
   dsv::AttnLayout lay{};
