@@ -34,7 +34,7 @@ struct Tiles {
 };
 
 // Tiles in steps of equal cost, `copies` (heads) of each, on `slots` workgroups at a time: every tile whole, or cut
-// into pieces of at most `piece` steps.
+// into pieces of at most `piece` steps, no shorter than `least`, if there are fewer tiles than most_tiles.
 struct Cut {
   std::vector<int32_t> items, join;
   int32_t n_items = 0, n_join = 0, n_slots = 0;
@@ -62,7 +62,8 @@ int64_t makespan(const std::vector<int64_t>& steps, int64_t copies, int64_t piec
 }
 
 // tiles: {-steps, {sequence, first row}}
-Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t copies, int slots) {
+Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t copies, int slots, int64_t least,
+        int64_t join, int64_t most_tiles) {
   std::stable_sort(t.begin(), t.end(), [](const auto& a, const auto& b) { return a.first < b.first; });
   std::vector<int64_t> steps;
   int64_t all = 0, most = 0;
@@ -74,11 +75,11 @@ Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t 
   int64_t piece = std::max<int64_t>(most, 1);
   const int64_t share = all * copies / slots;
   // With several rounds of tiles the short ones fill what the long ones leave.
-  if ((int64_t)t.size() * copies < 4 * slots && most > share + share / 4 && most > kAttnPieceSteps) {
+  if ((int64_t)t.size() * copies < most_tiles && most > share + share / 4 && most > least) {
     int64_t best = makespan(steps, copies, piece, slots, 0);
     for (int64_t d = 2; d <= 8; ++d) {  // shares of eighths
-      const int64_t p = std::max<int64_t>(kAttnPieceSteps, share * d / 4);
-      const int64_t m = makespan(steps, copies, p, slots, 2);
+      const int64_t p = std::max<int64_t>(least, share * d / 4);
+      const int64_t m = makespan(steps, copies, p, slots, join);
       if (m < best) best = m, piece = p;
     }
   }
@@ -235,8 +236,10 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     *out = (int32_t)c;
     return c;
   };
-  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots), ck = cut(std::move(dk.t), hkv, kAttnDkSlots),
-            cq = cut(std::move(dq.t), hq, kAttnFwdSlots);
+  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots, kAttnFwdPieceSteps, 2, 4 * kAttnFwdSlots);
+  const Cut ck = cut(std::move(dk.t), hkv, kAttnDkSlots, kAttnGradPieceSteps, 3, 4 * kAttnDkSlots);
+  // Query tiles that fill the CUs run two to a CU, and the long ones faster when the short ones end: only fewer are cut.
+  const Cut cq = cut(std::move(dq.t), hq, kAttnDkSlots, kAttnGradPieceSteps, 3, kAttnDkSlots);
   p.n_fwd = cf.n_items, p.n_fwd_join = cf.n_join, p.fwd_slots = cf.n_slots;
   p.n_dq = cq.n_items, p.n_dq_join = cq.n_join, p.dq_slots = cq.n_slots;
   p.n_dk = ck.n_items, p.n_dk_join = ck.n_join, p.dk_slots = ck.n_slots;
