@@ -13,6 +13,7 @@ contiguous: columns of a q/k/v product, a cache laid out [row][head][d] or [head
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import struct
@@ -55,6 +56,12 @@ _fwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 6, _sz, _vp)(("dsv_attn_fwd", _lib))
 _bwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 10, _sz, _vp)(("dsv_attn_bwd", _lib))
 
 
+def on(stream):
+    """Where a call allocates what it was not given: on the call's stream, so that neither the memory's earlier use nor
+    its filling runs beside the call."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 class Plan:
     """The packed sequences of a batch.  device=None builds a host-only plan (inspection only)."""
 
@@ -73,7 +80,8 @@ class Plan:
         _check(_lib.dsv_attn_train_rows(self._h, rows), "dsv_attn_train_rows")
         self.train_q, self.train_k = int(rows[0]), int(rows[1])
         if device is not None:
-            self.meta = torch.empty(self.meta_bytes, dtype=torch.uint8, device=device)
+            with on(stream):
+                self.meta = torch.empty(self.meta_bytes, dtype=torch.uint8, device=device)
             _check(_lib.dsv_attn_upload(self._h, _ptr(self.meta), n, _stream_handle(stream)), "dsv_attn_upload")
 
     def __del__(self):
@@ -122,22 +130,24 @@ def _dense(t, shape, name: str):
     return t.data_ptr()
 
 
-def _ws(given, plan, like):
-    return given if given is not None else torch.empty(workspace_bytes(plan, like.dtype), dtype=torch.uint8,
-                                                       device=like.device)
+def _ws(given, plan, like, stream):
+    if given is not None:
+        return given
+    with on(stream):
+        return torch.empty(workspace_bytes(plan, like.dtype), dtype=torch.uint8, device=like.device)
 
 
 def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse: bool = True, workspace=None, stream=None):
-    """dsv_attn_fwd; returns (O, lse).  scale: 1 / sqrt(head_dim) if None.  lse is [heads_q][n_q] fp32; with
-    want_lse=False and no lse given none is written (inference)."""
+    """dsv_attn_fwd; returns (O, lse).  scale: 1 / sqrt(head_dim) if None.  lse is [heads_q][n_q] fp32; without one
+    it is made where O is made, unless want_lse=False, and else not written (inference)."""
     hq, hkv, d = plan.heads_q, plan.heads_kv, plan.head_dim
-    made = O is None
-    if made:
-        # rows that no sequence holds are not written
-        O = torch.zeros((plan.n_q, hq, d), dtype=Q.dtype, device=Q.device)
-    if lse is None and want_lse and made:
-        lse = torch.full((hq, plan.n_q), -math.inf, dtype=torch.float32, device=Q.device)
-    ws, dt = _ws(workspace, plan, Q), Q.dtype
+    if O is None:
+        with on(stream):
+            # rows that no sequence holds are not written
+            O = torch.zeros((plan.n_q, hq, d), dtype=Q.dtype, device=Q.device)
+            if lse is None and want_lse:
+                lse = torch.full((hq, plan.n_q), -math.inf, dtype=torch.float32, device=Q.device)
+    ws, dt = _ws(workspace, plan, Q, stream), Q.dtype
     _check(_fwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
                 _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
                 _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),
@@ -149,9 +159,11 @@ def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse: bool = True
 def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, workspace=None, stream=None):
     """dsv_attn_bwd; returns (dQ, dK, dV): [train_q][heads_q][d] and twice [train_k][heads_kv][d]."""
     hq, hkv, d, nq, nk = plan.heads_q, plan.heads_kv, plan.head_dim, plan.train_q, plan.train_k
-    dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)
-                  for t, n, h in ((dQ, nq, hq), (dK, nk, hkv), (dV, nk, hkv)))
-    ws, dt = _ws(workspace, plan, Q), Q.dtype
+    if dQ is None or dK is None or dV is None:
+        with on(stream):
+            dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)
+                          for t, n, h in ((dQ, nq, hq), (dK, nk, hkv), (dV, nk, hkv)))
+    ws, dt = _ws(workspace, plan, Q, stream), Q.dtype
     _check(_bwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
                 _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
                 _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 
 from . import dsv
+from .attn import on
 from .dsv import _check, _ptr, _stream_handle, torch
 
 _lib = dsv.lib_handle()
@@ -57,19 +58,26 @@ def _vec(t, n: int, dtype, name: str):
     return t.data_ptr()
 
 
-def _ws(given, like, T, K, V, grad, ldw):
-    ws = given if given is not None else torch.empty(workspace_bytes(T, K, V, like.dtype, grad, ldw), dtype=torch.uint8,
-                                                     device=like.device)
-    return ws, ws.numel() * ws.element_size()
+def _ws(given, like, T, K, V, grad, ldw, stream):
+    if given is None:
+        with on(stream):
+            given = torch.empty(workspace_bytes(T, K, V, like.dtype, grad, ldw), dtype=torch.uint8, device=like.device)
+    return given, given.numel() * given.element_size()
+
+
+def _new(given, shape, dtype, device, stream):
+    if given is not None:
+        return given
+    with on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def loss(X, W, target, loss=None, workspace=None, stream=None):
     """dsv_vocab_loss: -log softmax(X W^T)[target] of every row, fp32."""
     (T, K), V = X.shape, W.shape[0]
-    if loss is None:
-        loss = torch.empty((T,), dtype=torch.float32, device=X.device)
+    loss = _new(loss, (T,), torch.float32, X.device, stream)
     (x, ldx), (w, ldw) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W")
-    ws, n = _ws(workspace, X, T, K, V, False, ldw)
+    ws, n = _ws(workspace, X, T, K, V, False, ldw, stream)
     _check(_lib.dsv_vocab_loss(_code(X.dtype), T, K, V, x, ldx, w, ldw, _vec(target, T, torch.int32, "target"),
                                _vec(loss, T, torch.float32, "loss"), _ptr(ws), n, _stream_handle(stream)),
            "dsv_vocab_loss")
@@ -80,13 +88,11 @@ def loss_grad(X, W, target, weight=None, Wt=None, loss=None, dX=None, workspace=
     """dsv_vocab_loss_grad; returns (loss, dX).  weight [T] fp32: the upstream gradient of each row's loss (ones if
     None).  Wt [K][V]: the head transposed, kept by the caller (read for bf16 where V is a multiple of 8)."""
     (T, K), V = X.shape, W.shape[0]
-    if loss is None:
-        loss = torch.empty((T,), dtype=torch.float32, device=X.device)
-    if dX is None:
-        dX = torch.empty((T, K), dtype=X.dtype, device=X.device)
+    loss = _new(loss, (T,), torch.float32, X.device, stream)
+    dX = _new(dX, (T, K), X.dtype, X.device, stream)
     (x, ldx), (w, ldw), (dx, lddx) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W"), _mat(dX, T, K, X.dtype, "dX")
     wt, ldwt = _mat(Wt, K, V, X.dtype, "Wt") if Wt is not None else (None, 0)
-    ws, n = _ws(workspace, X, T, K, V, True, ldw)
+    ws, n = _ws(workspace, X, T, K, V, True, ldw, stream)
     _check(_lib.dsv_vocab_loss_grad(_code(X.dtype), T, K, V, x, ldx, w, ldw, wt, ldwt,
                                     _vec(target, T, torch.int32, "target"), _vec(weight, T, torch.float32, "weight"),
                                     _vec(loss, T, torch.float32, "loss"), dx, lddx, _ptr(ws), n, _stream_handle(stream)),
