@@ -3,8 +3,8 @@
 //   attn_fwd    128 queries of one head against the keys they see, one pass with the running maximum
 //               and sum of the softmax.
 //   attn_split  the (query, head) pairs of a key head of a sequence of few queries (decode) against
-//               one piece of its keys; attn_join adds the pieces.
-//   attn_dq     dQ of 128 queries (and do . o); attn_dk: dK and dV of 128 keys.
+//               one piece of its keys; attn_join adds the pieces of both forms.
+//   attn_dq     dQ of 128 queries (and do . o); attn_dk: dK and dV of 128 keys; attn_grad_join adds their pieces.
 //
 // Products are v_mfma_f32_32x32x16_bf16: lane l holds A[l % 32][8 (l / 32) + e], B[8 (l / 32) + e][l % 32]
 // (e < 8) and C[8 (v / 4) + 4 (l / 32) + v % 4][l % 32] (v < 16).  The scores are computed with the
