@@ -9,7 +9,7 @@ fine-tuning samples -- and serves every layer:
     dQ, dK, dV = attn.bwd(plan, Q, K, V, O, lse, dO)      # rows of the fine-tuning samples alone ("compact order")
 
 Query i of a sequence sees its keys j <= i + k_len - q_len.  Tensors may be any views whose head vectors are
-contiguous: columns of a q/k/v product, a cache laid out [row][head][d] or [head][row][d].
+contiguous, but not broadcast ones: columns of a q/k/v product, a cache laid out [row][head][d] or [head][row][d].
 """
 from __future__ import annotations
 
@@ -120,6 +120,9 @@ def _view(t, rows: int, heads: int, d: int, dtype, name: str) -> bytes:
     row, head, one = t.stride()
     if one != 1 and rows:
         raise ValueError("%s: the elements of a head must be contiguous" % name)
+    # the library takes a stride of 0 for the dense one
+    if (row == 0 and rows > 1) or (head == 0 and heads > 1 and rows > 0):
+        raise ValueError("%s is broadcast (a stride of 0): make it contiguous" % name)
     # a stride of a dimension of one is arbitrary: the dense one then
     return _VIEW_PACK(t.data_ptr(), row if rows > 1 else 0, head if heads > 1 and rows > 0 else 0)
 

@@ -47,6 +47,8 @@ def _mat(t, rows: int, cols: int, dtype, name: str):
         raise ValueError("%s must be [%d][%d], got %s" % (name, rows, cols, tuple(t.shape)))
     if t.numel() and cols > 1 and t.stride(1) != 1:
         raise ValueError("%s: the elements of a row must be contiguous" % name)
+    if rows > 1 and t.stride(0) == 0:  # the library takes 0 for the dense stride
+        raise ValueError("%s is broadcast (a row stride of 0): make it contiguous" % name)
     return t.data_ptr(), 0 if rows <= 1 or t.stride(0) == cols else int(t.stride(0))
 
 
