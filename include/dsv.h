@@ -656,8 +656,9 @@ int dsv_vocab_loss(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const void*
 
 /* Losses (NULL: not written) and dX.  weight NULL: ones; the losses are not
  * multiplied by it.  Wt (optional, bf16): the head transposed, the same values, for a
- * second product that reads it contraction-contiguous; used where V is a multiple of
- * 8, else, and for fp32, ignored.  Errors as dsv_vocab_loss. */
+ * second product that reads it contraction-contiguous; used where V is a multiple of 8
+ * and its rows are less than 2^22 elements apart (dense: V < 2^22), else, and for fp32,
+ * ignored.  Errors as dsv_vocab_loss. */
 int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const void* X, int32_t ldx, const void* W,
                         int32_t ldw, const void* Wt, int32_t ldwt, const int32_t* target, const float* weight,
                         float* loss, void* dX, int32_t lddx, void* workspace, size_t workspace_bytes,

@@ -567,8 +567,9 @@ extern "C" int dsv_vocab_loss_grad(dsv_dtype dt, int32_t T, int32_t K, int32_t V
   int rc = check_shape(dt, T, K, V, ldw, &a.ldw);
   if (rc == DSV_OK) rc = stride(ldx, K, &a.ldx);
   if (rc == DSV_OK) rc = stride(lddx, K, &a.lddx);
-  const bool use_t = Wt && dt == DSV_BF16 && (V & 7) == 0;
+  bool use_t = Wt && dt == DSV_BF16 && (V & 7) == 0;
   if (rc == DSV_OK && use_t) rc = stride(ldwt, V, &a.ldwt);
+  use_t = use_t && 256 * 2 * a.ldwt < (int64_t)1 << 31;  // tile_nt's offsets over a tile's 256 rows
   if (rc != DSV_OK) return rc;
   if (!aligned(W, 16) || (use_t && !aligned(Wt, 16)) || (reinterpret_cast<uintptr_t>(weight) & 3) ||
       (reinterpret_cast<uintptr_t>(loss) & 3))

@@ -88,7 +88,7 @@ def loss(X, W, target, loss=None, workspace=None, stream=None):
 
 def loss_grad(X, W, target, weight=None, Wt=None, loss=None, dX=None, workspace=None, stream=None):
     """dsv_vocab_loss_grad; returns (loss, dX).  weight [T] fp32: the upstream gradient of each row's loss (ones if
-    None).  Wt [K][V]: the head transposed, kept by the caller (read for bf16 where V is a multiple of 8)."""
+    None).  Wt [K][V]: the head transposed, kept by the caller (read for bf16 where V is a multiple of 8 below 2^22)."""
     (T, K), V = X.shape, W.shape[0]
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     dX = _new(dX, (T, K), X.dtype, X.device, stream)
