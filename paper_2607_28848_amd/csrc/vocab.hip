@@ -406,8 +406,9 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
   int64_t width = (V + r.tw - 1) / r.tw * r.tw;
   r.split = 1;
   if (grad) {
-    // 32-bit offsets of the second product's reads of W, and P within its room
-    const int64_t most = std::min(kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 30) / (size * ldw)) / r.tw * r.tw;
+    // P within its room; 32-bit offsets of the second product's reads of W and of a tile's (up to 256) rows of P
+    const int64_t most = std::min({kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 30) / (size * ldw),
+                                   (((int64_t)1 << 31) - 1) / (size * 256)}) / r.tw * r.tw;
     const int64_t n = (V + std::max<int64_t>(most, r.tw) - 1) / std::max<int64_t>(most, r.tw);
     width = ((V + n - 1) / n + r.tw - 1) / r.tw * r.tw;
   }
