@@ -596,7 +596,8 @@ int dsv_attn_workspace(const dsv_attn_plan* plan, dsv_dtype dtype, size_t* bytes
 /*
  * dsv_attn_fwd -- O, and lse [heads_q][n_q] (fp32; NULL: not written, a backward
  * needs it), of every sequence of the plan.  Q and O have n_q rows of heads_q
- * heads, K and V n_kv rows of heads_kv heads.  scale is positive and finite in fp32.
+ * heads, K and V n_kv rows of heads_kv heads.  scale is positive in fp32, and scale log2 e
+ * finite there.
  * Rows and keys that no sequence holds are not read, whatever they hold.  A key that
  * only later queries see adds 0 v to the sums of queries before it: an infinite or NaN
  * v there can reach them, as it does in softmax(masked scores) V.

@@ -988,7 +988,8 @@ int view(const dsv_attn_view* v, int64_t rows, int32_t heads, int32_t d, bool ou
 int check(const dsv_attn_plan* p, dsv_dtype dt, double scale) {
   if (!p || !p->d_meta) return DSV_ERR_ARG;
   if (dt != DSV_BF16 && dt != DSV_F32) return DSV_ERR_RANGE;
-  if (!std::isfinite(scale) || !(scale > 0) || !std::isfinite((float)scale)) return DSV_ERR_RANGE;
+  const float f = (float)scale;  // what the kernels multiply with, and in bf16 mode f log2 e
+  if (!std::isfinite(scale) || !(f > 0) || !std::isfinite(f * kLog2e)) return DSV_ERR_RANGE;
   return DSV_OK;
 }
 
