@@ -717,10 +717,14 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   const float c = a.scale * kLog2e;
   // First wave: p of 64 queries as two blocks, the terms of one beside the products of the other.  CUT: some
-  // key lies behind a query's last one.
+  // key lies behind a query's last one, or some query does not exist (its scores are 0 times the key: NaN where that is
+  // infinite).
   auto form_p = [&](auto cut, char* cur, int qt, int ln) {
     constexpr bool CUT = decltype(cut)::value;
-    constexpr int V = (CUT ? 96 : 64) * 16 / D + 1;
+    constexpr int V = (CUT ? 112 : 64) * 16 / D + 1;
+    const int first = k0 + 32 * blk + (ln & 31) - off;  // the first query that sees the lane's key
+    const int ahead = qt + 4 * (ln >> 5) - first;
+    const uint32_t seen_by = s.ql - first;
     f32x16 x[2];
     f32x4 l4[2][4];
     bf16x8 p[2][2];
@@ -736,7 +740,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const float e = __builtin_amdgcn_exp2f(x[u][v] * c - l4[u][v >> 2][v & 3]);
-        x[u][v] = !CUT || k <= qt + 32 * u + tile_row(v) + off ? e : 0.f;
+        x[u][v] = !CUT || (uint32_t)(ahead + 32 * u + 8 * (v >> 2) + (v & 3)) < seen_by ? e : 0.f;
       }
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
@@ -839,7 +843,7 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
       const int ln = begin(n, nxt);
       if (n == steps) return;
       const int qt = q_of(n);
-      if (k0 + 32 * blk + 31 > qt + off) form_p(bool_c<true>{}, cur, qt, ln);
+      if (k0 + 32 * blk + 31 > qt + off || qt + TQ > s.ql) form_p(bool_c<true>{}, cur, qt, ln);
       else form_p(bool_c<false>{}, cur, qt, ln);
     };
     for (int n = 0; n <= steps; n += 3) {
