@@ -526,8 +526,8 @@ int dsv_gemm_config(const dsv_plan* plan, dsv_dtype dtype, int32_t K, int32_t N,
  * h / (heads_q / heads_kv), over the keys j <= i + k_len - q_len (the last query
  * sees the last key):
  *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
- * A query that sees no key (i < q_len - k_len, or k_len = 0) has o = 0 and
- * lse = -infinity, and no part in any gradient.  Keys that no query of a sequence
+ * A query that sees no key (i < q_len - k_len, or k_len = 0), or none whose score is
+ * above -infinity, has o = 0 and lse = -infinity, and no part in any gradient.  Keys that no query of a sequence
  * sees are never part of a sum, whatever they hold.  Backward, with
  * p_j = exp(s_j - lse) and D = do . o:
  *     dv_j += p_j do      ds_j = scale p_j (do . v_j - D)

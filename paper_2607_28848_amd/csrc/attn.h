@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 
 namespace dsv {
@@ -37,6 +38,10 @@ struct AttnArgs {
   const int32_t* first_join;
   int32_t first_groups;
 };
+
+// What the backward subtracts from a row's scores: its lse, or infinity where that is -infinity (no key, or none of a
+// score above -infinity), so that every p of the row is 0.
+__device__ __forceinline__ float exp_from(float lse) { return lse == -INFINITY ? INFINITY : lse; }
 
 // fp32 mode: tiles of kAttnF32Rows.
 hipError_t launch_attn_f32_fwd(const AttnArgs& a, hipStream_t s);

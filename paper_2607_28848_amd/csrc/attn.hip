@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
       for (int e = 0; e < 8; ++e) dot += (float)df[i][e] * (float)of[i][e];
   }
   const float delta = pair_sum(dot);
-  const float lse2 = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] * kLog2e : 0.f;
+  const float lse2 = in ? exp_from(a.lse[(int64_t)h * a.n_q + s.q0 + q]) * kLog2e : 0.f;
   if (in && lane < 32 && k_first == 0) {
     a.delta[h * a.train_q + s.cq + q] = delta;
     a.lse2[h * a.train_q + s.cq + q] = lse2;
@@ -654,6 +654,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     if (kt + TK < k_end) step(kt + TK, b1, b0);
   }
   if (!in) return;
+  if (lse2 == INFINITY)  // 0 times an infinite key
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   if (it[5] > 1) store_sums<D>(a.part_o + (((int64_t)it[4] * a.hq + h) * kAttnBwdRows + 32 * wave + (lane & 31)) * D, acc);
   else store_cols<D>(a.dQ, (int64_t)s.cq + q, h, acc, a.scale);
 }

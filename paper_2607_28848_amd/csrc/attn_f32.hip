@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   }
   const float delta = quad_sum(dot);
   if (in && wave == 0 && lane < 16) a.delta[h * a.train_q + s.cq + q] = delta;
-  const float lse = in ? a.lse[(int64_t)h * a.n_q + s.q0 + q] : 0.f;
+  const float lse = in ? exp_from(a.lse[(int64_t)h * a.n_q + s.q0 + q]) : 0.f;
   f32x4 acc[D / 16];
   clear<D>(acc);
   const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
@@ -224,6 +224,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
     }
     add_rows<D>(kc, ds, acc);
   }
+  if (lse == INFINITY) clear<D>(acc);  // 0 times an infinite key
   spread<D>(acc, 1.f, red);
   __syncthreads();
   for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int q = qt + 4 * (lane >> 4) + v;
-      const bool seen = q < s.ql && k <= q + off;
+      const bool seen = q < s.ql && k <= q + off && lse[v] != -INFINITY;  // as exp_from(), which spills here
       p[v] = seen ? expf(x[v] * a.scale - lse[v]) : 0.f;
       ds[v] = seen ? p[v] * (dp[v] - delta[v]) * a.scale : 0.f;
     }

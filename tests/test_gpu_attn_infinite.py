@@ -18,6 +18,15 @@ def test_keys_of_minus_infinity(dtype, d, ql, kl, gone):
     run(dtype, d, ql, kl, gone)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl,gone", [(40, 40, 6), (64, 64, 1), (150, 150, 70), (131, 131, 131), (9, 9, 4), (1, 1, 1),
+                                        (200, 140, 20), (700, 700, 300)])
+def test_queries_of_no_other_keys(dtype, d, ql, kl, gone):
+    """The first queries see only such keys, and count as if they saw none."""
+    run(dtype, d, ql, kl, gone)
+
+
 def run(dtype, d, ql, kl, gone):
     from paper_2607_28848_amd import attn
     hq, hkv = 4, 2
