@@ -39,11 +39,12 @@ struct VocabArgs {
 // References.  A row starts at 0, and a tile of the first piece takes its own maximum (m, base 2) where it lies
 // further than kVocabSlack from that on either side; in later pieces where it exceeds the row's reference by
 // more.  So terms stay below 2^kVocabSlack and the row's largest far from underflow, and for all but unusual
-// logits every tile of a row has one reference: its terms need no second look.
+// logits every tile of a row has one reference: its terms need no second look.  References are whole numbers, so that
+// terms go from one to another by a power of two, which rounds nothing.
 constexpr float kVocabSlack = 60.f;
 
-__device__ __forceinline__ bool own_reference(float m, float have, bool first) {
-  return m > have + kVocabSlack || (first && m < have - kVocabSlack);
+__device__ __forceinline__ float tile_reference(float m, float have, bool first) {
+  return m > have + kVocabSlack || (first && m < have - kVocabSlack) ? ceilf(m) : have;
 }
 
 // Rows of an fp32 tile (20 rows against 20000 of 1024, with the gradient: 56 us in tiles of 32, 94 in one of 64 rows).

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
       const bool in = row < a.T;
       const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
       const float have = !a.first && in ? a.ref[row] : 0.f;
-      const float ref = own_reference(m, have, a.first) ? m : have, base = ref == -INFINITY ? 0.f : ref;
+      const float ref = tile_reference(m, have, a.first), base = ref == -INFINITY ? 0.f : ref;
       const int tc = in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
       float sum = 0.f;
 #pragma unroll
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   for (int64_t c = threadIdx.x * E; c < (int64_t)a.n_ct * a.tw; c += 256 * E) {
     const float r = st[c / a.tw].x;
     if (r == ref || r == -INFINITY) continue;
-    const float f = exp2f(r - ref);
+    const float f = ldexpf(1.f, (int)fmaxf(r - ref, -1000.f));  // both are whole numbers, ref the larger one
     u32x4 v = *reinterpret_cast<const u32x4*>(P + c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
     const bool in = row < a.T;
     const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
     const float have = !a.first && in ? a.ref[row] : 0.f;
-    ref[i] = own_reference(m, have, a.first) ? m : have;
+    ref[i] = tile_reference(m, have, a.first);
     const float base = ref[i] == -INFINITY ? 0.f : ref[i];
     const int t = in ? a.target[row] - a.v0 - n0 - c0 : -1;
     float sum = 0.f;
