@@ -62,13 +62,24 @@ def on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def int32(**named):
+    """The numbers, in order; ValueError for one that the library, which takes 32 bits of it, would see cut off."""
+    for name, x in named.items():
+        if not -(1 << 31) <= int(x) < 1 << 31:
+            raise ValueError("%s = %d does not fit 32 bits" % (name, x))
+    return [int(x) for x in named.values()]
+
+
 class Plan:
     """The packed sequences of a batch.  device=None builds a host-only plan (inspection only)."""
 
     def __init__(self, seqs, n_q: int, n_kv: int, heads_q: int, heads_kv: int, head_dim: int, device=None, stream=None):
-        self.seqs = np.ascontiguousarray(np.asarray(seqs, np.int32).reshape(-1, 5))
-        self.n_q, self.n_kv = int(n_q), int(n_kv)
-        self.heads_q, self.heads_kv, self.head_dim = int(heads_q), int(heads_kv), int(head_dim)
+        table = np.asarray(seqs).reshape(-1, 5)
+        if not np.all((table >= -(1 << 31)) & (table < 1 << 31)):
+            raise ValueError("seqs holds numbers that do not fit 32 bits")
+        self.seqs = np.ascontiguousarray(table, np.int32)
+        self.n_q, self.n_kv, self.heads_q, self.heads_kv, self.head_dim = int32(
+            n_q=n_q, n_kv=n_kv, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim)
         self._h = _vp()
         self.meta = None
         n = _sz(0)

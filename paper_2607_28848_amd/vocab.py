@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 
 from . import dsv
-from .attn import on
+from .attn import int32, on
 from .dsv import _check, _ptr, _stream_handle, torch
 
 _lib = dsv.lib_handle()
@@ -35,6 +35,7 @@ def _code(dtype) -> int:
 def workspace_bytes(T: int, K: int, V: int, dtype, grad: bool, ldw: int = 0) -> int:
     """Bytes of device workspace; ldw: the head's row stride where it is not dense."""
     n = _sz(0)
+    T, K, V, ldw = int32(T=T, K=K, V=V, ldw=ldw)
     _check(_lib.dsv_vocab_workspace(_code(dtype), T, K, V, ldw, 1 if grad else 0, ctypes.byref(n)), "dsv_vocab_workspace")
     return int(n.value)
 
@@ -49,7 +50,10 @@ def _mat(t, rows: int, cols: int, dtype, name: str):
         raise ValueError("%s: the elements of a row must be contiguous" % name)
     if rows > 1 and t.stride(0) == 0:  # the library takes 0 for the dense stride
         raise ValueError("%s is broadcast (a row stride of 0): make it contiguous" % name)
-    return t.data_ptr(), 0 if rows <= 1 or t.stride(0) == cols else int(t.stride(0))
+    ld = 0 if rows <= 1 or t.stride(0) == cols else t.stride(0)
+    if max(rows, cols, ld) >= 1 << 31:  # the library takes 32 bits of them
+        raise ValueError("%s: [%d][%d] of row stride %d does not fit 32 bits" % (name, rows, cols, ld))
+    return t.data_ptr(), ld
 
 
 def _vec(t, n: int, dtype, name: str):

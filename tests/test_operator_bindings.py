@@ -2,6 +2,7 @@
 has a host-only plan or no workspace, which the library refuses as well (DsvError): nothing is ever launched."""
 import types
 
+import numpy as np
 import pytest
 import torch
 
@@ -62,3 +63,39 @@ def test_strides_of_single_rows_and_heads_are_free():
     with pytest.raises(dsv.DsvError):
         loss(X=torch.zeros((1, 16)).as_strided((1, 16), (0, 1)), target=torch.zeros(1, dtype=torch.int32), loss=torch.zeros(1),
              dX=torch.zeros((1, 16)))
+
+
+def far(rows, cols, row):
+    return torch.empty_strided((rows, cols), (row, 1), dtype=torch.float32, device="meta")
+
+
+def test_sizes_and_strides_past_32_bits():
+    """The library takes them as 32-bit numbers: what does not fit is refused, not cut off."""
+    big = 1 << 32
+    for changed in (dict(X=far(6, 16, big + 16)), dict(W=far(8, 16, big + 16)), dict(dX=far(6, 16, big + 16)),
+                    dict(Wt=far(16, 8, big + 8)), dict(X=far(big + 6, 16, 16), dX=far(big + 6, 16, 16)),
+                    dict(W=far(big + 8, 16, 16)), dict(X=far(6, big + 16, big + 16), W=far(8, big + 16, big + 16),
+                                                       dX=far(6, big + 16, big + 16))):
+        with pytest.raises(ValueError):
+            loss(**changed)
+    for sizes in ((big + 6, 16, 8), (6, big + 16, 8), (6, 16, big + 8)):
+        with pytest.raises(ValueError):
+            vocab.workspace_bytes(*sizes, torch.float32, grad=True)
+    with pytest.raises(ValueError):
+        vocab.workspace_bytes(6, 16, 8, torch.float32, grad=True, ldw=big + 16)
+
+
+def test_plans_past_32_bits():
+    big = 1 << 32
+    good = dict(seqs=[(0, 10, 0, 12, 1)], n_q=10, n_kv=12, heads_q=4, heads_kv=2, head_dim=64)
+    attn.Plan(**good)
+    attn.Plan(**dict(good, seqs=np.asarray(good["seqs"], np.int64)))
+    for name, x in (("n_q", 10), ("n_kv", 12), ("heads_q", 4), ("heads_kv", 2), ("head_dim", 64)):
+        with pytest.raises(ValueError):
+            attn.Plan(**dict(good, **{name: big + x}))
+    for i in range(5):
+        for kind in (np.int64, np.uint32, float):
+            s = np.asarray(good["seqs"], kind)
+            s[0, i] += 1 << 31 if kind is np.uint32 else big
+            with pytest.raises(ValueError):
+                attn.Plan(**dict(good, seqs=s))
