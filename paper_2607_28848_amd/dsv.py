@@ -194,6 +194,8 @@ def _ld(t, row_len: int) -> int:
         return 0
     if t.dim() != 2 or t.shape[1] != row_len or t.stride(1) != 1:
         raise ValueError("a strided operand must be 2-D with contiguous rows of %d elements" % row_len)
+    if t.stride(0) == 0:  # the library takes 0 for the dense stride
+        raise ValueError("a broadcast operand (a row stride of 0): make it contiguous")
     return int(t.stride(0))
 
 

@@ -99,3 +99,20 @@ def test_plans_past_32_bits():
             s[0, i] += 1 << 31 if kind is np.uint32 else big
             with pytest.raises(ValueError):
                 attn.Plan(**dict(good, seqs=s))
+
+
+def test_broadcast_rows_of_the_grouped_linear_calls():
+    p = dsv.segments_build([(0, 6, 0, 1)], 6, [8], [1.0], 8)
+    t = dict(X=torch.zeros((6, 64)), W=torch.zeros((32, 64)), A=torch.zeros((1, 8, 64)), B=torch.zeros((1, 32, 8)))
+    fwd = dict(t, Y=torch.zeros((6, 32)))
+    bwd = dict(t, H=torch.zeros((6, 8)), dY=torch.zeros((6, 32)))
+    with pytest.raises(dsv.DsvError):
+        dsv.cobatch_fwd_grouped(p, [tuple(fwd.values())], **NONE)
+    with pytest.raises(dsv.DsvError):
+        dsv.lora_bwd_grouped(p, [tuple(bwd.values())], **NONE)
+    for call, args, names in ((dsv.cobatch_fwd_grouped, fwd, ("X", "W", "Y")), (dsv.lora_bwd_grouped, bwd, ("X", "W", "dY"))):
+        for name in names:
+            rows, cols = args[name].shape
+            bad = dict(args, **{name: torch.zeros((1, cols)).expand(rows, cols)})
+            with pytest.raises(ValueError):
+                call(p, [tuple(bad.values())], **NONE)
