@@ -151,15 +151,18 @@ def _ws(given, plan, like, stream):
         return torch.empty(workspace_bytes(plan, like.dtype), dtype=torch.uint8, device=like.device)
 
 
-def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse: bool = True, workspace=None, stream=None):
-    """dsv_attn_fwd; returns (O, lse).  scale: 1 / sqrt(head_dim) if None.  lse is [heads_q][n_q] fp32; without one
-    it is made where O is made, unless want_lse=False, and else not written (inference)."""
+def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse=None, workspace=None, stream=None):
+    """dsv_attn_fwd; returns (O, lse).  scale: 1 / sqrt(head_dim) if None.  lse is [heads_q][n_q] fp32, which a backward
+    needs; without one it is made if want_lse, which stands for "where O is made" if None, else it is not written and
+    None is returned for it (inference)."""
     hq, hkv, d = plan.heads_q, plan.heads_kv, plan.head_dim
-    if O is None:
+    make_lse = lse is None and (O is None if want_lse is None else want_lse)
+    if O is None or make_lse:
         with on(stream):
             # rows that no sequence holds are not written
-            O = torch.zeros((plan.n_q, hq, d), dtype=Q.dtype, device=Q.device)
-            if lse is None and want_lse:
+            if O is None:
+                O = torch.zeros((plan.n_q, hq, d), dtype=Q.dtype, device=Q.device)
+            if make_lse:
                 lse = torch.full((hq, plan.n_q), -math.inf, dtype=torch.float32, device=Q.device)
     ws, dt = _ws(workspace, plan, Q, stream), Q.dtype
     _check(_fwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
@@ -171,8 +174,11 @@ def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse: bool = True
 
 
 def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, workspace=None, stream=None):
-    """dsv_attn_bwd; returns (dQ, dK, dV): [train_q][heads_q][d] and twice [train_k][heads_kv][d]."""
+    """dsv_attn_bwd; returns (dQ, dK, dV): [train_q][heads_q][d] and twice [train_k][heads_kv][d].  lse: the forward's
+    (None only where the plan has no fine-tuning rows)."""
     hq, hkv, d, nq, nk = plan.heads_q, plan.heads_kv, plan.head_dim, plan.train_q, plan.train_k
+    if lse is None and nq > 0:
+        raise ValueError("lse is None: the forward returns it with lse=... or want_lse=True")
     if dQ is None or dK is None or dV is None:
         with on(stream):
             dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)
@@ -181,7 +187,7 @@ def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, 
     _check(_bwd(plan.handle, _code(dt), 1 / math.sqrt(d) if scale is None else scale,
                 _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
                 _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),
-                _dense(lse, (hq, plan.n_q), "lse"), _view(dO, nq, hq, d, dt, "dO"), _view(dQ, nq, hq, d, dt, "dQ"),
-                _view(dK, nk, hkv, d, dt, "dK"), _view(dV, nk, hkv, d, dt, "dV"), ws.data_ptr(), ws.nbytes,
+                None if lse is None else _dense(lse, (hq, plan.n_q), "lse"), _view(dO, nq, hq, d, dt, "dO"),
+                _view(dQ, nq, hq, d, dt, "dQ"), _view(dK, nk, hkv, d, dt, "dK"), _view(dV, nk, hkv, d, dt, "dV"), ws.data_ptr(), ws.nbytes,
                 _stream_handle(stream)), "dsv_attn_bwd")
     return dQ, dK, dV

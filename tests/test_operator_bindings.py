@@ -1,5 +1,6 @@
 """What the bindings of attention and the vocabulary loss refuse before the library is called (CPU only).  Each call
 has a host-only plan or no workspace, which the library refuses as well (DsvError): nothing is ever launched."""
+import contextlib
 import types
 
 import numpy as np
@@ -116,3 +117,36 @@ def test_broadcast_rows_of_the_grouped_linear_calls():
             bad = dict(args, **{name: torch.zeros((1, cols)).expand(rows, cols)})
             with pytest.raises(ValueError):
                 call(p, [tuple(bad.values())], **NONE)
+
+
+def test_backward_without_the_forwards_lse():
+    """Refused by name where the plan has fine-tuning samples, else a no-op as in the library, which reads none then."""
+    with pytest.raises(ValueError, match="lse"):
+        attention(True, lse=None)
+    p = attn.Plan([(0, 10, 0, 12, 0)], 10, 12, 4, 2, 64)
+    q, k, none = torch.zeros((10, 4, 64)), torch.zeros((12, 2, 64)), torch.zeros((0, 4, 64))
+    with pytest.raises(dsv.DsvError):  # it reaches the library: the plan is on the host
+        attn.bwd(p, q, k, k, q, None, none, **NONE)
+
+
+def test_lse_is_made_where_it_is_wanted():
+    """As shown by where the call would make it: on a device of its own making, here the host."""
+    made = []
+    p = attn.Plan([(0, 10, 0, 12, 1)], 10, 12, 4, 2, 64)
+    full = torch.full
+
+    def record(*a, **kw):
+        made.append(a[0])
+        return full(*a, **kw)
+
+    q, k = torch.zeros((10, 4, 64)), torch.zeros((12, 2, 64))
+    lse = torch.zeros((4, 10))
+    for kw, n in ((dict(), 1), (dict(O=q), 0), (dict(O=q, want_lse=True), 1), (dict(want_lse=True), 1), (dict(want_lse=False), 0),
+                  (dict(O=q, want_lse=False), 0), (dict(lse=lse), 0), (dict(O=q, lse=lse, want_lse=True), 0)):
+        made.clear()
+        with pytest.MonkeyPatch.context() as m:
+            m.setattr(torch, "full", record)
+            m.setattr(attn, "on", lambda stream: contextlib.nullcontext())
+            with pytest.raises(dsv.DsvError):
+                attn.fwd(p, q, k, k, **kw, **NONE)
+        assert made == [(4, 10)] * n, kw
