@@ -108,7 +108,7 @@ class MixedStep:
         X, Q, O, lse, H = saved
         target = self.target[self.train]
         weight = (target >= 0).float()
-        weight /= weight.sum()
+        weight /= weight.sum().clamp(min=1)  # samples of one row have no target
         loss, dZ = vocab.loss_grad(hidden[self.train], self.head, target, weight=weight, Wt=self.head_t)
         grads = {}
         grads["o"] = dsv.lora_bwd(self.plan, O.flatten(1), self.W["o"], self.A["o"], self.B["o"], H["o"], dZ)
