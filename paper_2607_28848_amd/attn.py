@@ -188,6 +188,6 @@ def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, 
                 _view(Q, plan.n_q, hq, d, dt, "Q"), _view(K, plan.n_kv, hkv, d, dt, "K"),
                 _view(V, plan.n_kv, hkv, d, dt, "V"), _view(O, plan.n_q, hq, d, dt, "O"),
                 None if lse is None else _dense(lse, (hq, plan.n_q), "lse"), _view(dO, nq, hq, d, dt, "dO"),
-                _view(dQ, nq, hq, d, dt, "dQ"), _view(dK, nk, hkv, d, dt, "dK"), _view(dV, nk, hkv, d, dt, "dV"), ws.data_ptr(), ws.nbytes,
-                _stream_handle(stream)), "dsv_attn_bwd")
+                _view(dQ, nq, hq, d, dt, "dQ"), _view(dK, nk, hkv, d, dt, "dK"), _view(dV, nk, hkv, d, dt, "dV"),
+                ws.data_ptr(), ws.nbytes, _stream_handle(stream)), "dsv_attn_bwd")
     return dQ, dK, dV
