@@ -628,7 +628,9 @@ int dsv_attn_bwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const
  *     loss = log sum_v exp z_v - z_t
  *     dx   = weight (sum_v softmax(z)_v W_v - W_t)
  * A target outside [0, V) marks a row without one (a prompt's token): its loss is 0 and
- * its dx zeros, whatever the row holds.  The logits are never held whole: the
+ * its dx zeros, whatever the row holds.  A logit of -infinity drops out; where it comes
+ * from an infinite element of its head row, that element of every dx is 0 times it, NaN,
+ * as in softmax(z) W.  The logits are never held whole: the
  * vocabulary is taken in pieces, whose exponentials, relative to a reference that a
  * row carries from piece to piece, are at once summed and multiplied with the
  * head again.  The target's own term is kept apart in fp32, so a loss near 0 and its
