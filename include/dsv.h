@@ -527,14 +527,15 @@ int dsv_gemm_config(const dsv_plan* plan, dsv_dtype dtype, int32_t K, int32_t N,
  * sees the last key):
  *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
  * A query that sees no key (i < q_len - k_len, or k_len = 0), or none whose score is
- * above -infinity, has o = 0 and lse = -infinity, and no part in any gradient.  Keys that no query of a sequence
- * sees are never part of a sum, whatever they hold.  Backward, with
+ * above -infinity, has o = 0 and lse = -infinity, and no part in any gradient.  Keys that
+ * no query of a sequence sees are never part of a sum, whatever they hold.  Backward, with
  * p_j = exp(s_j - lse) and D = do . o:
  *     dv_j += p_j do      ds_j = scale p_j (do . v_j - D)
  *     dq = sum_j ds_j k_j     dk_j += ds_j q     (sums over the key head's query heads)
  *
- * Scores, softmax statistics and sums are fp32 in both types; in bf16 mode the
- * products run on bf16 operands, for which p and ds are rounded to bf16 once, and
+ * Scores, softmax statistics and sums are fp32 in both types.  In bf16 mode the
+ * products run on bf16 operands: p and ds are rounded to bf16 (8 bits) for them, once,
+ * but the ds of dk is formed from a p that was rounded to 10 bits before.  In both types
  * every output is rounded once.  No atomics: repeated calls give the same bits.
  */
 
@@ -612,8 +613,9 @@ int dsv_attn_fwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const
 /*
  * dsv_attn_bwd -- dQ, dK and dV of the fine-tuning samples (compact rows) from
  * the forward's Q, K, V, O and lse and the upstream gradient dO (compact rows).
- * Where samples share key rows, dK and dV hold each sample's own part.  Without
- * fine-tuning samples the call is a no-op.  Errors as dsv_attn_fwd.
+ * Where samples share key rows, dK and dV hold each sample's own part.  As in the
+ * forward, an infinite or NaN value of a row that the mask parts from another can reach
+ * its gradients as 0 times it.  Without fine-tuning samples the call is a no-op.  Errors as dsv_attn_fwd.
  */
 int dsv_attn_bwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const dsv_attn_view* Q,
                  const dsv_attn_view* K, const dsv_attn_view* V, const dsv_attn_view* O, const float* lse,
@@ -630,11 +632,11 @@ int dsv_attn_bwd(const dsv_attn_plan* plan, dsv_dtype dtype, double scale, const
  * A target outside [0, V) marks a row without one (a prompt's token): its loss is 0 and
  * its dx zeros, whatever the row holds.  A logit of -infinity drops out; where it comes
  * from an infinite element of its head row, that element of every dx is 0 times it, NaN,
- * as in softmax(z) W.  The logits are never held whole: the
- * vocabulary is taken in pieces, whose exponentials, relative to a reference that a
- * row carries from piece to piece, are at once summed and multiplied with the
- * head again.  The target's own term is kept apart in fp32, so a loss near 0 and its
- * gradient keep their relative accuracy.
+ * as in softmax(z) W.  The logits are never held whole: the vocabulary is taken in pieces,
+ * whose exponentials, relative to a reference that a row carries from piece to piece, are
+ * at once summed and multiplied with the head again.  The target's own term is kept apart
+ * and, like the row's loss, formed in 64 bits, so a loss near 0 and its gradient keep
+ * their relative accuracy.
  * In bf16 mode the products run on bf16 operands with fp32 sums, the exponentials
  * being rounded to bf16 once for the second one; losses are fp32 in both types.  No
  * atomics: repeated calls give the same bits.

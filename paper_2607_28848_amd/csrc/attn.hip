@@ -13,6 +13,10 @@
 // slot (l / 32, e) stands for row 16 t + 8 (e / 4) + 4 (l / 32) + e % 4, and the other operand is read in that
 // order (two transposing LDS reads of four rows each).  No value crosses lanes but for a query's maximum and
 // sum, which two lanes share.
+//
+// p and ds are rounded to bf16 for the second product because an fp32 one takes 16 times as long on the matrix core.
+// Against 64 bits the outputs are then off by 0.21 to 0.27% in the root mean square, where fp32 products of the same
+// operands, rounded once at the end, leave 0.16 to 0.20%.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -267,8 +271,8 @@ __device__ __forceinline__ void store_sums(float* p, const f32x16 (&acc)[D / 32]
 // A wave's products read a fragment of K or V from LDS for each matrix instruction, 1 KiB in the 32 cycles that one
 // takes: all of a CU's LDS bandwidth with four waves at it, so two workgroups share a CU and one's softmax runs beside
 // the other's products.  With heads of 64 the exponentials (one for 256 operations, a quarter of the vector rate) take
-// as long as the products.  16384 queries, 32 heads of 128 on 8: 1.95 ms (1130 TFLOP/s; a large bf16 product reaches
-// 1290 on the same card).  Nine prompts of about 700, 24 heads of 64 on 4: 36 us (560 TFLOP/s).
+// as long as the products.  16384 queries, 32 heads of 128 on 8: 1.90 ms (1155 TFLOP/s; a large bf16 product reaches
+// 1290 on the same card).  Nine prompts of about 700, 24 heads of 64 on 4: 36 us (570 TFLOP/s).
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 // r / group and head r % group.  Each wave takes every fourth block of 32 keys through buffers of its
 // own (no barrier until the end), then the four waves' sums are added.  Every key is read once for all of
 // its head's queries: the stream of K and V is what bounds it where there are many keys (64 sequences of about 2600,
-// 8 heads of 128: 577 MB in 104 us, 5.5 TB/s), and the loads' latency one after the other where there are few (8 of
+// 8 heads of 128: 577 MB in 105 us, 5.5 TB/s), and the loads' latency one after the other where there are few (8 of
 // about 400: 10 us for 12 MB).
 template <int D>
 __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
@@ -523,7 +527,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
 }
 
 // Both forms' pieces in one launch: 32 rows a workgroup, row tid / 8, D / 8 columns each; forward tiles first.
-// The launch and two reads one after the other: 4.8 us for 512 tiles of the split form, 7.9 for 48 sequences' beside
+// The launch and two reads one after the other: 4.9 us for 512 tiles of the split form, 8.0 for 48 sequences' beside
 // 96 forward tiles in five pieces (two launches: 12.2).
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
@@ -550,7 +554,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dQ of 128 queries of one head over the keys they see, 32 queries a wave, 64 keys a step, in three products: the scores
 // again (p = 2^(c s - lse) needs no maximum), dO V^T, and ds K.  It also leaves delta = do . o and the base-2 lse of its
 // rows for attn_dk, which runs after it.  Bound as attn_fwd is (three fragments of LDS for three matrix instructions),
-// matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.47 ms (412 GFLOP, 880 TFLOP/s).
+// matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.45 ms (412 GFLOP, 920 TFLOP/s).
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -674,7 +678,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // Four products of 2 D operations a score (attn_dq: three), because dQ's sums run along the other axis and would need
 // atomics here.  The matrix core is 45% busy: 64 queries against 128 keys read 272 KB of LDS, 2200 cycles beside 2048 of
 // products, and two waves a SIMD overlap them in part.  Four samples of 2048, 64 heads of 128 on
-// 8: 0.70 to 0.74 ms (550 GFLOP, 750 TFLOP/s); two of 1024, 32 heads on 8: 66 us and 8 for the join.
+// 8: 0.65 ms (550 GFLOP, 845 TFLOP/s); two of 1024, 32 heads on 8: 72 us and 8 for the join.
 template <int D>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;

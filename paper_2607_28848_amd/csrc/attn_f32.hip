@@ -11,8 +11,8 @@
 // batches of this mode are small, and what bounds them is the number of tiles that one wave walks one after the other,
 // each with its loads' time in front.  Rows are read through descriptors, whose lanes need no pointers and no
 // predicates of their own (with pointers the dK kernel of heads of 128 kept 215 registers in memory: 157 us against 58).
-// Two samples of 96 and three of 157 rows, 8 heads on 2 of 64: forward 7.8 us, dQ 8.4, dK and dV 10.6, their join 3.6
-// (four waves on 64 rows with staged tiles: 135 in all).  Two of 200 and three of 300, 16 on 2 of 128: 40, 47, 58, 5.
+// Two samples of 96 and three of 157 rows, 8 heads on 2 of 64: forward 7.7 us, dQ 9.7, dK and dV 10.3, their join 4.0
+// (four waves on 64 rows with staged tiles: 135 in all).  Two of 200 and three of 300, 16 on 2 of 128: 39, 46, 57, 5.
 #include <hip/hip_runtime.h>
 
 #include "attn.h"
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
 
 // dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
 // heads (so the sums over them need no atomics), or of one of a.parts ranges of them, whose sums go to the workspace
-// (32 us whole, 10.6 and 3.6 for the join in four parts: the first batch above).
+// (32 us whole, 10.3 and 4.0 for the join in four parts: the first batch above).
 template <int D>
 __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
   constexpr int NW = 8;

@@ -17,14 +17,21 @@ constexpr int kAttnFwdRows = 128;
 constexpr int kAttnBwdRows = 128;
 constexpr int kAttnF32Rows = 16;
 // A sequence of up to kAttnSplitQ queries takes the split form: the (query, head) pairs of a
-// key head form rows, kAttnPackRows to a tile, and the keys are split into pieces.
+// key head form rows, kAttnPackRows to a tile, and the keys are split into pieces.  Heads of 128, split form and tiles:
+// 16 queries behind 5000 keys, 32 heads on 8, 14.1 us and 22.4; 20 14.3 and 23.0; 64 18.5 and 26.6.  16 sequences of
+// 16 or 20 queries behind 600 keys, 11.6 and 21.1 or 18.9 and 21.0; of 40, 27.9 and 21.8.  16 prompts of 16 tokens, 6.5
+// and 5.9; of 20, 9.5 and 6.6.  So one limit on the queries is ahead up to 16 but for short prompts, and one sequence
+// behind a long prefix would gain from a higher one.
 constexpr int kAttnSplitQ = 16;
 constexpr int kAttnPackRows = 32;
 // Pieces of the split form: multiples of kAttnPieceKeys keys (each of the workgroup's four waves takes blocks of
 // 32 of them by turns), of a length that makes about as many as run at a time (one workgroup per CU with heads of
 // 128, two with 64; 64 sequences of 2600 keys: 104 us in 536 pieces, 114 in 1144).  Where no sequence has more than
-// kAttnWholeKeys keys each is one piece: the join's launch costs more than the shorter walk saves
-// (8 sequences of 400 keys: 12.4 us in pieces of 128, 10.9 whole).
+// kAttnWholeKeys keys each is one piece: the join's launch costs more than the shorter walk saves.
+// In pieces of 256 and whole, 8 sequences on 8 key heads of 128: 300 keys, 9.6 us and 7.5; 600 keys, 9.9 and 9.6; 1000 keys,
+// 10.6 and 12.9; 1500 keys, 15.8 and 17.7 (1 or 2 sequences: 10 us in pieces of any of these; whole 7.4, 9.5, 12.3, 16;
+// 32 sequences: the same either way from 600 keys on).  So the two cross between 600 and 1000 keys, and the limit lies
+// above that by up to 2.5 us.
 constexpr int kAttnPieceKeys = 256;
 constexpr int kAttnWholeKeys = 1024;
 constexpr int kAttnSplitTarget = 256;

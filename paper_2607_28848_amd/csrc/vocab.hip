@@ -8,7 +8,8 @@
 // So the logits are computed once: 4 T K V operations where recomputing them would take 6.  A piece is as wide as P's
 // room (kPieceBytes) allows, so that what one kernel writes of it the next one finds in the last-level cache.
 // 256 rows against 128256 of 4096, with the head transposed at hand: 0.57 ms, 0.42 at the rate of a large product on
-// this card (1290 TFLOP/s); 4096 rows against 128256 of 8192: 13.3 ms (1290 TFLOP/s).
+// this card (1290 TFLOP/s); 4096 rows against 128256 of 8192: 13.1 ms (1320 TFLOP/s).  The exponentials are rounded to
+// bf16 for the second product; dX is off from 64 bits by 0.17% in the root mean square either way: its own rounding.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,8 +36,8 @@ __device__ __forceinline__ float quad_sum(float x) {
 
 // ---- logits -------------------------------------------------------------------------------------------
 // GRAD: P is written.  Tiles of 32 FM rows and 32 FN columns; NB: buffers (2: tile_nt, else tile_ring).  Up to 128 rows
-// the stream of a large head is what bounds it: one row against 128256 of 4096 takes 180 us, 5.8 TB/s, 128 rows 195.
-// Else the matrix core: 4096 rows, 32256 x 8192 a piece, 1.62 ms (1330 TFLOP/s).
+// the stream of a large head is what bounds it: one row against 128256 of 4096 takes 185 us with the fold, 5.7 TB/s, 128 rows 206.
+// Else the matrix core: 4096 rows, 32256 x 8192 a piece, 1.61 ms (1340 TFLOP/s).
 template <bool GRAD, int FM, int FN, int NB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 ? 1 : 2))) void vocab_logits_kernel(VocabArgs a) {
   constexpr int WM = 16 * FM, TM = 2 * WM, WN = 16 * FN, TN = 2 * WN;
@@ -152,9 +153,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
 
 // ---- second product -------------------------------------------------------------------------------------
 // Range `part` of the piece's contraction: O[part] = alpha O[part] + P W (O[part] = P W for the first piece).  Matrix
-// core: 4096 rows, 32256 x 8192 a piece, 1.55 to 1.62 ms (1340 TFLOP/s).  With few tiles the contraction is cut into
+// core: 4096 rows, 32256 x 8192 a piece, 1.59 ms (1360 TFLOP/s).  With few tiles the contraction is cut into
 // ranges with sums of their own, which vocab_finish adds (256 rows of 4096, 128256 columns: 16 tiles in 16 ranges,
-// 0.29 ms).
+// 0.28 ms).
 template <bool NN, int FM>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void vocab_grad_kernel(VocabArgs a) {
   constexpr int WM = 16 * FM, TM = 2 * WM;

@@ -4,9 +4,9 @@
 // contraction values through three LDS buffers that global memory is loaded straight into.  A step's order of
 // contraction values is free: slot l / 16 of instruction e stands for value 16 s + 4 (l / 16) + e, so a lane's
 // values of a row of P (and of Q, NT) are a 16-byte chunk.  The loads of a step have two steps' time to arrive, and one
-// barrier a step: 600 rows against 20000 of 1024, losses 264 us, with the gradient 487 (101 TFLOP/s; a large fp32 product
+// barrier a step: 600 rows against 20000 of 1024, losses 250 us, with the gradient 478 (103 TFLOP/s; a large fp32 product
 // reaches 132; 64 x 64 tiles staged through registers, two barriers a step: 290 and 571).  333 rows against 5003 of 512:
-// 26 us and 24 for the products, 59 in all: two waves a SIMD for 16 steps, and the tiles' start and end.
+// 25 us and 23 for the products, 52 a pass: two waves a SIMD for 16 steps, and the tiles' start and end.
 #include <hip/hip_runtime.h>
 
 #include "device_common.h"
