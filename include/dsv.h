@@ -517,6 +517,79 @@ int dsv_gemm_config(const dsv_plan* plan, dsv_dtype dtype, int32_t K, int32_t N,
                     int32_t out[6]);
 
 /*
+ * Norms of queries and keys for each head and the position rotation, in one pass: what
+ * stands between the q/k/v products and the attention.  For a head's vector x of a row
+ * at position p, with weight w (no norm without one) and d = head_dim:
+ *     u = x w / sqrt(mean(x^2) + eps)
+ *     y_a = u_a cos t - u_b sin t,  y_b = u_b cos t + u_a sin t,  t = p freq[i]
+ * for the pairs (a, b) = (i, i + rotated / 2), or (2 i, 2 i + 1) where interleaved, of
+ * i < rotated / 2; the elements from `rotated` on keep u.  Angles are reduced in 64 bits,
+ * so far positions turn as exactly as near ones; norms and rotations are fp32, every
+ * output is rounded once.  Backward, with g the upstream gradient turned back:
+ *     dw += g x / sqrt(mean(x^2) + eps)          (over rows and heads)
+ *     dx = (g w - x mean(g w x) / (mean(x^2) + eps)) / sqrt(mean(x^2) + eps)
+ * No atomics: repeated calls give the same bits.  The norm squares in fp32: a vector
+ * whose mean square exceeds fp32 (elements beyond about 10^19) is not normalised rightly.
+ */
+typedef struct {
+  int32_t n;                   /* rows of Q, K, V and pos */
+  int32_t heads_q, heads_kv;   /* 0 to 1024 each, not both 0 (0: its tensors are not looked at) */
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t rotated;             /* elements of a head that turn: a multiple of 16, 0 to head_dim */
+  int32_t interleaved;         /* 0 or 1 */
+  double eps;                  /* a normal positive fp32 number; looked at where there is a weight */
+  const int32_t* pos;          /* [n] any number; not read where rotated is 0 */
+  const double* freq;          /* [rotated / 2] radians a position, 8-byte aligned */
+  const float* q_weight;       /* [head_dim], 16-byte aligned, or NULL: queries are not normalised */
+  const float* k_weight;       /* the same for keys */
+} dsv_rope;
+
+/* A tensor [rows][heads][head_dim]: element (t, h, c) at ptr[t * row + h * head + c].
+ * Strides in elements, multiples of 8 and at least head_dim, row at most 2^23, head at
+ * most 2^40; 0 stands for the dense one (row: heads * head_dim, head: head_dim).  ptr
+ * is 16-byte aligned.  So q, k and v may be columns of one product's rows, and a cache
+ * may be [row][head][d] or [head][row][d].  The vectors of an output must not overlap
+ * (DSV_ERR_SIZE), nor an output and another tensor of the call (not checked). */
+typedef struct {
+  void* ptr;
+  int64_t row;
+  int64_t head;
+} dsv_attn_view;
+
+/*
+ * dsv_rope_fwd -- Q_out (n rows) and K_out from Q and K (n rows), and, given V, its rows
+ * as they are in V_out.  slots [n] (with n_slots, the rows of K_out and V_out): row i of
+ * K and V goes to row slots[i]; a row whose slot is outside [0, n_slots) is left out, and
+ * slots that no row names stay as they are.  Two rows of one slot: either's elements.
+ * slots NULL: row i to row i, n_slots not looked at.  V and V_out NULL: none.
+ * Q_out may be Q itself, the same address and strides; without slots K_out may be K.
+ * Errors: DSV_ERR_ARG (null or misaligned pointer, negative count), DSV_ERR_RANGE (dtype,
+ * heads, head_dim, rotated, flag, eps), DSV_ERR_SIZE (strides, overlapping outputs, more
+ * than 2^31 - 1 work items).
+ */
+int dsv_rope_fwd(dsv_dtype dtype, const dsv_rope* rope, const dsv_attn_view* Q, const dsv_attn_view* K,
+                 const dsv_attn_view* V, const int32_t* slots, int32_t n_slots, const dsv_attn_view* Q_out,
+                 const dsv_attn_view* K_out, const dsv_attn_view* V_out, void* hip_stream);
+
+/* Device workspace of dsv_rope_bwd for n_rows gradient rows (256-byte aligned there). */
+int dsv_rope_workspace(const dsv_rope* rope, int32_t n_rows, size_t* bytes);
+
+/*
+ * dsv_rope_bwd -- dQ_out and dK_out, the gradients of Q and K, from dQ and dK, those of
+ * Q_out and K_out, for n_rows rows (the fine-tuning rows in compact order, as the
+ * attention's backward leaves them): gradient row i belongs to row rows[i] of Q, K and
+ * pos, or to row i (rows NULL, n_rows <= n).  A row outside [0, n) gets zeros.
+ * Q and K are the forward's inputs, looked at only where the head is normalised.
+ * dq_weight, dk_weight [head_dim] fp32, 16-byte aligned: overwritten with the weights'
+ * gradients over these rows; NULL: not computed; refused without the weight.  dQ_out
+ * may be dQ itself, dK_out dK.  Errors as dsv_rope_fwd, and DSV_ERR_SIZE for the workspace.
+ */
+int dsv_rope_bwd(dsv_dtype dtype, const dsv_rope* rope, int32_t n_rows, const int32_t* rows, const dsv_attn_view* dQ,
+                 const dsv_attn_view* dK, const dsv_attn_view* Q, const dsv_attn_view* K, const dsv_attn_view* dQ_out,
+                 const dsv_attn_view* dK_out, float* dq_weight, float* dk_weight, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
+
+/*
  * Attention of a mixed batch (softmax(scale Q K^T) V, causal, grouped heads): the
  * operator between the q/k/v and the o projections.  One call serves whole
  * prompts, chunks behind a cached prefix, single decode tokens over long caches
@@ -577,18 +650,6 @@ int dsv_attn_upload(dsv_attn_plan* plan, void* d_meta, size_t meta_bytes, void* 
 int dsv_attn_train_rows(const dsv_attn_plan* plan, int64_t out[2]);
 /* Releases the plan (NULL is a no-op); waits for its upload like dsv_plan_free. */
 void dsv_attn_free(dsv_attn_plan* plan);
-
-/* A tensor [rows][heads][head_dim]: element (t, h, c) at ptr[t * row + h * head + c].
- * Strides in elements, multiples of 8 and at least head_dim, row at most 2^23, head at
- * most 2^40; 0 stands for the dense one (row: heads * head_dim, head: head_dim).  ptr
- * is 16-byte aligned.  So q, k and v may be columns of one product's rows, and a cache
- * may be [row][head][d] or [head][row][d].  The vectors of an output must not overlap
- * (DSV_ERR_SIZE), nor an output and another tensor of the call (not checked). */
-typedef struct {
-  void* ptr;
-  int64_t row;
-  int64_t head;
-} dsv_attn_view;
 
 /* Device workspace that dsv_attn_fwd and dsv_attn_bwd need for this plan (one
  * buffer may serve both; 256-byte aligned). */

@@ -62,6 +62,25 @@ def on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def here(*tensors):
+    """ValueError unless the tensors (None: not given) are on one device, the current one where it is a GPU: a call's
+    kernels run there."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError("the tensors of a call are on several devices: %s" % sorted(map(str, devices)))
+    for d in devices:
+        if d.type == "cuda" and d.index != torch.cuda.current_device():
+            raise ValueError("the tensors are on %s, the current device is cuda:%d" % (d, torch.cuda.current_device()))
+
+
+def made(given, shape, dtype, like, stream):
+    """The tensor given, else one made as the call's stream needs it."""
+    if given is not None:
+        return given
+    with on(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def int32(**named):
     """The numbers, in order; ValueError for one that the library, which takes 32 bits of it, would see cut off."""
     for name, x in named.items():

@@ -1,0 +1,464 @@
+// rope.hip -- norms of queries and keys and the position rotation, forward and backward (gfx950), and the C entry points.
+//
+// A head's vector is held by D / 16 lanes, 16 elements each, as two chunks of 8 (16 or 32 bytes a load): lane l has
+// chunks l and l + rotated / 16, or 2 l and 2 l + 1 where neighbours turn together, so both elements of a pair lie in
+// one lane and in both orders the lane's pairs are i = 8 l .. 8 l + 7.  A wave takes 64 / (D / 16) heads of one row at a
+// time.  The row's cosines and sines are formed once a wave, one angle a lane, and go to the lanes through LDS.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "device_common.h"
+#include "view.h"
+
+namespace dsv {
+namespace {
+
+struct RopeArgs {
+  int32_t n;            // rows of the forward's tensors
+  int32_t hq, hkv, hv;  // hv: heads of V that are copied (0: none)
+  int32_t rot;
+  int32_t split;        // waves a row
+  float eps;
+  const int32_t* pos;
+  const double* freq;
+  const float *qw, *kw;
+  AttnView Q, K, V, Qo, Ko, Vo;
+  const int32_t* slots;  // nullptr: row i to row i
+  int32_t n_slots;
+  // backward
+  int32_t n_rows;
+  const int32_t* rows;  // nullptr: row i
+  AttnView dQ, dK, dQo, dKo;
+  float* part;          // [groups][2][D] sums of the weights' gradients (nullptr: none)
+  int32_t groups;
+  float *dqw, *dkw;
+};
+
+template <typename T>
+struct Chunk;  // eight elements as they lie in memory
+template <>
+struct Chunk<uint16_t> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<u32x4*>(p) = v; }
+  __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  }
+  __device__ __forceinline__ void set(const float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = f2bf2(x[2 * i], x[2 * i + 1]);
+  }
+};
+template <>
+struct Chunk<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = *reinterpret_cast<const f32x4*>(p), v[1] = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    *reinterpret_cast<f32x4*>(p) = v[0], *reinterpret_cast<f32x4*>(p + 4) = v[1];
+  }
+  __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i / 4][i % 4];
+  }
+  __device__ __forceinline__ void set(const float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = x[i];
+  }
+};
+
+// Cosine and sine of pos * freq radians.  The angle in quarter turns is formed and reduced to [-1/2, 1/2] in 64 bits;
+// what is left, at most pi / 4, goes through the Taylor series of both (next terms below 3e-9 and 2e-10 of the value).
+__device__ __forceinline__ float2 turn_of(int pos, double freq) {
+  const double quarters = (double)pos * (freq * 0.63661977236758134308);  // 2 / pi
+  const double whole = rint(quarters);
+  const float x = (float)((quarters - whole) * 1.57079632679489661923), x2 = x * x;
+  const float s = x + x * x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880))));
+  const float c = 1.f + x2 * (-0.5f + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 + x2 * (-1.f / 3628800)))));
+  const int turn = (int)(whole - 4. * floor(whole * 0.25));  // 0 to 3
+  const float a = turn & 1 ? s : c, b = turn & 1 ? c : s;    // cosine and sine but for their signs
+  return make_float2(turn == 1 || turn == 2 ? -a : a, turn >= 2 ? -b : b);
+}
+
+// The sum over the LPH lanes of a head.
+template <int LPH>
+__device__ __forceinline__ float head_sum(float x) {
+  auto add = [&](auto ctrl) {
+    x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  add(std::integral_constant<int, 0xB1>{});   // quads: lanes 1 0 3 2
+  add(std::integral_constant<int, 0x4E>{});   // lanes 2 3 0 1
+  if constexpr (LPH == 8) add(std::integral_constant<int, 0x141>{});  // eights reversed: the other quad's sum
+  return x;
+}
+
+// A lane's place in its wave's heads.
+template <int D>
+struct Lane {
+  static constexpr int LPH = D / 16, HPW = 64 / LPH;
+  int l, g, a, b;  // lane of the head, head, first elements of the two chunks
+  bool turns;
+  __device__ __forceinline__ Lane(int rot, bool next) {
+    const int lane = threadIdx.x & 63, nr = rot / 16;
+    l = lane % LPH, g = lane / LPH;
+    turns = l < nr;
+    const bool half = turns && !next;
+    a = half ? 8 * l : 16 * l;
+    b = half ? 8 * (l + nr) : 16 * l + 8;
+  }
+};
+
+// cos and sin of the row's pairs, for the lane's own eight; cs: the wave's room.
+template <int D>
+__device__ __forceinline__ void row_turns(const RopeArgs& a, int pos, const Lane<D>& at, float (*cs)[64], float (&c)[8],
+                                          float (&s)[8]) {
+  const int lane = threadIdx.x & 63;
+  asm volatile("" ::: "memory");  // the row before has read its own (a wave's LDS accesses run in order)
+  if (lane < a.rot / 2) {
+    const float2 t = turn_of(pos, a.freq[lane]);
+    cs[0][lane] = t.x, cs[1][lane] = t.y;
+  }
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(&cs[0][8 * at.l + i]), y = *reinterpret_cast<const f32x4*>(&cs[1][8 * at.l + i]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[i + e] = x[e], s[i + e] = y[e];
+  }
+}
+
+// The lane's pairs turned: x[0 .. 8) and x[8 .. 16) are its chunks.
+template <bool NEXT>
+__device__ __forceinline__ void turn(float (&x)[16], const float (&c)[8], const float (&s)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int a = NEXT ? 2 * i : i, b = NEXT ? 2 * i + 1 : 8 + i;
+    const float u = x[a], v = x[b];
+    x[a] = u * c[i] - v * s[i], x[b] = v * c[i] + u * s[i];
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void weight_of(const float* w, const Lane<D>& at, float (&x)[16]) {
+  Chunk<float> a, b;
+  a.load(w + at.a), b.load(w + at.b);
+  a.get(x), b.get(x + 8);
+}
+
+__device__ __forceinline__ float square_sum(const float (&x)[16]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += x[i] * x[i];
+  return s;
+}
+
+template <typename T>
+__device__ __forceinline__ T* element(const AttnView& t, int64_t row, int h) {
+  return static_cast<T*>(t.ptr) + row * t.row + h * t.head;
+}
+
+// Heads of a row: queries, keys, values, one list; wave `part` of `split` takes every split-th 64 / (D / 16) of them.
+template <typename T, int D, bool NEXT>
+__global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs a) {
+  __shared__ __attribute__((aligned(16))) float cs[4][2][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
+  const int row = (int)(w / a.split), part = (int)(w % a.split);
+  if (row >= a.n) return;
+  const Lane<D> at(a.rot, NEXT);
+  constexpr int HPW = Lane<D>::HPW;
+  const int heads = a.hq + a.hkv + a.hv, slot = a.slots ? a.slots[row] : row;
+  const bool kept = !a.slots || (uint32_t)slot < (uint32_t)a.n_slots;
+  float c[8], s[8];
+  row_turns<D>(a, a.rot ? a.pos[row] : 0, at, cs[wave], c, s);
+  for (int h0 = part * HPW; h0 < heads; h0 += a.split * HPW) {
+    const int h = h0 + at.g;
+    if (h >= heads) continue;
+    const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
+    const int hh = is_q ? h : is_v ? h - a.hq - a.hkv : h - a.hq;
+    const T* x = element<const T>(is_q ? a.Q : is_v ? a.V : a.K, row, hh);
+    T* y = element<T>(is_q ? a.Qo : is_v ? a.Vo : a.Ko, is_q ? row : slot, hh);
+    Chunk<T> p, q;
+    p.load(x + at.a), q.load(x + at.b);
+    if (!is_v) {
+      float v[16];
+      p.get(v), q.get(v + 8);
+      const float* weight = is_q ? a.qw : a.kw;
+      const float sum = head_sum<Lane<D>::LPH>(square_sum(v));
+      if (weight) {
+        float wt[16];
+        weight_of<D>(weight, at, wt);
+        const float r = __builtin_amdgcn_rsqf(sum * (1.f / D) + a.eps);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = v[i] * r * wt[i];
+      }
+      if (at.turns) turn<NEXT>(v, c, s);
+      p.set(v), q.set(v + 8);
+    }
+    if (is_q || kept) p.store(y + at.a), q.store(y + at.b);
+  }
+}
+
+// Gradient rows: a wave takes every (4 groups / split)-th row and, of its heads, every split-th wave's share, queries
+// first; the weights' gradients stay in registers over its rows.
+template <typename T, int D, bool NEXT>
+__global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs a) {
+  constexpr int LPH = Lane<D>::LPH, HPW = Lane<D>::HPW;
+  __shared__ __attribute__((aligned(16))) float cs[4][2][64];
+  __shared__ __attribute__((aligned(16))) float red[4 * HPW][D];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
+  const int part = (int)(w % a.split);
+  const int64_t step = (int64_t)a.groups * 4 / a.split;  // groups * 4 is a multiple of split
+  const Lane<D> at(a.rot, NEXT);
+  const int qb = (a.hq + HPW - 1) / HPW, kb = (a.hkv + HPW - 1) / HPW;
+  float dw[2][16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0.f;
+  for (int64_t i = w / a.split; i < a.n_rows; i += step) {
+    const int row = a.rows ? a.rows[i] : (int)i;
+    const bool in = (uint32_t)row < (uint32_t)a.n;
+    float c[8], s[8];
+    row_turns<D>(a, a.rot && in ? a.pos[row] : 0, at, cs[wave], c, s);
+    auto head = [&](int h, int heads, const AttnView& dy, const AttnView& x_of, const AttnView& dx, const float* weight,
+                    float (&sums)[16]) {
+      if (h >= heads) return;
+      float g[16], x[16];
+      Chunk<T> p, q;
+      const T* from = element<const T>(dy, i, h);
+      p.load(from + at.a), q.load(from + at.b);
+      p.get(g), q.get(g + 8);
+      if (at.turns) {
+        float back[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) back[e] = -s[e];
+        turn<NEXT>(g, c, back);
+      }
+      if (weight && in) {
+        const T* seen = element<const T>(x_of, row, h);
+        p.load(seen + at.a), q.load(seen + at.b);
+        p.get(x), q.get(x + 8);
+        float wt[16], dot = 0.f;
+        weight_of<D>(weight, at, wt);
+        const float r = __builtin_amdgcn_rsqf(head_sum<LPH>(square_sum(x)) * (1.f / D) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[e] *= r;
+          sums[e] += g[e] * x[e];
+          g[e] *= wt[e];
+          dot += g[e] * x[e];
+        }
+        dot = head_sum<LPH>(dot) * (1.f / D);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) g[e] = r * (g[e] - x[e] * dot);
+      }
+      if (!in)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) g[e] = 0.f;
+      T* to = element<T>(dx, i, h);
+      p.set(g), q.set(g + 8);
+      p.store(to + at.a), q.store(to + at.b);
+    };
+    for (int b = part; b < qb + kb; b += a.split) {
+      if (b < qb) head(b * HPW + at.g, a.hq, a.dQ, a.Q, a.dQo, a.qw, dw[0]);
+      else head((b - qb) * HPW + at.g, a.hkv, a.dK, a.K, a.dKo, a.kw, dw[1]);
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    __syncthreads();
+    Chunk<float> p, q;
+    p.set(dw[k]), q.set(dw[k] + 8);
+    p.store(&red[wave * HPW + at.g][at.a]), q.store(&red[wave * HPW + at.g][at.b]);
+    __syncthreads();
+    if (threadIdx.x < D) {
+      float x = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4 * HPW; ++g) x += red[g][threadIdx.x];
+      a.part[((int64_t)blockIdx.x * 2 + k) * D + threadIdx.x] = x;
+    }
+  }
+}
+
+// The workgroups' sums of 16 columns added in order, in 64 bits: 16 ranges of the workgroups, then the ranges.
+template <int D>
+__global__ __launch_bounds__(256) void rope_weight_kernel(RopeArgs a) {
+  __shared__ double red[16][17];
+  const int col = blockIdx.x * 16 + (threadIdx.x & 15), range = threadIdx.x >> 4;
+  double x = 0.;
+  for (int g = range; g < a.groups; g += 16) x += (double)a.part[(int64_t)g * 2 * D + col];
+  red[range][threadIdx.x & 15] = x;
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  x = 0.;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x += red[r][threadIdx.x];
+  float* const to = col < D ? a.dqw : a.dkw;
+  if (to) to[col % D] = (float)x;
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+constexpr int kFwdWaves = 4096;  // waves a launch should have before a row's heads stay in one
+constexpr int kBwdGroups = 1024;
+
+// Waves that share a row: a power of two, so that the backward's four waves a group divide evenly.
+int split_of(int64_t rows, int blocks, int64_t waves) {
+  int s = 1;
+  while (s < blocks && rows * s < waves && s < 64) s *= 2;
+  return s;
+}
+
+int heads_a_wave(int d) { return 64 / (d / 16); }
+
+int bwd_blocks(const dsv_rope& r) {
+  const int hpw = heads_a_wave(r.head_dim);
+  return (r.heads_q + hpw - 1) / hpw + (r.heads_kv + hpw - 1) / hpw;
+}
+
+// Workgroups of the backward: a number of waves that the split divides.
+int bwd_groups(const dsv_rope& r, int32_t n_rows, int* split) {
+  *split = split_of(n_rows, bwd_blocks(r), 4 * kBwdGroups);
+  const int64_t waves = std::min<int64_t>((int64_t)n_rows * *split, 4 * kBwdGroups);
+  const int64_t per = std::max(1, *split / 4);  // groups of four waves that one row takes
+  return (int)std::max<int64_t>(per, (waves + 4 * per - 1) / (4 * per) * per);
+}
+
+int check(const dsv_rope* r) {
+  if (!r || r->n < 0) return DSV_ERR_ARG;
+  if (r->heads_q < 0 || r->heads_q > 1024 || r->heads_kv < 0 || r->heads_kv > 1024 || r->heads_q + r->heads_kv == 0)
+    return DSV_ERR_RANGE;
+  if (r->head_dim != 64 && r->head_dim != 128) return DSV_ERR_RANGE;
+  if (r->rotated < 0 || r->rotated > r->head_dim || (r->rotated & 15) || (r->interleaved != 0 && r->interleaved != 1))
+    return DSV_ERR_RANGE;
+  if (r->q_weight || r->k_weight) {
+    const float e = (float)r->eps;
+    if (!(e >= FLT_MIN) || !std::isfinite(e)) return DSV_ERR_RANGE;
+  }
+  auto off = [](const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
+  if (off(r->pos, 4) || off(r->freq, 8) || off(r->q_weight, 16) || off(r->k_weight, 16)) return DSV_ERR_ARG;
+  if (r->rotated > 0 && (!r->freq || (r->n > 0 && !r->pos))) return DSV_ERR_ARG;
+  return DSV_OK;
+}
+
+RopeArgs common(const dsv_rope& r) {
+  RopeArgs a{};
+  a.n = r.n;
+  a.hq = r.heads_q, a.hkv = r.heads_kv;
+  a.rot = r.rotated;
+  a.eps = (float)r.eps;
+  a.pos = r.pos, a.freq = r.freq;
+  a.qw = r.q_weight, a.kw = r.k_weight;
+  return a;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? DSV_OK : DSV_ERR_DEVICE; }
+
+template <typename T, bool NEXT>
+hipError_t launch_fwd(const RopeArgs& a, int d, int64_t groups, hipStream_t s) {
+  if (d == 64) hipLaunchKernelGGL((rope_fwd_kernel<T, 64, NEXT>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_fwd_kernel<T, 128, NEXT>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool NEXT>
+hipError_t launch_bwd(const RopeArgs& a, int d, hipStream_t s) {
+  if (d == 64) hipLaunchKernelGGL((rope_bwd_kernel<T, 64, NEXT>), dim3((unsigned)a.groups), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_bwd_kernel<T, 128, NEXT>), dim3((unsigned)a.groups), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace dsv
+
+using namespace dsv;
+
+extern "C" int dsv_rope_fwd(dsv_dtype dt, const dsv_rope* r, const dsv_attn_view* Q, const dsv_attn_view* K,
+                            const dsv_attn_view* V, const int32_t* slots, int32_t n_slots, const dsv_attn_view* Q_out,
+                            const dsv_attn_view* K_out, const dsv_attn_view* V_out, void* hip_stream) {
+  int rc = check(r);
+  if (rc != DSV_OK) return rc;
+  if (dt != DSV_BF16 && dt != DSV_F32) return DSV_ERR_RANGE;
+  if ((!V) != (!V_out) || (slots && n_slots < 0) || (reinterpret_cast<uintptr_t>(slots) & 3)) return DSV_ERR_ARG;
+  RopeArgs a = common(*r);
+  const int32_t d = r->head_dim, kept = slots ? n_slots : r->n;
+  if (a.hq > 0) {
+    if ((rc = view(Q, r->n, a.hq, d, false, &a.Q)) != DSV_OK) return rc;
+    if ((rc = view(Q_out, r->n, a.hq, d, true, &a.Qo)) != DSV_OK) return rc;
+  }
+  if (a.hkv > 0) {
+    if ((rc = view(K, r->n, a.hkv, d, false, &a.K)) != DSV_OK) return rc;
+    if ((rc = view(K_out, kept, a.hkv, d, true, &a.Ko)) != DSV_OK) return rc;
+    if (V) {
+      if ((rc = view(V, r->n, a.hkv, d, false, &a.V)) != DSV_OK) return rc;
+      if ((rc = view(V_out, kept, a.hkv, d, true, &a.Vo)) != DSV_OK) return rc;
+      a.hv = a.hkv;
+    }
+  }
+  if (r->n == 0) return DSV_OK;
+  a.slots = slots, a.n_slots = n_slots;
+  const int hpw = heads_a_wave(d);
+  a.split = split_of(r->n, (a.hq + a.hkv + a.hv + hpw - 1) / hpw, kFwdWaves);
+  const int64_t groups = ((int64_t)r->n * a.split + 3) / 4;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (dt == DSV_BF16)
+    return status(r->interleaved ? launch_fwd<uint16_t, true>(a, d, groups, s) : launch_fwd<uint16_t, false>(a, d, groups, s));
+  return status(r->interleaved ? launch_fwd<float, true>(a, d, groups, s) : launch_fwd<float, false>(a, d, groups, s));
+}
+
+extern "C" int dsv_rope_workspace(const dsv_rope* r, int32_t n_rows, size_t* bytes) {
+  if (!bytes || n_rows < 0) return DSV_ERR_ARG;
+  const int rc = check(r);
+  if (rc != DSV_OK) return rc;
+  int split;
+  *bytes = std::max<size_t>(256, (size_t)bwd_groups(*r, n_rows, &split) * 2 * r->head_dim * sizeof(float));
+  return DSV_OK;
+}
+
+extern "C" int dsv_rope_bwd(dsv_dtype dt, const dsv_rope* r, int32_t n_rows, const int32_t* rows, const dsv_attn_view* dQ,
+                            const dsv_attn_view* dK, const dsv_attn_view* Q, const dsv_attn_view* K,
+                            const dsv_attn_view* dQ_out, const dsv_attn_view* dK_out, float* dq_weight, float* dk_weight,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  int rc = check(r);
+  if (rc != DSV_OK) return rc;
+  if (dt != DSV_BF16 && dt != DSV_F32) return DSV_ERR_RANGE;
+  if (n_rows < 0 || (!rows && n_rows > r->n) || (reinterpret_cast<uintptr_t>(rows) & 3)) return DSV_ERR_ARG;
+  if ((dq_weight && (!r->q_weight || r->heads_q == 0)) || (dk_weight && (!r->k_weight || r->heads_kv == 0)))
+    return DSV_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(dq_weight) | reinterpret_cast<uintptr_t>(dk_weight)) & 15) return DSV_ERR_ARG;
+  RopeArgs a = common(*r);
+  const int32_t d = r->head_dim;
+  if (a.hq > 0) {
+    if ((rc = view(dQ, n_rows, a.hq, d, false, &a.dQ)) != DSV_OK) return rc;
+    if ((rc = view(dQ_out, n_rows, a.hq, d, true, &a.dQo)) != DSV_OK) return rc;
+    if (a.qw && (rc = view(Q, r->n, a.hq, d, false, &a.Q)) != DSV_OK) return rc;
+  }
+  if (a.hkv > 0) {
+    if ((rc = view(dK, n_rows, a.hkv, d, false, &a.dK)) != DSV_OK) return rc;
+    if ((rc = view(dK_out, n_rows, a.hkv, d, true, &a.dKo)) != DSV_OK) return rc;
+    if (a.kw && (rc = view(K, r->n, a.hkv, d, false, &a.K)) != DSV_OK) return rc;
+  }
+  a.groups = bwd_groups(*r, n_rows, &a.split);
+  const bool sums = dq_weight || dk_weight;
+  if (sums) {
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
+    if (ws_bytes < (size_t)a.groups * 2 * d * sizeof(float)) return DSV_ERR_SIZE;
+    a.part = static_cast<float*>(ws);
+  }
+  if (n_rows == 0 && !sums) return DSV_OK;
+  a.n_rows = n_rows, a.rows = rows;
+  a.dqw = dq_weight, a.dkw = dk_weight;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e =
+      dt == DSV_BF16 ? (r->interleaved ? launch_bwd<uint16_t, true>(a, d, s) : launch_bwd<uint16_t, false>(a, d, s))
+                     : (r->interleaved ? launch_bwd<float, true>(a, d, s) : launch_bwd<float, false>(a, d, s));
+  if (e != hipSuccess || !sums) return status(e);
+  hipLaunchKernelGGL(d == 64 ? rope_weight_kernel<64> : rope_weight_kernel<128>, dim3((unsigned)(d / 8)), dim3(256), 0, s, a);
+  return status(hipGetLastError());
+}
