@@ -643,6 +643,19 @@ typedef struct dsv_attn_plan dsv_attn_plan;
 int dsv_attn_build(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv,
                    int32_t heads_q, int32_t heads_kv, int32_t head_dim, size_t* meta_bytes,
                    dsv_attn_plan** out_plan);
+/*
+ * dsv_attn_build_window -- the same for attention that looks back over a window, with a
+ * few first keys that stay visible (sinks): query i of a sequence, which stands at key
+ * p = i + k_len - q_len, sees the keys j <= p with j > p - window or j < sinks.
+ * window >= 1 (1: its own key), sinks >= 0, else DSV_ERR_RANGE.  Every call takes the
+ * plan like any other; only blocks of keys that some query of a tile sees are read, so a
+ * decode token costs window + sinks keys, whatever its cache holds.  A cache that keeps
+ * the sinks' and the last keys alone serves as well: positions count within the sequence's
+ * key rows.  A window that hides no key of the batch gives dsv_attn_build's plan.
+ */
+int dsv_attn_build_window(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv, int32_t heads_q,
+                          int32_t heads_kv, int32_t head_dim, int32_t window, int32_t sinks, size_t* meta_bytes,
+                          dsv_attn_plan** out_plan);
 /* Copies the blob to d_meta (256-byte aligned, at least *meta_bytes bytes),
  * asynchronously on hip_stream; rules and errors of dsv_plan_upload. */
 int dsv_attn_upload(dsv_attn_plan* plan, void* d_meta, size_t meta_bytes, void* hip_stream);

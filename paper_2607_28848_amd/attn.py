@@ -8,7 +8,8 @@ fine-tuning samples -- and serves every layer:
     O, lse = attn.fwd(plan, Q, K, V)                      # Q [n_q][heads_q][d]; K, V [n_kv][heads_kv][d]
     dQ, dK, dV = attn.bwd(plan, Q, K, V, O, lse, dO)      # rows of the fine-tuning samples alone ("compact order")
 
-Query i of a sequence sees its keys j <= i + k_len - q_len.  Tensors may be any views whose head vectors are
+Query i of a sequence sees its keys j <= i + k_len - q_len; Plan(..., window=w, sinks=s) hides those more than w - 1 keys
+back but for the first s.  Tensors may be any views whose head vectors are
 contiguous, but not broadcast ones: columns of a q/k/v product, a cache laid out [row][head][d] or [head][row][d].
 """
 from __future__ import annotations
@@ -34,6 +35,8 @@ class View(ctypes.Structure):
 _viewp = ctypes.POINTER(View)
 _lib.dsv_attn_build.argtypes = [_vp, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_vp)]
 _lib.dsv_attn_build.restype = ctypes.c_int
+_lib.dsv_attn_build_window.argtypes = [_vp] + [_i32] * 8 + [ctypes.POINTER(_sz), ctypes.POINTER(_vp)]
+_lib.dsv_attn_build_window.restype = ctypes.c_int
 _lib.dsv_attn_upload.argtypes = [_vp, _vp, _sz, _vp]
 _lib.dsv_attn_upload.restype = ctypes.c_int
 _lib.dsv_attn_train_rows.argtypes = [_vp, ctypes.POINTER(_i64)]
@@ -90,21 +93,30 @@ def int32(**named):
 
 
 class Plan:
-    """The packed sequences of a batch.  device=None builds a host-only plan (inspection only)."""
+    """The packed sequences of a batch.  device=None builds a host-only plan (inspection only).  window: a query at key
+    p of its sequence sees the keys j <= p with j > p - window or j < sinks (None: every key up to its own)."""
 
-    def __init__(self, seqs, n_q: int, n_kv: int, heads_q: int, heads_kv: int, head_dim: int, device=None, stream=None):
+    def __init__(self, seqs, n_q: int, n_kv: int, heads_q: int, heads_kv: int, head_dim: int, device=None, stream=None,
+                 window=None, sinks: int = 0):
         table = np.asarray(seqs).reshape(-1, 5)
         if not np.all((table >= -(1 << 31)) & (table < 1 << 31)):
             raise ValueError("seqs holds numbers that do not fit 32 bits")
         self.seqs = np.ascontiguousarray(table, np.int32)
         self.n_q, self.n_kv, self.heads_q, self.heads_kv, self.head_dim = int32(
             n_q=n_q, n_kv=n_kv, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim)
+        if window is None and sinks != 0:
+            raise ValueError("sinks without a window")
         self._h = _vp()
         self.meta = None
         n = _sz(0)
-        _check(_lib.dsv_attn_build(self.seqs.ctypes.data, self.seqs.shape[0], self.n_q, self.n_kv, self.heads_q,
-                                   self.heads_kv, self.head_dim, ctypes.byref(n), ctypes.byref(self._h)),
-               "dsv_attn_build")
+        head = (self.seqs.ctypes.data, self.seqs.shape[0], self.n_q, self.n_kv, self.heads_q, self.heads_kv, self.head_dim)
+        if window is None:
+            self.window, self.sinks = None, 0
+            _check(_lib.dsv_attn_build(*head, ctypes.byref(n), ctypes.byref(self._h)), "dsv_attn_build")
+        else:
+            self.window, self.sinks = int32(window=window, sinks=sinks)
+            _check(_lib.dsv_attn_build_window(*head, self.window, self.sinks, ctypes.byref(n), ctypes.byref(self._h)),
+                   "dsv_attn_build_window")
         self.meta_bytes = int(n.value)
         rows = (_i64 * 2)()
         _check(_lib.dsv_attn_train_rows(self._h, rows), "dsv_attn_train_rows")

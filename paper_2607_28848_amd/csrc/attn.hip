@@ -274,7 +274,7 @@ __device__ __forceinline__ void store_sums(float* p, const f32x16 (&acc)[D / 32]
 // the other's products.  With heads of 64 the exponentials (one for 256 operations, a quarter of the vector rate) take
 // as long as the products.  16384 queries, 32 heads of 128 on 8: 1.90 ms (1155 TFLOP/s; a large bf16 product reaches
 // 1290 on the same card).  Nine prompts of about 700, 24 heads of 64 on 4: 36 us (570 TFLOP/s).
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
@@ -287,11 +287,13 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const int off = s.kl - s.ql, hk = h / a.group;
   const int q = qt + 32 * wave + (lane & 31);
   // the tile's keys, or a piece of them
-  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnFwdRows, s.ql) + off), TK * it[3]);
+  const AttnKeys<WIN> keys(it[6], it[7]);
+  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnFwdRows, s.ql) + off) - keys.shift, TK * it[3]);
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
-  auto load = [&](int kt, char* b) {
-    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave);
-    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave);
+  auto load = [&](int kv, char* b) {
+    const int kt = keys.at(kv), n = min(TK, keys.end(a, kv, s.kl) - kt);
+    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, n, D), krow, b, wave);
+    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, n, D), vrow, b + TILE, wave);
   };
   if (k_first < k_end) load(k_first, b0);
   bf16x8 qf[D / 16];
@@ -301,14 +303,15 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   Running run;
   const float c = a.scale * kLog2e;
-  const int seen = q + off;                                        // the lane's last key
+  const int seen = WIN ? max(q + off, -1) : q + off;               // the lane's last key
   const int wave_all = qt + 32 * wave + off;                       // keys up to here are seen by the whole wave
   const int wave_end = min(s.kl, wave_all + 32);                   // keys from here on by none of it
-  auto step = [&](int kt, const char* cur, char* nxt) {
+  auto step = [&](int kv, const char* cur, char* nxt) {
     vmem_wait_all();
     __syncthreads();
-    if (kt + TK < k_end) load(kt + TK, nxt);
-    if (kt >= wave_end) return;
+    if (kv + TK < k_end) load(kv + TK, nxt);
+    const int kt = keys.at(kv);
+    if (kt >= wave_end || AttnKeys<WIN>::passed(a, kt, TK, wave_all)) return;
     f32x16 x[2];
     x[0] = x[1] = zero16();
     __builtin_amdgcn_sched_barrier(0);
@@ -318,11 +321,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
       for (int u = 0; u < 2; ++u) x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, u, i), qf[i], x[u], 0, 0, 0);
     feed<D / 8, 1, 4>();
     __builtin_amdgcn_sched_barrier(0);
-    if (kt + TK - 1 > wave_all) {
+    const uint32_t back = keys.back(a, kv);
+    if (kt + TK - 1 > wave_all || AttnKeys<WIN>::cut(a, back, kt, TK, wave_all + 31)) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[u][v] = kt + 32 * u + tile_row(v) <= seen ? x[u][v] : -INFINITY;
+        for (int v = 0; v < 16; ++v) x[u][v] = AttnKeys<WIN>::sees(a, back, seen, kt + 32 * u + tile_row(v)) ? x[u][v] : -INFINITY;
     }
     softmax_ref(x, c, run, acc);
     const float base = run.ref == -INFINITY ? 0.f : run.ref;
@@ -373,7 +377,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 // its head's queries: the stream of K and V is what bounds it where there are many keys (64 sequences of about 2600,
 // 8 heads of 128: 577 MB in 105 us, 5.5 TB/s), and the loads' latency one after the other where there are few (8 of
 // about 400: 10 us for 12 MB).
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   constexpr int TK = 32, TILE = TK * 2 * D, LDO = D + 4;
   constexpr int kOut = 4 * 32 * LDO * 4, kBuf = 4 * 2 * TILE;
@@ -388,11 +392,13 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   const int off = s.kl - s.ql, rows = s.ql * a.group;
   const int r = r0 + (lane & 31), q = min(r, rows - 1) / a.group, h = hk * a.group + min(r, rows - 1) % a.group;
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
+  const AttnKeys<WIN> keys(it[9], it[10]);
   char* const w0 = b0 + wave * 2 * TILE;
   char* const w1 = b1 + wave * 2 * TILE;
-  auto load = [&](int kt, char* b) {
-    stage<D, TK, 1>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, 0);
-    stage<D, TK, 1>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, 0);
+  auto load = [&](int kv, char* b) {
+    const int kt = keys.at(kv), n = min(TK, keys.end(a, kv, s.kl) - kt);
+    stage<D, TK, 1>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, n, D), krow, b, 0);
+    stage<D, TK, 1>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, n, D), vrow, b + TILE, 0);
   };
   constexpr int LOADS = 2 * TILE / 1024;
   const int kb = k_first + TK * wave;
@@ -405,11 +411,12 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   Running run;
   const float c = a.scale * kLog2e;
-  const int seen = q + off;
+  const int seen = WIN ? max(q + off, -1) : q + off;
   const int all = min(r0, rows - 1) / a.group + off;  // keys up to here are seen by every row
-  auto step = [&](int kt, const char* cur, char* nxt) {
-    if (kt + 4 * TK < k_last) {
-      load(kt + 4 * TK, nxt);
+  const int last = min(r0 + 31, rows - 1) / a.group + off;
+  auto step = [&](int kv, const char* cur, char* nxt) {
+    if (kv + 4 * TK < k_last) {
+      load(kv + 4 * TK, nxt);
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));
     } else {
       vmem_wait_all();
@@ -422,10 +429,12 @@ __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
     for (int i = 0; i < D / 16; ++i) x[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag<D>(cur, 0, i), qf[i], x[0], 0, 0, 0);
     feed<D / 16, 1, D / 16>();
     __builtin_amdgcn_sched_barrier(0);
-    if (kt + TK - 1 > all || kt + TK > k_last) {
+    const int kt = keys.at(kv);
+    const uint32_t back = keys.back(a, kv);
+    if (kt + TK - 1 > all || kv + TK > k_last || AttnKeys<WIN>::cut(a, back, kt, TK, last)) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        x[0][v] = kt + tile_row(v) <= seen && kt + tile_row(v) < k_last ? x[0][v] : -INFINITY;
+        x[0][v] = AttnKeys<WIN>::sees(a, back, seen, kt + tile_row(v)) && kv + tile_row(v) < k_last ? x[0][v] : -INFINITY;
     }
     softmax_ref(x, c, run, acc);
     const float base = run.ref == -INFINITY ? 0.f : run.ref;
@@ -556,7 +565,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // again (p = 2^(c s - lse) needs no maximum), dO V^T, and ds K.  It also leaves delta = do . o and the base-2 lse of its
 // rows for attn_dk, which runs after it.  Bound as attn_fwd is (three fragments of LDS for three matrix instructions),
 // matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.45 ms (412 GFLOP, 920 TFLOP/s).
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
   __shared__ __attribute__((aligned(1024))) char b0[2 * TILE];
@@ -569,12 +578,14 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   const int off = s.kl - s.ql, hk = h / a.group;
   const int q = qt + 32 * wave + (lane & 31);
   const bool in = q < s.ql;
-  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnBwdRows, s.ql) + off), TK * it[3]);
+  const AttnKeys<WIN> keys(it[6], it[7]);
+  const int k_first = TK * it[2], k_end = min(min(s.kl, min(qt + kAttnBwdRows, s.ql) + off) - keys.shift, TK * it[3]);
   const int krow = (int)a.K.row * 2, vrow = (int)a.V.row * 2;
-  auto load = [&](int kt, char* b) {
+  auto load = [&](int kv, char* b) {
+    const int kt = keys.at(kv), n = min(TK, keys.end(a, kv, s.kl) - kt);
     const int ln = fresh_lane();  // the loads' addresses kept in registers would spill others
-    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), krow, b, wave, ln);
-    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, min(TK, s.kl - kt), D), vrow, b + TILE, wave, ln);
+    stage<D, TK, 4>(rows_rsrc(a.K, (int64_t)s.k0 + kt, hk, n, D), krow, b, wave, ln);
+    stage<D, TK, 4>(rows_rsrc(a.V, (int64_t)s.k0 + kt, hk, n, D), vrow, b + TILE, wave, ln);
   };
   if (k_first < k_end) load(k_first, b0);
   bf16x8 qf[D / 16], df[D / 16];
@@ -599,10 +610,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   const float c = a.scale * kLog2e;
-  const int seen = q + off, wave_all = qt + 32 * wave + off, wave_end = min(s.kl, wave_all + 32);
+  const int seen = WIN ? max(q + off, -1) : q + off, wave_all = qt + 32 * wave + off, wave_end = min(s.kl, wave_all + 32);
   // 64 keys as two blocks: the terms of one are formed beside the products of the other.  CUT: some query of
   // the wave does not see all of them.
-  auto block = [&](auto cut, int kt, const char* cur) {
+  auto block = [&](auto cut, int kt, uint32_t back, const char* cur) {
     constexpr bool CUT = decltype(cut)::value;
     constexpr int V = (CUT ? 104 : 72) * 8 / D + 1;
     f32x16 x[2], dp[2];
@@ -619,7 +630,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const float t = __builtin_amdgcn_exp2f(x[u][v] * c - lse2) * (dp[u][v] - delta);
-        x[u][v] = !CUT || kt + 32 * u + tile_row(v) <= seen ? t : 0.f;
+        x[u][v] = !CUT || AttnKeys<WIN>::sees(a, back, seen, kt + 32 * u + tile_row(v)) ? t : 0.f;
       }
       ds[u][0] = pack8(x[u], 0), ds[u][1] = pack8(x[u], 1);
     };
@@ -646,13 +657,15 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     feed<D / 16, 2, 2>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto step = [&](int kt, const char* cur, char* nxt) {
+  auto step = [&](int kv, const char* cur, char* nxt) {
     vmem_wait_all();
     __syncthreads();
-    if (kt + TK < k_end) load(kt + TK, nxt);
-    if (kt >= wave_end) return;
-    if (kt + TK - 1 > wave_all) block(bool_c<true>{}, kt, cur);
-    else block(bool_c<false>{}, kt, cur);
+    if (kv + TK < k_end) load(kv + TK, nxt);
+    const int kt = keys.at(kv);
+    if (kt >= wave_end || AttnKeys<WIN>::passed(a, kt, TK, wave_all)) return;
+    const uint32_t back = keys.back(a, kv);
+    if (kt + TK - 1 > wave_all || AttnKeys<WIN>::cut(a, back, kt, TK, wave_all + 31)) block(bool_c<true>{}, kt, back, cur);
+    else block(bool_c<false>{}, kt, back, cur);
   };
   for (int kt = k_first; kt < k_end; kt += 2 * TK) {
     step(kt, b0, b1);
@@ -680,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // atomics here.  The matrix core is 45% busy: 64 queries against 128 keys read 272 KB of LDS, 2200 cycles beside 2048 of
 // products, and two waves a SIMD overlap them in part.  Four samples of 2048, 64 heads of 128 on
 // 8: 0.65 ms (550 GFLOP, 845 TFLOP/s); two of 1024, 32 heads on 8: 72 us and 8 for the join.
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;
   // Q, dO, p of 4 x 32 keys, lse (base 2) and delta
@@ -700,7 +713,8 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   const int qrow = (int)a.Q.row * 2, drow = (int)a.dO.row * 2;
   const int q_first = max(0, k0 - off);
   // the tile's steps, or a piece of them
-  const int per_head = q_first < s.ql ? (s.ql - q_first + TQ - 1) / TQ : 0, n0 = it[2], steps = it[3] - n0;
+  const int q_end = WIN ? it[6] : s.ql;
+  const int per_head = q_first < q_end ? (q_end - q_first + TQ - 1) / TQ : 0, n0 = it[2], steps = it[3] - n0;
   // The last queries first, one query head after the other: the workgroups of a sequence's key tiles run
   // through the same rows at the same time, whatever their first query, and share them in L2 (heads
   // outside and queries upwards missed 56% of its lines, this order 25%: four samples of 2048, 64 heads on 8, 1156 us
@@ -732,7 +746,8 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
     constexpr int V = (CUT ? 112 : 64) * 16 / D + 1;
     const int first = k0 + 32 * blk + (ln & 31) - off;  // the first query that sees the lane's key
     const int ahead = qt + 4 * (ln >> 5) - first;
-    const uint32_t seen_by = s.ql - first;
+    const int to_end = s.ql - first;
+    const uint32_t seen_by = WIN && k0 + 32 * blk + (ln & 31) >= a.sinks ? min(to_end, a.window) : to_end;
     f32x16 x[2];
     f32x4 l4[2][4];
     bf16x8 p[2][2];
@@ -851,7 +866,9 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
       const int ln = begin(n, nxt);
       if (n == steps) return;
       const int qt = q_of(n);
-      if (k0 + 32 * blk + 31 > qt + off || qt + TQ > s.ql) form_p(bool_c<true>{}, cur, qt, ln);
+      if (k0 + 32 * blk + 31 > qt + off || qt + TQ > s.ql ||
+          AttnKeys<WIN>::cut(a, a.window, k0 + 32 * blk, 32, qt + TQ - 1 + off))
+        form_p(bool_c<true>{}, cur, qt, ln);
       else form_p(bool_c<false>{}, cur, qt, ln);
     };
     for (int n = 0; n <= steps; n += 3) {
@@ -873,6 +890,9 @@ __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
     }
   }
   if (!in) return;
+  if (AttnKeys<WIN>::unseen(a, off, k))  // 0 times an infinite value
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = zero16();
   if (it[5] > 1) {
     float* p = a.part_o + ((((int64_t)it[4] * a.hkv + hk) * 2 + (second ? 0 : 1)) * kAttnBwdRows + 32 * blk + (lane & 31)) * D +
                4 * (lane >> 5);
@@ -998,10 +1018,22 @@ AttnArgs common(const dsv_attn_plan& p, double scale) {
   a.n_q = p.n_q;
   a.train_q = p.train_q;
   a.scale = (float)scale;
+  a.window = p.window;
+  a.sinks = p.sinks;
   return a;
 }
 
 int status(hipError_t e) { return e == hipSuccess ? DSV_OK : DSV_ERR_DEVICE; }
+
+// One of a kernel's four forms.
+template <typename K>
+hipError_t launch(K k64, K k128, K w64, K w128, bool windowed, const AttnArgs& a, int64_t groups, hipStream_t s,
+                  int threads = 256) {
+  if (groups <= 0) return hipSuccess;
+  hipLaunchKernelGGL(windowed ? (a.d == 64 ? w64 : w128) : a.d == 64 ? k64 : k128, dim3((unsigned)groups),
+                     dim3((unsigned)threads), 0, s, a);
+  return hipGetLastError();
+}
 
 template <typename K>
 hipError_t launch(K k64, K k128, const AttnArgs& a, int64_t groups, hipStream_t s, int threads = 256) {
@@ -1041,18 +1073,20 @@ extern "C" int dsv_attn_fwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   if (dt == DSV_F32) {
     a.items = p->dptr(p->lay.f32_items);
     a.n_items = p->n_f32;
-    return status(launch_attn_f32_fwd(a, s));
+    return status(launch_attn_f32_fwd(a, p->windowed, s));
   }
   const int64_t hq = p->hq, hkv = p->hkv;
   a.items = p->dptr(p->lay.fwd_items);
   a.first_o = a.part_o = at<float>(ws, w.fwd_o);
   a.first_ml = a.part_ml = at<float>(ws, w.fwd_ml);
-  hipError_t e = launch(attn_fwd_kernel<64>, attn_fwd_kernel<128>, a, p->n_fwd * hq, s);
+  hipError_t e = launch(attn_fwd_kernel<64, false>, attn_fwd_kernel<128, false>, attn_fwd_kernel<64, true>,
+                        attn_fwd_kernel<128, true>, p->windowed, a, p->n_fwd * hq, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.split_items);
   a.part_o = at<float>(ws, w.split_o);
   a.part_ml = at<float>(ws, w.split_ml);
-  e = launch(attn_split_kernel<64>, attn_split_kernel<128>, a, p->n_split * hkv, s);
+  e = launch(attn_split_kernel<64, false>, attn_split_kernel<128, false>, attn_split_kernel<64, true>,
+             attn_split_kernel<128, true>, p->windowed, a, p->n_split * hkv, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.join_items);
   a.first_join = p->dptr(p->lay.fwd_join);
@@ -1089,20 +1123,22 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
   if (dt == DSV_F32) {
     a.items = p->dptr(p->lay.f32_dq_items);
     a.n_items = p->n_f32_dq;
-    const hipError_t e = launch_attn_f32_dq(a, s);
+    const hipError_t e = launch_attn_f32_dq(a, p->windowed, s);
     if (e != hipSuccess) return status(e);
     a.items = p->dptr(p->lay.f32_dk_items);
     a.n_items = p->n_f32_dk;
     a.parts = f32_parts(*p);
-    return status(launch_attn_f32_dk(a, s));
+    return status(launch_attn_f32_dk(a, p->windowed, s));
   }
   a.items = p->dptr(p->lay.dq_items);
   a.first_o = a.part_o = at<float>(ws, w.dq);
-  hipError_t e = launch(attn_dq_kernel<64>, attn_dq_kernel<128>, a, p->n_dq * hq, s);
+  hipError_t e = launch(attn_dq_kernel<64, false>, attn_dq_kernel<128, false>, attn_dq_kernel<64, true>,
+                        attn_dq_kernel<128, true>, p->windowed, a, p->n_dq * hq, s);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.dk_items);
   a.part_o = at<float>(ws, w.dk);
-  e = launch(attn_dk_kernel<64>, attn_dk_kernel<128>, a, p->n_dk * hkv, s, 512);
+  e = launch(attn_dk_kernel<64, false>, attn_dk_kernel<128, false>, attn_dk_kernel<64, true>, attn_dk_kernel<128, true>,
+             p->windowed, a, p->n_dk * hkv, s, 512);
   if (e != hipSuccess) return status(e);
   a.items = p->dptr(p->lay.dk_join);
   a.first_join = p->dptr(p->lay.dq_join);

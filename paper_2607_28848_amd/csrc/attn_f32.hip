@@ -118,8 +118,19 @@ __device__ __forceinline__ f32x4 gather(const float* red, int r, int c) {
   return x;
 }
 
+// The blocks of 16 keys that a tile of 16 queries walks, as the plan lays them down for the bf16 tiles.
+template <bool WIN>
+__device__ __forceinline__ AttnKeys<WIN> keys_of(const AttnArgs& a, const Seq& s, int qt, int& end) {
+  const int off = s.kl - s.ql;
+  end = min(s.kl, min(qt + 16, s.ql) + off);
+  if (!WIN || end <= 0 || qt + off < a.window || qt + off - a.window + 1 <= a.sinks) return AttnKeys<WIN>(0, 0);
+  const int sink = (a.sinks + 15) & ~15, shift = qt + off - a.window + 1 - sink;
+  end -= shift;
+  return AttnKeys<WIN>(sink, shift);
+}
+
 // 16 queries of one head over the keys that the last of them sees.
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
   constexpr int NW = 4;
   __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
@@ -134,16 +145,19 @@ __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
   f32x4 acc[D / 16];
   clear<D>(acc);
   float m = -INFINITY, l = 0.f;
-  const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
-  for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
+  int k_end;
+  const AttnKeys<WIN> keys = keys_of<WIN>(a, s, qt, k_end);
+  for (int b = 16 * wave; b < k_end; b += 16 * NW) {
+    const int kt = keys.at(b), n = keys.end(a, b, s.kl) - kt;
+    const uint32_t back = keys.back(a, b);
     float kv[D / 4], vv[4][D / 16];
-    load_quarter<D>(rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, s.kl - kt), a.K.row, kv);
-    load_columns<D>(rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, s.kl - kt), a.V.row, vv);
+    load_quarter<D>(rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, n), a.K.row, kv);
+    load_columns<D>(rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, n), a.V.row, vv);
     f32x4 x = dot_tile<D>(kv, qv);
     float mx = m;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      x[v] = kt + 4 * (lane >> 4) + v <= q + off ? x[v] * a.scale : -INFINITY;
+      x[v] = AttnKeys<WIN>::sees(a, back, WIN ? max(q + off, -1) : q + off, kt + 4 * (lane >> 4) + v) ? x[v] * a.scale : -INFINITY;
       mx = fmaxf(mx, x[v]);
     }
     mx = quad_max(mx);
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
 }
 
 // dQ of 16 queries of one head, and delta = do . o for the launch of dK and dV.
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   constexpr int NW = 4;
   __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
@@ -207,11 +221,14 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   const float lse = in ? exp_from(a.lse[(int64_t)h * a.n_q + s.q0 + q]) : 0.f;
   f32x4 acc[D / 16];
   clear<D>(acc);
-  const int k_end = min(s.kl, min(qt + 16, s.ql) + off);
-  for (int kt = 16 * wave; kt < k_end; kt += 16 * NW) {
+  int k_end;
+  const AttnKeys<WIN> keys = keys_of<WIN>(a, s, qt, k_end);
+  for (int b = 16 * wave; b < k_end; b += 16 * NW) {
+    const int kt = keys.at(b), n = keys.end(a, b, s.kl) - kt;
+    const uint32_t back = keys.back(a, b);
     float kv[D / 4], vv[D / 4], kc[4][D / 16];
-    const auto kr = rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, s.kl - kt);
-    const auto vr = rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, s.kl - kt);
+    const auto kr = rows_of<D>(a.K, (int64_t)s.k0 + kt, hk, n);
+    const auto vr = rows_of<D>(a.V, (int64_t)s.k0 + kt, hk, n);
     load_quarter<D>(kr, a.K.row, kv);
     load_quarter<D>(vr, a.V.row, vv);
     load_columns<D>(kr, a.K.row, kc);
@@ -219,7 +236,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
     f32x4 ds;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const bool seen = kt + 4 * (lane >> 4) + v <= q + off;
+      const bool seen = AttnKeys<WIN>::sees(a, back, WIN ? max(q + off, -1) : q + off, kt + 4 * (lane >> 4) + v);
       ds[v] = seen ? expf(x[v] * a.scale - lse) * (dp[v] - delta) * a.scale : 0.f;
     }
     add_rows<D>(kc, ds, acc);
@@ -238,7 +255,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
 // dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
 // heads (so the sums over them need no atomics), or of one of a.parts ranges of them, whose sums go to the workspace
 // (32 us whole, 10.3 and 4.0 for the join in four parts: the first batch above).
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
   constexpr int NW = 8;
   __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
@@ -254,7 +271,9 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
   clear<D>(dk);
   clear<D>(dv);
   const int q_first = max(0, k0 - off);
-  const int per_head = q_first < s.ql ? (s.ql - q_first + 15) / 16 : 0;
+  // the keys' last query: with a window that of the last key, but the sinks are seen to the end
+  const int q_end = WIN && k0 >= a.sinks ? (int)min((int64_t)s.ql, (int64_t)min(k0 + 16, s.kl) - 1 - off + a.window) : s.ql;
+  const int per_head = q_first < q_end ? (q_end - q_first + 15) / 16 : 0;
   const int h0 = part * a.group / a.parts, h1 = (part + 1) * a.group / a.parts;
   for (int n = wave; n < per_head * (h1 - h0); n += NW) {
     const int h = g * a.group + h0 + n / per_head, qt = q_first + n % per_head * 16;
@@ -278,12 +297,16 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int q = qt + 4 * (lane >> 4) + v;
-      const bool seen = q < s.ql && k <= q + off && lse[v] != -INFINITY;  // as exp_from(), which spills here
+      const bool seen = q < s.ql && AttnKeys<WIN>::sees(a, a.window, WIN ? max(q + off, -1) : q + off, k) && lse[v] != -INFINITY;  // as exp_from(), which spills here
       p[v] = seen ? expf(x[v] * a.scale - lse[v]) : 0.f;
       ds[v] = seen ? p[v] * (dp[v] - delta[v]) * a.scale : 0.f;
     }
     add_rows<D>(oc, p, dv);
     add_rows<D>(qc, ds, dk);
+  }
+  if (AttnKeys<WIN>::unseen(a, off, k)) {  // 0 times an infinite value
+    clear<D>(dk);
+    clear<D>(dv);
   }
   auto put = [&](const f32x4 (&acc)[D / 16], const AttnView& t, int half) {
     __syncthreads();
@@ -321,28 +344,34 @@ __global__ __launch_bounds__(256) void attn_f32_dk_join_kernel(AttnArgs a) {
 
 }  // namespace
 
-hipError_t launch_attn_f32_fwd(const AttnArgs& a, hipStream_t s) {
+hipError_t launch_attn_f32_fwd(const AttnArgs& a, bool windowed, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)(a.n_items * (int64_t)a.hq));
-  if (a.d == 64) hipLaunchKernelGGL(attn_f32_fwd_kernel<64>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(attn_f32_fwd_kernel<128>, grid, dim3(256), 0, s, a);
+  if (windowed && a.d == 64) hipLaunchKernelGGL((attn_f32_fwd_kernel<64, true>), grid, dim3(256), 0, s, a);
+  else if (windowed) hipLaunchKernelGGL((attn_f32_fwd_kernel<128, true>), grid, dim3(256), 0, s, a);
+  else if (a.d == 64) hipLaunchKernelGGL((attn_f32_fwd_kernel<64, false>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attn_f32_fwd_kernel<128, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s) {
+hipError_t launch_attn_f32_dq(const AttnArgs& a, bool windowed, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)(a.n_items * (int64_t)a.hq));
-  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dq_kernel<64>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(attn_f32_dq_kernel<128>, grid, dim3(256), 0, s, a);
+  if (windowed && a.d == 64) hipLaunchKernelGGL((attn_f32_dq_kernel<64, true>), grid, dim3(256), 0, s, a);
+  else if (windowed) hipLaunchKernelGGL((attn_f32_dq_kernel<128, true>), grid, dim3(256), 0, s, a);
+  else if (a.d == 64) hipLaunchKernelGGL((attn_f32_dq_kernel<64, false>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attn_f32_dq_kernel<128, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s) {
+hipError_t launch_attn_f32_dk(const AttnArgs& a, bool windowed, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   const int64_t tiles = a.n_items * (int64_t)a.hkv;
   const dim3 grid((unsigned)(tiles * a.parts));
-  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_kernel<64>, grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL(attn_f32_dk_kernel<128>, grid, dim3(512), 0, s, a);
+  if (windowed && a.d == 64) hipLaunchKernelGGL((attn_f32_dk_kernel<64, true>), grid, dim3(512), 0, s, a);
+  else if (windowed) hipLaunchKernelGGL((attn_f32_dk_kernel<128, true>), grid, dim3(512), 0, s, a);
+  else if (a.d == 64) hipLaunchKernelGGL((attn_f32_dk_kernel<64, false>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((attn_f32_dk_kernel<128, false>), grid, dim3(512), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_join_kernel<64>, dim3((unsigned)(2 * tiles)), dim3(256), 0, s, a);

@@ -61,16 +61,20 @@ int64_t makespan(const std::vector<int64_t>& steps, int64_t copies, int64_t piec
   return end;
 }
 
-// tiles: {-steps, {sequence, first row}}
-Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t copies, int slots, int64_t least,
-        int64_t join, int64_t most_tiles) {
-  std::stable_sort(t.begin(), t.end(), [](const auto& a, const auto& b) { return a.first < b.first; });
+struct Tile {
+  int64_t steps;
+  int32_t seq, first;
+  int32_t x = 0, y = 0;  // the descriptor's last words
+};
+
+Cut cut(std::vector<Tile> t, int64_t copies, int slots, int64_t least, int64_t join, int64_t most_tiles) {
+  std::stable_sort(t.begin(), t.end(), [](const Tile& a, const Tile& b) { return a.steps > b.steps; });
   std::vector<int64_t> steps;
   int64_t all = 0, most = 0;
-  for (const auto& e : t) {
-    steps.push_back(-e.first);
-    all += -e.first;
-    most = std::max(most, -e.first);
+  for (const Tile& e : t) {
+    steps.push_back(e.steps);
+    all += e.steps;
+    most = std::max(most, e.steps);
   }
   int64_t piece = std::max<int64_t>(most, 1);
   const int64_t share = all * copies / slots;
@@ -89,16 +93,15 @@ Cut cut(std::vector<std::pair<int64_t, std::pair<int32_t, int32_t>>> t, int64_t 
     int32_t w[kAttnTileWords];
   };
   std::vector<Piece> all_pieces;
-  for (const auto& e : t) {
-    const int64_t s = -e.first, n = std::max<int64_t>(1, (s + piece - 1) / piece), len = (s + n - 1) / n;
+  for (const Tile& e : t) {
+    const int64_t s = e.steps, n = std::max<int64_t>(1, (s + piece - 1) / piece), len = (s + n - 1) / n;
     if (n > 1) {
-      c.join.insert(c.join.end(), {e.second.first, e.second.second, c.n_slots, (int32_t)n});
+      c.join.insert(c.join.end(), {e.seq, e.first, c.n_slots, (int32_t)n});
       ++c.n_join;
     }
     for (int64_t k = 0; k < n; ++k) {
       const int64_t b = std::min(k * len, s), l = std::min((k + 1) * len, s);
-      all_pieces.push_back({l - b, {e.second.first, e.second.second, (int32_t)b, (int32_t)l, n > 1 ? c.n_slots++ : 0,
-                                    (int32_t)n, 0, 0}});
+      all_pieces.push_back({l - b, {e.seq, e.first, (int32_t)b, (int32_t)l, n > 1 ? c.n_slots++ : 0, (int32_t)n, e.x, e.y}});
     }
   }
   std::stable_sort(all_pieces.begin(), all_pieces.end(), [](const Piece& a, const Piece& b) { return a.steps > b.steps; });
@@ -112,10 +115,32 @@ int64_t keys_seen(const dsv_attn_seq& s, int64_t last) {
   return std::max<int64_t>(0, std::min<int64_t>(s.k_len, last + 1 + s.k_len - s.q_len));
 }
 
+// The keys that queries [q0, q1) of a sequence see, in steps of `step` keys.  Where the window leaves a gap behind the
+// sinks: `sink` keys' worth of steps for the sinks alone, and behind them the keys from the window's first one on, which
+// lie `shift` keys from where they would without the gap (`shift` may be negative: a step of sinks may be short).  So no
+// key is read that none of the queries sees.  Else sink and shift are 0.
+struct Span {
+  int64_t steps, sink, shift;
+};
+Span span_of(const dsv_attn_plan& p, const dsv_attn_seq& s, int64_t q0, int64_t q1, int64_t step) {
+  const int64_t end = keys_seen(s, q1 - 1), all = (end + step - 1) / step;
+  const int64_t first = q0 + s.k_len - s.q_len + 1 - p.window;
+  if (!p.windowed || end == 0 || first <= p.sinks) return {all, 0, 0};
+  const int64_t sink = (p.sinks + step - 1) / step;
+  return {sink + (end - first + step - 1) / step, sink * step, first - sink * step};
+}
+
+// One past the last query that sees one of the keys [k0, k1): the sinks are seen to the end.
+int64_t queries_end(const dsv_attn_plan& p, const dsv_attn_seq& s, int64_t k0, int64_t k1) {
+  if (!p.windowed || k0 < p.sinks) return s.q_len;
+  return std::min<int64_t>(s.q_len, std::min<int64_t>(k1, s.k_len) - 1 - ((int64_t)s.k_len - s.q_len) + p.window);
+}
+
 int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_t hq, int32_t hkv, int32_t d,
-          dsv_attn_plan& p) {
+          int32_t window, int32_t sinks, dsv_attn_plan& p) {
   if (n < 0 || n_q < 0 || n_kv < 0 || (n > 0 && !seqs)) return DSV_ERR_ARG;
   if (hkv < 1 || hq < hkv || hq > 1024 || hq % hkv != 0 || (d != 64 && d != 128)) return DSV_ERR_RANGE;
+  if (window < 1 || sinks < 0) return DSV_ERR_RANGE;
   std::vector<int32_t> order(n);
   std::iota(order.begin(), order.end(), 0);
   for (int32_t i = 0; i < n; ++i) {
@@ -140,6 +165,11 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   }
   if (8 * tiles_q * hq > INT32_MAX || 8 * tiles_k * hkv > INT32_MAX) return DSV_ERR_SIZE;
 
+  // A window that hides nothing is none.
+  for (int32_t i = 0; i < n; ++i)
+    if (seqs[i].q_len > 0 && seqs[i].k_len > window && sinks < seqs[i].k_len - window) p.windowed = true;
+  p.window = window;
+  p.sinks = sinks;
   p.n_seqs = n;
   p.n_q = n_q;
   p.n_kv = n_kv;
@@ -165,35 +195,48 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     }
   }
 
-  Tiles fwd, f32, dq, dk, f32_dq, f32_dk;
+  Tiles f32, f32_dq, f32_dk;
+  std::vector<Tile> fwd, dq, dk;
+  // query tiles: the words that their kernels find the keys by
+  auto query_tile = [&](std::vector<Tile>& to, int32_t i, int64_t q, int64_t rows) {
+    const Span sp = span_of(p, seqs[i], q, std::min<int64_t>(q + rows, seqs[i].q_len), 64);
+    to.push_back({sp.steps, i, (int32_t)q, (int32_t)sp.sink, (int32_t)sp.shift});
+  };
+  auto f32_tile = [&](Tiles& to, int32_t i, int64_t q) {
+    const dsv_attn_seq& s = seqs[i];
+    const int64_t q1 = std::min<int64_t>(q + kAttnF32Rows, s.q_len);
+    to.add(p.windowed ? 16 * span_of(p, s, q, q1, 16).steps : keys_seen(s, q1 - 1), i, q);
+  };
+  // keys that a sequence of the split form walks: those of all its queries, the sinks' blocks whole
+  auto split_shift = [&](const dsv_attn_seq& s) { return span_of(p, s, 0, s.q_len, 32).shift; };
+  auto split_keys = [&](const dsv_attn_seq& s) { return s.k_len - split_shift(s); };
   int64_t split_keys_all = 0, split_most = 0;  // keys that the split form's tiles read; the longest sequence's
   std::vector<int32_t> split;
   for (int32_t i = 0; i < n; ++i) {
     const dsv_attn_seq& s = seqs[i];
-    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows)
-      f32.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
+    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows) f32_tile(f32, i, q);
     if (s.q_len <= kAttnSplitQ) {
       if (s.q_len == 0) continue;
       split.push_back(i);
       const int64_t tiles = ((int64_t)s.q_len * group + kAttnPackRows - 1) / kAttnPackRows;
-      split_keys_all += tiles * s.k_len;
-      split_most = std::max<int64_t>(split_most, s.k_len);
+      split_keys_all += tiles * split_keys(s);
+      split_most = std::max<int64_t>(split_most, split_keys(s));
     } else {
-      for (int64_t q = 0; q < s.q_len; q += kAttnFwdRows)
-        fwd.add((keys_seen(s, std::min<int64_t>(q + kAttnFwdRows, s.q_len) - 1) + 63) / 64, i, q);
+      for (int64_t q = 0; q < s.q_len; q += kAttnFwdRows) query_tile(fwd, i, q, kAttnFwdRows);
     }
   }
   for (int32_t i = 0; i < n; ++i) {
     const dsv_attn_seq& s = seqs[i];
     if (!s.is_train) continue;
-    for (int64_t q = 0; q < s.q_len; q += kAttnBwdRows)
-      dq.add((keys_seen(s, std::min<int64_t>(q + kAttnBwdRows, s.q_len) - 1) + 63) / 64, i, q);
-    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows)
-      f32_dq.add(keys_seen(s, std::min<int64_t>(q + kAttnF32Rows, s.q_len) - 1), i, q);
-    // queries that see key k: from max(0, k - (k_len - q_len)) on
-    auto seen_by = [&](int64_t k) { return s.q_len - std::max<int64_t>(0, k - ((int64_t)s.k_len - s.q_len)); };
-    for (int64_t k = 0; k < s.k_len; k += kAttnBwdRows) dk.add(std::max<int64_t>(0, (seen_by(k) + 63) / 64) * group, i, k);
-    for (int64_t k = 0; k < s.k_len; k += kAttnF32Rows) f32_dk.add(seen_by(k), i, k);
+    for (int64_t q = 0; q < s.q_len; q += kAttnBwdRows) query_tile(dq, i, q, kAttnBwdRows);
+    for (int64_t q = 0; q < s.q_len; q += kAttnF32Rows) f32_tile(f32_dq, i, q);
+    // queries that see keys from k on: from max(0, k - (k_len - q_len)) on, up to `end`
+    auto seen_by = [&](int64_t k, int64_t end) { return end - std::max<int64_t>(0, k - ((int64_t)s.k_len - s.q_len)); };
+    for (int64_t k = 0; k < s.k_len; k += kAttnBwdRows) {
+      const int64_t end = std::max<int64_t>(0, queries_end(p, s, k, k + kAttnBwdRows));
+      dk.push_back({std::max<int64_t>(0, (seen_by(k, end) + 63) / 64) * group, i, (int32_t)k, (int32_t)end, 0});
+    }
+    for (int64_t k = 0; k < s.k_len; k += kAttnF32Rows) f32_dk.add(seen_by(k, queries_end(p, s, k, k + kAttnF32Rows)), i, k);
   }
 
   // Pieces: one length for the whole call
@@ -207,8 +250,11 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     const dsv_attn_seq& s = seqs[i];
     const int64_t rows = (int64_t)s.q_len * group;
     // pieces of equal length (to a multiple of 32 keys)
-    const int64_t np = std::max<int64_t>(1, (s.k_len + piece - 1) / piece);
-    const int64_t len = std::max<int64_t>(32, ((s.k_len + np - 1) / np + 31) / 32 * 32);
+    const Span sp = span_of(p, s, 0, s.q_len, 32);
+    const int32_t sink = (int32_t)sp.sink, shift = (int32_t)sp.shift;
+    const int64_t keys = split_keys(s);
+    const int64_t np = std::max<int64_t>(1, (keys + piece - 1) / piece);
+    const int64_t len = std::max<int64_t>(32, ((keys + np - 1) / np + 31) / 32 * 32);
     for (int64_t r = 0; r < rows; r += kAttnPackRows) {
       const int64_t first = (int64_t)pieces.size();
       if (first + np > INT32_MAX / kAttnSplitWords) return DSV_ERR_SIZE;
@@ -216,8 +262,8 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
                                            s.k_len, 0, 0, 0});
       for (int64_t k = 0; k < np; ++k)
         pieces.push_back({s.q_start, s.q_len, s.k_start, s.k_len, (int32_t)r, (int32_t)np, (int32_t)(first + k),
-                          (int32_t)std::min<int64_t>(k * len, s.k_len), (int32_t)std::min<int64_t>((k + 1) * len, s.k_len), 0,
-                          0, 0});
+                          (int32_t)std::min<int64_t>(k * len, keys), (int32_t)std::min<int64_t>((k + 1) * len, keys), sink,
+                          shift, 0});
     }
   }
   std::stable_sort(pieces.begin(), pieces.end(), [](const auto& a, const auto& b) { return a[8] - a[7] > b[8] - b[7]; });
@@ -236,10 +282,11 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
     *out = (int32_t)c;
     return c;
   };
-  const Cut cf = cut(std::move(fwd.t), hq, kAttnFwdSlots, kAttnFwdPieceSteps, 2, 4 * kAttnFwdSlots);
-  const Cut ck = cut(std::move(dk.t), hkv, kAttnDkSlots, kAttnGradPieceSteps, 3, 4 * kAttnDkSlots);
+  const Cut cf = cut(std::move(fwd), hq, kAttnFwdSlots, kAttnFwdPieceSteps, 2, 4 * kAttnFwdSlots);
+  // The sinks' key tile has every query of its sequence, however many tiles of a window there are beside it.
+  const Cut ck = cut(std::move(dk), hkv, kAttnDkSlots, kAttnGradPieceSteps, 3, p.windowed ? INT64_MAX : 4 * kAttnDkSlots);
   // Query tiles that fill the CUs run two to a CU, and the long ones faster when the short ones end: only fewer are cut.
-  const Cut cq = cut(std::move(dq.t), hq, kAttnDkSlots, kAttnGradPieceSteps, 3, kAttnDkSlots);
+  const Cut cq = cut(std::move(dq), hq, kAttnDkSlots, kAttnGradPieceSteps, 3, kAttnDkSlots);
   p.n_fwd = cf.n_items, p.n_fwd_join = cf.n_join, p.fwd_slots = cf.n_slots;
   p.n_dq = cq.n_items, p.n_dq_join = cq.n_join, p.dq_slots = cq.n_slots;
   p.n_dk = ck.n_items, p.n_dk_join = ck.n_join, p.dk_slots = ck.n_slots;
@@ -273,13 +320,19 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
 
 extern "C" int dsv_attn_build(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv, int32_t heads_q,
                               int32_t heads_kv, int32_t head_dim, size_t* meta_bytes, dsv_attn_plan** out_plan) {
+  return dsv_attn_build_window(seqs, n_seqs, n_q, n_kv, heads_q, heads_kv, head_dim, INT32_MAX, 0, meta_bytes, out_plan);
+}
+
+extern "C" int dsv_attn_build_window(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv, int32_t heads_q,
+                                     int32_t heads_kv, int32_t head_dim, int32_t window, int32_t sinks,
+                                     size_t* meta_bytes, dsv_attn_plan** out_plan) {
   if (out_plan) *out_plan = nullptr;
   if (!meta_bytes || !out_plan) return DSV_ERR_ARG;
   dsv_attn_plan* p = nullptr;
   int rc = DSV_OK;
   try {
     p = new dsv_attn_plan();
-    rc = build(seqs, n_seqs, n_q, n_kv, heads_q, heads_kv, head_dim, *p);
+    rc = build(seqs, n_seqs, n_q, n_kv, heads_q, heads_kv, head_dim, window, sinks, *p);
   } catch (const std::bad_alloc&) {
     rc = DSV_ERR_SIZE;
   } catch (...) {

@@ -48,11 +48,16 @@ constexpr int kAttnDkSlots = 256;
 constexpr int kAttnFwdPieceSteps = 8;
 constexpr int kAttnGradPieceSteps = 4;
 
-// tile descriptor: {sequence, first row, first step, last step + 1, slot of its sums, pieces, 0, 0}
+// A plan with a window: a query tile (or a sequence of the split form) walks blocks of the sinks alone and, behind them,
+// blocks from the first key of its first query's window on; keys are counted through both.
+
+// tile descriptor: {sequence, first row, first step, last step + 1, slot of its sums, pieces, x, y}
+// query tiles: x keys' worth of sinks' blocks, y to be added to the count of a key behind them; key tiles: x one past the
+// last query
 constexpr int kAttnTileWords = 8;
 
 // split form descriptor: {q_start, q_len, k_start, k_len, first row, pieces, slot (join: the first one's), first key,
-// last key + 1, 0, 0, 0}.  The sequence's fields stand in the item: short calls wait for every load that
+// last key + 1, the tiles' x and y, 0}.  The sequence's fields stand in the item: short calls wait for every load that
 // another one's address depends on.
 constexpr int kAttnSplitWords = 12;
 
@@ -77,6 +82,8 @@ struct AttnLayout {
 
 struct dsv_attn_plan {
   int32_t n_seqs = 0, n_q = 0, n_kv = 0, hq = 0, hkv = 0, d = 0;
+  bool windowed = false;  // some key that causality leaves is hidden by the window
+  int32_t window = 0, sinks = 0;
   int64_t train_q = 0, train_k = 0;
   int32_t n_fwd = 0, n_fwd_join = 0, fwd_slots = 0, n_dk_join = 0, dk_slots = 0;  // *_slots: pieces with sums of their own
   int32_t n_dq_join = 0, dq_slots = 0;
