@@ -743,6 +743,39 @@ int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const 
                         float* loss, void* dX, int32_t lddx, void* workspace, size_t workspace_bytes,
                         void* hip_stream);
 
+/*
+ * Distillation: how far the student's softmax over the vocabulary is from a teacher that
+ * gives its k largest logits a row, and the gradient that reaches the rows.  For row x
+ * with entries (id_j, t_j), j < k, and temperature tau:
+ *     q = softmax(t / tau) over the entries,   p = softmax(x W^T / tau)
+ *     loss = sum_j q_j (log q_j - log p_{id_j})
+ *     dx   = weight / tau (sum_v p_v W_v - sum_j q_j W_{id_j})
+ * (the Kullback-Leibler divergence of p from q; the factor tau^2 that keeps gradients of
+ * different temperatures alike is the caller's, in weight).  An id outside [0, V) is no
+ * entry (padding); a teacher logit of -infinity is an entry of q = 0.  A row without an
+ * entry of q > 0 has loss 0 and dx zeros, whatever it holds.  The same id twice: two
+ * entries, each with its q.  The cross entropy's conventions hold else: the logits are
+ * never held whole, shapes, strides, alignment, Wt, and its workspace but for the entries'
+ * room.  The student's terms at the teacher's ids are formed apart in fp32 or more, so in
+ * bf16 mode dX keeps its accuracy where student and teacher agree; the others are rounded
+ * to bf16 once.  No atomics: repeated calls give the same bits.
+ *
+ * ids [T][k] int32 and teacher [T][k] fp32, dense, 4-byte aligned; 1 <= k <= 1024
+ * (DSV_ERR_SIZE).  temperature positive and finite, as are 1 / tau and, in fp32, log2 e /
+ * tau (DSV_ERR_RANGE).  Other errors as dsv_vocab_loss and dsv_vocab_loss_grad.
+ */
+int dsv_vocab_distill_workspace(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_t k, int32_t ldw, int32_t grad,
+                                size_t* bytes);
+/* The losses alone: the head is read once. */
+int dsv_vocab_distill(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_t k, const void* X, int32_t ldx, const void* W,
+                      int32_t ldw, const int32_t* ids, const float* teacher, double temperature, float* loss,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Losses (NULL: not written) and dX.  weight NULL: ones; the losses are not multiplied by it. */
+int dsv_vocab_distill_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_t k, const void* X, int32_t ldx,
+                           const void* W, int32_t ldw, const void* Wt, int32_t ldwt, const int32_t* ids,
+                           const float* teacher, double temperature, const float* weight, float* loss, void* dX,
+                           int32_t lddx, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static description of a status code. */
 const char* dsv_status_string(int status);
 

@@ -14,7 +14,8 @@ struct VocabArgs {
   const void* W;
   const void* Wt;         // nullptr: the second product reads W
   int64_t ldx, ldw, ldwt, lddx;
-  const int32_t* target;
+  float c;                // log2 e over the temperature: exponents are c z
+  const int32_t* target;  // nullptr: no row has one (distillation)
   const float* weight;    // nullptr: ones
   float* loss;            // nullptr: not written
   void* dX;
@@ -31,6 +32,14 @@ struct VocabArgs {
   float* others;          // [T] sum of the terms that are not the target's, at the reference
   float* term;            // [T] the target's term at the reference (after the last piece)
   float* alpha;           // [T] what the sums so far are multiplied by (the reference moved)
+  // Distillation: k entries a row, [T][k] each, and what the rows' sums of them come to.
+  const int32_t* ids;
+  const float* teacher;
+  int32_t k;
+  double inv_tau;
+  double* exponent;       // c z of the entry, -infinity where it is none or its token stands at an earlier one too
+  float* share;           // the teacher's probability of it
+  double* base;           // [T] sum of share (log2 share - c z)
   // second product: contraction in `split` ranges of split_len columns, each with its own sums
   float* O;               // [split][T][K]
   int32_t split, split_len;

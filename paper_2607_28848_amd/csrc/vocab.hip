@@ -23,7 +23,9 @@
 namespace dsv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxEntries = 1024;  // of a teacher, a row
+
+constexpr double kLog2e = 1.4426950408889634;
 
 __device__ __forceinline__ float quad_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -109,10 +111,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
     for (int h = 0; h < 2; ++h) {
       const int i = 2 * t + h, r = wm * WM + 16 * i + l15, row = m0 + r;
       const bool in = row < a.T;
-      const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
+      const float m = fmaxf(red[0][0][r], red[0][1][r]) * a.c;
       const float have = !a.first && in ? a.ref[row] : 0.f;
       const float ref = tile_reference(m, have, a.first), base = ref == -INFINITY ? 0.f : ref;
-      const int tc = in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
+      const int tc = in && a.target ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const float z = acc[i][j][v];
-          e[v] = __builtin_amdgcn_exp2f(z * kLog2e - base);
+          e[v] = __builtin_amdgcn_exp2f(z * a.c - base);
           if (tc == 16 * j + v) e[v] = 0.f;
           if (cols < TN && c0 + 16 * j + v >= cols) e[v] = 0.f;
           sum += e[v];
@@ -262,12 +264,13 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
 // reference are brought to the row's.  After the last piece the target's logit, its term and the loss, in 64 bits: the
 // logarithm and the logit nearly cancel for a sure row, and there is one of each per row (one row against 128256 of
 // 4096: the loss is off by 8e-7 in the root mean square with the logit from the products, whose sums are fp32).
-template <typename T>
+// KD (distillation): no target, the row's loss from what vocab_teacher left, and the entries' terms out of P.
+template <typename T, bool KD>
 __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   __shared__ float red[4];
   __shared__ double red64[4];
   const int row = blockIdx.x;
-  const int target = a.last ? a.target[row] : -1;
+  const int target = !KD && a.last ? a.target[row] : -1;
   const bool has = target >= 0 && target < a.V;
   double zt = 0.;
   if (has) {
@@ -301,7 +304,10 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     a.others[row] = others;
     a.ref[row] = ref;
     a.alpha[row] = f;
-    if (a.last) {
+    if (KD && a.last) {
+      if (a.loss)
+        a.loss[row] = a.term[row] == 0.f ? 0.f : (float)((a.base[row] + log2((double)others) + ref) * 0.69314718055994531);
+    } else if (a.last) {
       const double et = has ? exp2(zt * 1.4426950408889634 - ref) : 1.;
       a.term[row] = (float)et;
       // near 0 the loss keeps its relative accuracy
@@ -311,10 +317,11 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
                                      : (float)(log(others + et) + ref * 0.69314718055994531 - zt);
     }
   }
-  if (!a.grad || !__syncthreads_or(moved)) return;
+  if (!a.grad) return;
   T* P = static_cast<T*>(a.P) + (int64_t)row * a.ldp;
   constexpr int E = 16 / sizeof(T);
-  for (int64_t c = threadIdx.x * E; c < (int64_t)a.n_ct * a.tw; c += 256 * E) {
+  const bool scale = __syncthreads_or(moved);
+  for (int64_t c = threadIdx.x * E; scale && c < (int64_t)a.n_ct * a.tw; c += 256 * E) {
     const float r = st[c / a.tw].x;
     if (r == ref || r == -INFINITY) continue;
     const float f = ldexpf(1.f, (int)fmaxf(r - ref, -1000.f));  // both are whole numbers, ref the larger one
@@ -327,6 +334,92 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
         v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
     }
     *reinterpret_cast<u32x4*>(P + c) = v;
+  }
+  if constexpr (KD) {
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.k; j += 256) {
+      const uint32_t at = (uint32_t)(a.ids[(int64_t)row * a.k + j] - a.v0);
+      if (at < (uint32_t)a.vn) P[at] = 0;
+    }
+  }
+}
+
+// ---- distillation -----------------------------------------------------------------------------------------
+// The entries of a row: the student's logits at their tokens, as products of the row with the head's rows, and the
+// teacher's probabilities (its softmax over the entries), in 64 bits from 8 products on.  The student's term of an entry
+// is kept out of P and formed from these, so that where student and teacher agree their difference, not bf16's rounding
+// of both, is what reaches dX.  A wave takes four entries at a time, whose head rows are read side by side.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_teacher_kernel(VocabArgs a) {
+  __shared__ int32_t ids[kMaxEntries];
+  __shared__ double ex[kMaxEntries];
+  __shared__ bool again[kMaxEntries];  // the token stands at an earlier entry too
+  __shared__ double red[4];
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const double c = a.inv_tau * kLog2e;
+  double top = -INFINITY;
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    const int id = a.ids[row * a.k + j];
+    ids[j] = (uint32_t)id < (uint32_t)a.V ? id : -1;
+    const double t = ids[j] < 0 ? -INFINITY : (double)a.teacher[row * a.k + j] * c;
+    ex[j] = t;
+    top = fmax(top, t);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+  if (lane == 0) red[wave] = top;
+  __syncthreads();
+  top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+  __syncthreads();
+  double mass = 0.;
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    if (ids[j] >= 0) mass += ex[j] == -INFINITY ? 0. : exp2(ex[j] - top);
+    bool seen = false;
+    for (int i = 0; i < j; ++i) seen |= ids[i] == ids[j];
+    again[j] = seen;
+  }
+  mass = block_sum<4>(mass, red);
+  __syncthreads();
+  const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+  double sum = 0.;
+  for (int j0 = 4 * wave; j0 < a.k; j0 += 16) {
+    const T* w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = static_cast<const T*>(a.W) + max(j0 + e < a.k ? ids[j0 + e] : -1, 0) * a.ldw;
+    double z[4] = {0., 0., 0., 0.};
+    for (int at = 8 * lane; at < a.K; at += 512) {
+      float xs[8], ws[4][8];
+      load8(x + at, xs);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) load8(w[e] + at, ws[e]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part += xs[i] * ws[e][i];
+        z[e] += part;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) z[e] += __shfl_xor(z[e], d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + e;
+      if (lane != e || j >= a.k) continue;
+      const bool is = ids[j] >= 0;
+      const double q = !is || ex[j] == -INFINITY ? 0. : exp2(ex[j] - top) / mass;
+      a.share[row * a.k + j] = (float)q;
+      a.exponent[row * a.k + j] = is && !again[j] ? z[e] * c : -INFINITY;
+      if (q != 0.) sum += q * ((ex[j] - top - log2(mass)) - z[e] * c);
+    }
+  }
+  sum = block_sum<4>(sum, red);
+  if (threadIdx.x == 0) {
+    a.base[row] = sum;
+    a.term[row] = mass == 0. ? 0.f : 1.f;
   }
 }
 
@@ -359,6 +452,46 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(VocabArgs a) {
     }
     store4(dx + c, x);
   }
+}
+
+// dx = weight / temperature (sum of the terms kept in P over their total + sum_j (p_j - share_j) W_j), 1024 columns a
+// workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_kd_finish_kernel(VocabArgs a) {
+  __shared__ float coef[kMaxEntries];
+  __shared__ int32_t ids[kMaxEntries];
+  __shared__ int32_t count;
+  const int64_t row = blockIdx.x;
+  const bool has = a.term[row] != 0.f;
+  const float total = a.others[row], ref = a.ref[row], f = (float)((a.weight ? a.weight[row] : 1.f) * a.inv_tau);
+  // the entries that are some, in order, by the first wave
+  if (threadIdx.x < 64) {
+    int n = 0;
+    for (int j0 = 0; j0 < a.k; j0 += 64) {
+      const int j = j0 + threadIdx.x, id = j < a.k ? a.ids[row * a.k + j] : -1;
+      const bool is = (uint32_t)id < (uint32_t)a.V;
+      const uint64_t which = __builtin_amdgcn_ballot_w64(is);
+      if (is) {
+        const int at = n + __builtin_popcountll(which & ((1ull << threadIdx.x) - 1));
+        ids[at] = id;
+        coef[at] = exp2f((float)(a.exponent[row * a.k + j] - ref)) / total - a.share[row * a.k + j];
+      }
+      n += __builtin_popcountll(which);
+    }
+    if (threadIdx.x == 0) count = n;
+  }
+  __syncthreads();
+  const int c = 1024 * blockIdx.y + 4 * threadIdx.x, n = has ? count : 0;
+  if (c >= a.K) return;
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (has) {
+#pragma unroll 4
+    for (int s = 0; s < a.split; ++s) x += *reinterpret_cast<const f32x4*>(a.O + ((int64_t)s * a.T + row) * a.K + c);
+    x *= 1.f / total;
+  }
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) x += load4(static_cast<const T*>(a.W) + ids[j] * a.ldw + c) * coef[j];
+  store4(static_cast<T*>(a.dX) + row * a.lddx + c, has ? x * f : x);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -492,12 +625,26 @@ hipError_t launch_grad(const VocabArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Room of a distillation's entries behind the pieces'.
+struct Entries {
+  size_t exponent, base, share, total;
+};
+Entries entries(size_t from, int32_t T, int32_t k) {
+  Entries e{};
+  e.exponent = align256(from);
+  e.base = align256(e.exponent + (size_t)T * k * sizeof(double));
+  e.share = align256(e.base + (size_t)T * sizeof(double));
+  e.total = align256(e.share + (size_t)T * k * sizeof(float));
+  return e;
+}
+
 int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
-  const bool bf = dt == DSV_BF16;
+  const bool bf = dt == DSV_BF16, kd = a.k > 0;
   const int cus = device_cus();
   const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, cus);
+  const Entries en = entries(pc.total, a.T, a.k);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
-  if (ws_bytes < pc.total) return DSV_ERR_SIZE;
+  if (ws_bytes < (kd ? en.total : pc.total)) return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
   char* b = static_cast<char*>(ws);
   a.P = a.grad ? b + pc.p : nullptr;
@@ -511,6 +658,14 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   a.O = reinterpret_cast<float*>(b + pc.o);
   a.tw = pc.tw;
   a.split_len = pc.split_len;
+  if (kd) {
+    a.exponent = reinterpret_cast<double*>(b + en.exponent);
+    a.base = reinterpret_cast<double*>(b + en.base);
+    a.share = reinterpret_cast<float*>(b + en.share);
+    if (bf) hipLaunchKernelGGL(vocab_teacher_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(vocab_teacher_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return DSV_ERR_DEVICE;
+  }
   for (int i = 0; i < pc.n; ++i) {
     a.v0 = i * pc.width;
     a.vn = std::min(pc.width, a.V - a.v0);
@@ -520,16 +675,22 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.split = pc.split;
     hipError_t e = !bf ? launch_vocab_f32_logits(a, cus, s) : a.grad ? launch_logits<true>(a, cus, s) : launch_logits<false>(a, cus, s);
     if (e != hipSuccess) return DSV_ERR_DEVICE;
-    if (bf) hipLaunchKernelGGL(vocab_fold_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(vocab_fold_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
+    const dim3 rows((unsigned)a.T);
+    if (kd && bf) hipLaunchKernelGGL((vocab_fold_kernel<uint16_t, true>), rows, dim3(256), 0, s, a);
+    else if (kd) hipLaunchKernelGGL((vocab_fold_kernel<float, true>), rows, dim3(256), 0, s, a);
+    else if (bf) hipLaunchKernelGGL((vocab_fold_kernel<uint16_t, false>), rows, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((vocab_fold_kernel<float, false>), rows, dim3(256), 0, s, a);
     if (hipGetLastError() != hipSuccess) return DSV_ERR_DEVICE;
     if (!a.grad) continue;
     e = bf ? launch_grad(a, s) : launch_vocab_f32_grad(a, s);
     if (e != hipSuccess) return DSV_ERR_DEVICE;
   }
   if (!a.grad) return DSV_OK;
-  if (bf) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, dim3((unsigned)a.T, (a.K + 1023) / 1024), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(vocab_finish_kernel<float>, dim3((unsigned)a.T, (a.K + 1023) / 1024), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)a.T, (a.K + 1023) / 1024);
+  if (kd && bf) hipLaunchKernelGGL(vocab_kd_finish_kernel<uint16_t>, grid, dim3(256), 0, s, a);
+  else if (kd) hipLaunchKernelGGL(vocab_kd_finish_kernel<float>, grid, dim3(256), 0, s, a);
+  else if (bf) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(vocab_finish_kernel<float>, grid, dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? DSV_OK : DSV_ERR_DEVICE;
 }
 
@@ -558,6 +719,7 @@ extern "C" int dsv_vocab_loss(dsv_dtype dt, int32_t T, int32_t K, int32_t V, con
   if (!aligned(W, 16) || (T > 0 && (!aligned(X, 16) || !aligned(target, 4) || !aligned(loss, 4)))) return DSV_ERR_ARG;
   a.T = T, a.K = K, a.V = V;
   a.X = X, a.W = W, a.target = target, a.loss = loss;
+  a.c = (float)kLog2e;
   return run(a, dt, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -580,6 +742,72 @@ extern "C" int dsv_vocab_loss_grad(dsv_dtype dt, int32_t T, int32_t K, int32_t V
   a.T = T, a.K = K, a.V = V;
   a.X = X, a.W = W, a.Wt = use_t ? Wt : nullptr;
   a.target = target, a.weight = weight, a.loss = loss, a.dX = dX;
+  a.c = (float)kLog2e;
+  a.grad = 1;
+  return run(a, dt, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+namespace {
+
+// The entries' and the temperature's checks.
+int check_teacher(int32_t T, int32_t k, double tau, const int32_t* ids, const float* teacher, VocabArgs* a) {
+  if (k < 1 || k > kMaxEntries) return DSV_ERR_SIZE;
+  const float c = (float)(kLog2e / tau);  // what the logits are multiplied with
+  if (!std::isfinite(tau) || !(tau > 0) || !std::isnormal(c) || !std::isfinite(1 / tau)) return DSV_ERR_RANGE;
+  if (T > 0 && (!aligned(ids, 4) || !aligned(teacher, 4))) return DSV_ERR_ARG;
+  a->ids = ids, a->teacher = teacher, a->k = k;
+  a->inv_tau = 1 / tau;
+  a->c = c;
+  return DSV_OK;
+}
+
+}  // namespace
+
+extern "C" int dsv_vocab_distill_workspace(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t k, int32_t ldw,
+                                           int32_t grad, size_t* bytes) {
+  if (!bytes) return DSV_ERR_ARG;
+  int64_t w = 0;
+  const int rc = check_shape(dt, T, K, V, ldw, &w);
+  if (rc != DSV_OK) return rc;
+  if (k < 1 || k > kMaxEntries) return DSV_ERR_SIZE;
+  *bytes = entries(pieces(dt, T, K, V, w, grad != 0, device_cus()).total, T, k).total;
+  return DSV_OK;
+}
+
+extern "C" int dsv_vocab_distill(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t k, const void* X, int32_t ldx,
+                                 const void* W, int32_t ldw, const int32_t* ids, const float* teacher, double temperature,
+                                 float* loss, void* ws, size_t ws_bytes, void* hip_stream) {
+  VocabArgs a{};
+  int rc = check_shape(dt, T, K, V, ldw, &a.ldw);
+  if (rc == DSV_OK) rc = stride(ldx, K, &a.ldx);
+  if (rc == DSV_OK) rc = check_teacher(T, k, temperature, ids, teacher, &a);
+  if (rc != DSV_OK) return rc;
+  if (!aligned(W, 16) || (T > 0 && (!aligned(X, 16) || !aligned(loss, 4)))) return DSV_ERR_ARG;
+  a.T = T, a.K = K, a.V = V;
+  a.X = X, a.W = W, a.loss = loss;
+  return run(a, dt, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int dsv_vocab_distill_grad(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t k, const void* X, int32_t ldx,
+                                      const void* W, int32_t ldw, const void* Wt, int32_t ldwt, const int32_t* ids,
+                                      const float* teacher, double temperature, const float* weight, float* loss, void* dX,
+                                      int32_t lddx, void* ws, size_t ws_bytes, void* hip_stream) {
+  VocabArgs a{};
+  int rc = check_shape(dt, T, K, V, ldw, &a.ldw);
+  if (rc == DSV_OK) rc = stride(ldx, K, &a.ldx);
+  if (rc == DSV_OK) rc = stride(lddx, K, &a.lddx);
+  bool use_t = Wt && dt == DSV_BF16 && (V & 7) == 0;
+  if (rc == DSV_OK && use_t) rc = stride(ldwt, V, &a.ldwt);
+  use_t = use_t && 256 * 2 * a.ldwt < (int64_t)1 << 31;  // tile_nt's offsets over a tile's 256 rows
+  if (rc == DSV_OK) rc = check_teacher(T, k, temperature, ids, teacher, &a);
+  if (rc != DSV_OK) return rc;
+  if (!aligned(W, 16) || (use_t && !aligned(Wt, 16)) || (reinterpret_cast<uintptr_t>(weight) & 3) ||
+      (reinterpret_cast<uintptr_t>(loss) & 3))
+    return DSV_ERR_ARG;
+  if (T > 0 && (!aligned(X, 16) || !aligned(dX, 16))) return DSV_ERR_ARG;
+  a.T = T, a.K = K, a.V = V;
+  a.X = X, a.W = W, a.Wt = use_t ? Wt : nullptr;
+  a.weight = weight, a.loss = loss, a.dX = dX;
   a.grad = 1;
   return run(a, dt, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
 }

@@ -16,7 +16,6 @@
 namespace dsv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStage = kRingStage<2, 4>;
 
 // out[m][n] = sum_c P[m][c] Q[c][n] of a tile of 32 FM rows and 128 columns: tile_ring's loop with three buffers, and with
@@ -163,17 +162,17 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   for (int i = 0; i < FM; ++i) {
     const int r = WM * wm + 16 * i + l15, row = m0 + r;
     const bool in = row < a.T;
-    const float m = fmaxf(red[0][0][r], red[0][1][r]) * kLog2e;
+    const float m = fmaxf(red[0][0][r], red[0][1][r]) * a.c;
     const float have = !a.first && in ? a.ref[row] : 0.f;
     ref[i] = tile_reference(m, have, a.first);
     const float base = ref[i] == -INFINITY ? 0.f : ref[i];
-    const int t = in ? a.target[row] - a.v0 - n0 - c0 : -1;
+    const int t = in && a.target ? a.target[row] - a.v0 - n0 - c0 : -1;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        float e = exp2f(acc[i][j][v] * kLog2e - base);
+        float e = exp2f(acc[i][j][v] * a.c - base);
         if (t == 16 * j + v) e = 0.f;
         sum += e;
         acc[i][j][v] = e;
