@@ -68,12 +68,19 @@ def on(stream):
 def here(*tensors):
     """ValueError unless the tensors (None: not given) are on one device, the current one where it is a GPU: a call's
     kernels run there."""
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) > 1:
-        raise ValueError("the tensors of a call are on several devices: %s" % sorted(map(str, devices)))
-    for d in devices:
-        if d.type == "cuda" and d.index != torch.cuda.current_device():
-            raise ValueError("the tensors are on %s, the current device is cuda:%d" % (d, torch.cuda.current_device()))
+    at = None
+    for t in tensors:
+        if t is None:
+            continue
+        d = t.get_device()  # -1: no GPU's
+        if d < 0 and t.is_meta:
+            raise ValueError("a tensor of the call has no memory")
+        if at is None:
+            at = d
+        elif d != at:
+            raise ValueError("the tensors of a call are on several devices: %s" % sorted({str(t.device) for t in tensors if t is not None}))
+    if at is not None and at >= 0 and at != torch.cuda.current_device():
+        raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (at, torch.cuda.current_device()))
 
 
 def made(given, shape, dtype, like, stream):

@@ -963,6 +963,7 @@ struct Workspace {
 // fp32 key tiles of short batches are fewer than the CUs: the query heads of a key head are then divided among so many
 // workgroups.
 int f32_parts(const dsv_attn_plan& p) {
+  if (p.windowed) return p.hq / p.hkv;  // the sinks' tile has every query, the others the window's
   const int64_t tiles = std::max<int64_t>(1, (int64_t)p.n_f32_dk * p.hkv);
   return (int)std::min<int64_t>(p.hq / p.hkv, (kAttnDkSlots + tiles - 1) / tiles);
 }

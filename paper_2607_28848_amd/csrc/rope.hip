@@ -293,6 +293,7 @@ __global__ __launch_bounds__(256) void rope_weight_kernel(RopeArgs a) {
   __shared__ double red[16][17];
   const int col = blockIdx.x * 16 + (threadIdx.x & 15), range = threadIdx.x >> 4;
   double x = 0.;
+#pragma unroll 16
   for (int g = range; g < a.groups; g += 16) x += (double)a.part[(int64_t)g * 2 * D + col];
   red[range][threadIdx.x & 15] = x;
   __syncthreads();

@@ -12,10 +12,11 @@ broadcast ones; outputs may be the inputs themselves.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import dsv
 from .attn import View, _code, _view, here, int32, made
-from .dsv import _check, _stream_handle, torch
+from .dsv import OK, _check, _stream_handle, torch
 
 _lib = dsv.lib_handle()
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
@@ -36,9 +37,12 @@ _lib.dsv_rope_fwd.restype = ctypes.c_int
 _lib.dsv_rope_bwd.argtypes = [ctypes.c_int, _ropep, _i32, _vp] + [_viewp] * 6 + [_vp, _vp, _vp, _sz, _vp]
 _lib.dsv_rope_bwd.restype = ctypes.c_int
 
-# The calls below pass their views as packed bytes, read during the call only, as the attention's do.
-_fwd = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_int, _ropep, *[_vp] * 4, _i32, *[_vp] * 4)(("dsv_rope_fwd", _lib))
-_bwd = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_int, _ropep, _i32, *[_vp] * 10, _sz, _vp)(("dsv_rope_bwd", _lib))
+# The calls below pass their structures as packed bytes, read during the call only, as the attention's do: the rotation of
+# a decode step takes the GPU 3 us, and marshalling structures takes the host several times that.
+_fwd = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_int, *[_vp] * 5, _i32, *[_vp] * 4)(("dsv_rope_fwd", _lib))
+_bwd = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_int, _vp, _i32, *[_vp] * 10, _sz, _vp)(("dsv_rope_bwd", _lib))
+_ROPE_PACK = struct.Struct("@6id4P").pack
+assert len(_ROPE_PACK(*[0] * 6, 0.0, *[0] * 4)) == ctypes.sizeof(Rope)
 
 
 def frequencies(rotated: int, theta: float = 10000.0, device=None):
@@ -47,9 +51,10 @@ def frequencies(rotated: int, theta: float = 10000.0, device=None):
 
 
 def _vec(t, n: int, dtype, name: str):
+    """The address of a vector, 0 for none."""
     if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+        return 0
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %d elements" % (name, dtype, n))
     return t.data_ptr()
 
@@ -60,12 +65,13 @@ def _heads(t, name: str):
     return t.shape
 
 
-def _rope(n, hq, hkv, d, pos, freq, q_weight, k_weight, eps, interleaved) -> Rope:
+def _rope(n, hq, hkv, d, pos, freq, q_weight, k_weight, eps, interleaved) -> bytes:
     rotated = 0 if freq is None else 2 * freq.shape[0]
-    int32(n=n, heads_q=hq, heads_kv=hkv, head_dim=d, rotated=rotated)
-    return Rope(n, hq, hkv, d, rotated, 1 if interleaved else 0, eps, None if freq is None else _vec(pos, n, torch.int32, "pos"),
-                _vec(freq, rotated // 2, torch.float64, "freq"), _vec(q_weight, d, torch.float32, "q_weight"),
-                _vec(k_weight, d, torch.float32, "k_weight"))
+    if n >= 1 << 31 or max(hq, hkv, d, rotated) >= 1 << 31:
+        int32(n=n, heads_q=hq, heads_kv=hkv, head_dim=d, rotated=rotated)
+    return _ROPE_PACK(n, hq, hkv, d, rotated, 1 if interleaved else 0, eps,
+                      0 if freq is None else _vec(pos, n, torch.int32, "pos"), _vec(freq, rotated // 2, torch.float64, "freq"),
+                      _vec(q_weight, d, torch.float32, "q_weight"), _vec(k_weight, d, torch.float32, "k_weight"))
 
 
 def workspace_bytes(n_rows: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
@@ -100,12 +106,17 @@ def fwd(Q, K, pos, freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=Fal
     if V is not None:
         V_out = made(V_out, (n, hkv, d), dt, V, stream)
     rows = n if slots is None else K_out.shape[0]
+    if rows >= 1 << 31:
+        int32(n_slots=rows)
     r = _rope(n, hq, hkv, d, pos, freq, q_weight if hq else None, k_weight if hkv else None, eps, interleaved)
-    _check(_fwd(_code(dt), r, Q if Q is None else _view(Q, n, hq, d, dt, "Q"), K if K is None else _view(K, n, hkv, d, dt, "K"),
-                V if V is None else _view(V, n, hkv, d, dt, "V"), _vec(slots, n, torch.int32, "slots"),
-                *int32(rows=rows), Q_out if Q is None else _view(Q_out, n, hq, d, dt, "Q_out"),
-                K_out if K is None else _view(K_out, rows, hkv, d, dt, "K_out"),
-                V_out if V is None else _view(V_out, rows, hkv, d, dt, "V_out"), _stream_handle(stream)), "dsv_rope_fwd")
+    rc = _fwd(_code(dt), r, None if Q is None else _view(Q, n, hq, d, dt, "Q"),
+              None if K is None else _view(K, n, hkv, d, dt, "K"), None if V is None else _view(V, n, hkv, d, dt, "V"),
+              None if slots is None else _vec(slots, n, torch.int32, "slots"), rows,
+              None if Q is None else _view(Q_out, n, hq, d, dt, "Q_out"),
+              None if K is None else _view(K_out, rows, hkv, d, dt, "K_out"),
+              None if V is None else _view(V_out, rows, hkv, d, dt, "V_out"), _stream_handle(stream))
+    if rc != OK:
+        _check(rc, "dsv_rope_fwd")
     return (Q_out, K_out) if V is None else (Q_out, K_out, V_out)
 
 
@@ -140,11 +151,14 @@ def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=No
     def view(t, rows, heads, name):
         return None if t is None else _view(t, rows, heads, d, dt, name)
 
-    _check(_bwd(_code(dt), r, *int32(rows=m), _vec(rows, m, torch.int32, "rows"), view(dQ, m, hq, "dQ"),
-                view(dK, m, hkv, "dK"), view(Q, n, hq, "Q") if hq and q_weight is not None else None,
-                view(K, n, hkv, "K") if hkv and k_weight is not None else None,
-                view(dQ_out, m, hq, "dQ_out") if hq else None, view(dK_out, m, hkv, "dK_out") if hkv else None,
-                _vec(dq_weight, d, torch.float32, "dq_weight"), _vec(dk_weight, d, torch.float32, "dk_weight"),
-                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                _stream_handle(stream)), "dsv_rope_bwd")
+    if m >= 1 << 31:
+        int32(n_rows=m)
+    rc = _bwd(_code(dt), r, m, None if rows is None else _vec(rows, m, torch.int32, "rows"), view(dQ, m, hq, "dQ"),
+              view(dK, m, hkv, "dK"), view(Q, n, hq, "Q") if hq and q_weight is not None else None,
+              view(K, n, hkv, "K") if hkv and k_weight is not None else None, view(dQ_out, m, hq, "dQ_out") if hq else None,
+              view(dK_out, m, hkv, "dK_out") if hkv else None, _vec(dq_weight, d, torch.float32, "dq_weight"),
+              _vec(dk_weight, d, torch.float32, "dk_weight"), None if workspace is None else workspace.data_ptr(),
+              0 if workspace is None else workspace.nbytes, _stream_handle(stream))
+    if rc != OK:
+        _check(rc, "dsv_rope_bwd")
     return dQ_out if hq else None, dK_out if hkv else None, dq_weight, dk_weight
