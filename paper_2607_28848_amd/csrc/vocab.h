@@ -15,7 +15,7 @@ struct VocabArgs {
   const void* Wt;         // nullptr: the second product reads W
   int64_t ldx, ldw, ldwt, lddx;
   float c;                // log2 e over the temperature: exponents are c z
-  const int32_t* target;  // nullptr: no row has one (distillation)
+  const int32_t* target;
   const float* weight;    // nullptr: ones
   float* loss;            // nullptr: not written
   void* dX;
@@ -36,6 +36,7 @@ struct VocabArgs {
   const int32_t* ids;
   const float* teacher;
   int32_t k;
+  int32_t n_entry;        // workgroups of entry_exponents ahead of the launch's tiles
   double inv_tau;
   double* exponent;       // c z of the entry, -infinity where it is none or its token stands at an earlier one too
   float* share;           // the teacher's probability of it
@@ -44,6 +45,10 @@ struct VocabArgs {
   float* O;               // [split][T][K]
   int32_t split, split_len;
 };
+
+// Distillation: the most entries a row, and how many of them a workgroup takes.
+constexpr int kMaxEntries = 1024, kEntryGroup = 16;
+__host__ __device__ inline int entry_groups(int k) { return (k + kEntryGroup - 1) / kEntryGroup; }
 
 // References.  A row starts at 0, and a tile of the first piece takes its own maximum (m, base 2) where it lies
 // further than kVocabSlack from that on either side; in later pieces where it exceeds the row's reference by

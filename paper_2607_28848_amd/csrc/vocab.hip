@@ -19,11 +19,11 @@
 #include "dsv.h"
 #include "gemm_tile.h"
 #include "vocab.h"
+#include "vocab_entries.h"
 
 namespace dsv {
 namespace {
 
-constexpr int kMaxEntries = 1024;  // of a teacher, a row
 
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -40,16 +40,20 @@ __device__ __forceinline__ float quad_sum(float x) {
 // GRAD: P is written.  Tiles of 32 FM rows and 32 FN columns; NB: buffers (2: tile_nt, else tile_ring).  Up to 128 rows
 // the stream of a large head is what bounds it: one row against 128256 of 4096 takes 185 us with the fold, 5.7 TB/s, 128 rows 206.
 // Else the matrix core: 4096 rows, 32256 x 8192 a piece, 1.61 ms (1340 TFLOP/s).
-template <bool GRAD, int FM, int FN, int NB>
+template <bool GRAD, int FM, int FN, int NB, bool KD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 ? 1 : 2))) void vocab_logits_kernel(VocabArgs a) {
   constexpr int WM = 16 * FM, TM = 2 * WM, WN = 16 * FN, TN = 2 * WN;
   constexpr int kStage = NB == 2 ? kTileStage : kRingStage<FM, FN>;
   __shared__ __attribute__((aligned(1024))) char smem0[kStage];
   __shared__ __attribute__((aligned(1024))) char smem1[kStage];
   __shared__ float red[3][2][TM];  // [maximum, sum, reference][column half][row]
-  const int n_m = (a.T + TM - 1) / TM;
+  const int n_m = (a.T + TM - 1) / TM, ahead = KD ? a.n_entry : 0;
+  if (KD && (int)blockIdx.x < ahead) {
+    entry_exponents<uint16_t>(a, blockIdx.x);
+    return;
+  }
   int mt, nt;
-  tile_at(tile_of(blockIdx.x, gridDim.x), n_m, a.n_ct, mt, nt);
+  tile_at(tile_of(blockIdx.x - ahead, gridDim.x - ahead), n_m, a.n_ct, mt, nt);
   const int m0 = mt * TM, n0 = nt * TN, cols = min(TN, a.vn - n0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, l15 = lane & 15, g4 = lane >> 4;
@@ -114,7 +118,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
       const float m = fmaxf(red[0][0][r], red[0][1][r]) * a.c;
       const float have = !a.first && in ? a.ref[row] : 0.f;
       const float ref = tile_reference(m, have, a.first), base = ref == -INFINITY ? 0.f : ref;
-      const int tc = in && a.target ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
+      const int tc = !KD && in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
@@ -245,18 +249,52 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
   return x;
 }
 
-// Eight values from p on.
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+// entry_exponents in a launch of its own.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a) {
+  entry_exponents<T>(a, blockIdx.x);
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+
+// The teacher's shares of a row's entries (its softmax over them, in 64 bits), what the loss takes from them, and each
+// token's exponent at its first entry alone.
+__device__ __forceinline__ void teacher_row(const VocabArgs& a, int64_t row, double* red) {
+  __shared__ int32_t ids[kMaxEntries];
+  const double c = a.inv_tau * kLog2e;
+  const float* teacher = a.teacher + row * a.k;
+  double* exponent = a.exponent + row * a.k;
+  // an entry's logit, -infinity where it is none
+  auto logit = [&](int j) { return ids[j] < 0 ? -INFINITY : teacher[j] * c; };
+  double top = -INFINITY;
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    const int id = a.ids[row * a.k + j];
+    ids[j] = (uint32_t)id < (uint32_t)a.V ? id : -1;
+    top = fmax(top, logit(j));
+  }
 #pragma unroll
-  for (int i = 0; i < 8; i += 4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+  __syncthreads();
+  auto term = [&](int j) { const double t = logit(j); return t == -INFINITY ? 0. : exp2(t - top); };
+  double mass = 0.;
+  for (int j = threadIdx.x; j < a.k; j += 256) mass += term(j);
+  mass = block_sum<4>(mass, red);
+  __syncthreads();
+  double sum = 0.;
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    const double e = term(j), q = e == 0. ? 0. : e / mass;
+    a.share[row * a.k + j] = (float)q;
+    if (q != 0.) sum += q * ((logit(j) - top - log2(mass)) - exponent[j]);
+    bool again = false;
+    for (int i = 0; i < j; ++i) again |= ids[i] == ids[j];
+    if (again) exponent[j] = -INFINITY;
+  }
+  sum = block_sum<4>(sum, red);
+  if (threadIdx.x == 0) {
+    a.base[row] = sum;
+    a.term[row] = mass == 0. ? 0.f : 1.f;
   }
 }
 
@@ -264,10 +302,10 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
 // reference are brought to the row's.  After the last piece the target's logit, its term and the loss, in 64 bits: the
 // logarithm and the logit nearly cancel for a sure row, and there is one of each per row (one row against 128256 of
 // 4096: the loss is off by 8e-7 in the root mean square with the logit from the products, whose sums are fp32).
-// KD (distillation): no target, the row's loss from what vocab_teacher left, and the entries' terms out of P.  Where P holds
-// the terms as they were summed (fp32), the entries' are taken out of the sum as well and the ones from vocab_teacher put
-// in: a sure row's total and its largest term then have the same error, which drops out of p - q (333 rows against 5003 of
-// 512: dX off by 2.6e-6 in the root mean square with the products' own terms in the sum).
+// KD (distillation): no target; the first piece turns the teacher's logits into its shares, and the entries' terms come out
+// of P.  Where P holds the terms as they were summed (fp32), the entries' are taken out of the sum as well and the ones
+// of entry_exponents put in: a sure row's total and its largest term then have the same error, which drops out of p - q
+// (333 rows against 5003 of 512: dX off by 2.6e-6 in the root mean square with the products' own terms in the sum).
 template <typename T, bool KD>
 __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   __shared__ float red[4];
@@ -338,6 +376,7 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   }
   if constexpr (KD) {
     constexpr bool F32 = sizeof(T) == 4;
+    if (a.first) teacher_row(a, row, red64);
     __syncthreads();
     double put = 0.;  // what comes into the sum: all of it that is to, in the last piece
     float out = 0.f;
@@ -362,85 +401,6 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
       if (a.last && a.loss)
         a.loss[row] = a.term[row] == 0.f ? 0.f : (float)((a.base[row] + log2(total) + ref) * 0.69314718055994531);
     }
-  }
-}
-
-// ---- distillation -----------------------------------------------------------------------------------------
-// The entries of a row: the student's logits at their tokens, as products of the row with the head's rows, and the
-// teacher's probabilities (its softmax over the entries), in 64 bits from 8 products on.  The student's term of an entry
-// is kept out of P and formed from these, so that where student and teacher agree their difference, not bf16's rounding
-// of both, is what reaches dX.  A wave takes four entries at a time, whose head rows are read side by side.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_teacher_kernel(VocabArgs a) {
-  __shared__ int32_t ids[kMaxEntries];
-  __shared__ double ex[kMaxEntries];
-  __shared__ bool again[kMaxEntries];  // the token stands at an earlier entry too
-  __shared__ double red[4];
-  const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const double c = a.inv_tau * kLog2e;
-  double top = -INFINITY;
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    const int id = a.ids[row * a.k + j];
-    ids[j] = (uint32_t)id < (uint32_t)a.V ? id : -1;
-    const double t = ids[j] < 0 ? -INFINITY : (double)a.teacher[row * a.k + j] * c;
-    ex[j] = t;
-    top = fmax(top, t);
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d));
-  if (lane == 0) red[wave] = top;
-  __syncthreads();
-  top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
-  __syncthreads();
-  double mass = 0.;
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    if (ids[j] >= 0) mass += ex[j] == -INFINITY ? 0. : exp2(ex[j] - top);
-    bool seen = false;
-    for (int i = 0; i < j; ++i) seen |= ids[i] == ids[j];
-    again[j] = seen;
-  }
-  mass = block_sum<4>(mass, red);
-  __syncthreads();
-  const T* x = static_cast<const T*>(a.X) + row * a.ldx;
-  double sum = 0.;
-  for (int j0 = 4 * wave; j0 < a.k; j0 += 16) {
-    const T* w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = static_cast<const T*>(a.W) + max(j0 + e < a.k ? ids[j0 + e] : -1, 0) * a.ldw;
-    double z[4] = {0., 0., 0., 0.};
-    for (int at = 8 * lane; at < a.K; at += 512) {
-      float xs[8], ws[4][8];
-      load8(x + at, xs);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) load8(w[e] + at, ws[e]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float part = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) part += xs[i] * ws[e][i];
-        z[e] += part;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) z[e] += __shfl_xor(z[e], d);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = j0 + e;
-      if (lane != e || j >= a.k) continue;
-      const bool is = ids[j] >= 0;
-      const double q = !is || ex[j] == -INFINITY ? 0. : exp2(ex[j] - top) / mass;
-      a.share[row * a.k + j] = (float)q;
-      a.exponent[row * a.k + j] = is && !again[j] ? z[e] * c : -INFINITY;
-      if (q != 0.) sum += q * ((ex[j] - top - log2(mass)) - z[e] * c);
-    }
-  }
-  sum = block_sum<4>(sum, red);
-  if (threadIdx.x == 0) {
-    a.base[row] = sum;
-    a.term[row] = mass == 0. ? 0.f : 1.f;
   }
 }
 
@@ -620,16 +580,17 @@ int check_shape(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t ldw, int6
 
 // Tiles of 64 rows have six buffers where each has a CU to itself, else four, which leave room for two on a CU (one row of
 // 4096 against 5000: 22 us with six, 25 with four; 45 rows of 816 against 113000: 65 and 57).
-template <bool GRAD>
+template <bool GRAD, bool KD>
 hipError_t launch_logits(const VocabArgs& a, int cus, hipStream_t s) {
   const int tm = a.tw < 256 ? a.tw : a.T <= 128 ? 128 : 256;
-  const dim3 grid((unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm)));
-  if (a.tw == 64 && grid.x <= (unsigned)cus)
-    hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 6>), grid, dim3(256), 0, s, a);
-  else if (a.tw == 64) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 4>), grid, dim3(256), 0, s, a);
-  else if (a.tw == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 4, 3>), grid, dim3(256), 0, s, a);
-  else if (tm == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 8, 2>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 8, 8, 2>), grid, dim3(256), 0, s, a);
+  const unsigned tiles = (unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm));
+  const dim3 grid(tiles + (KD ? a.n_entry : 0));
+  if (a.tw == 64 && tiles <= (unsigned)cus)
+    hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 6, KD>), grid, dim3(256), 0, s, a);
+  else if (a.tw == 64) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 2, 2, 4, KD>), grid, dim3(256), 0, s, a);
+  else if (a.tw == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 4, 3, KD>), grid, dim3(256), 0, s, a);
+  else if (tm == 128) hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 4, 8, 2, KD>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((vocab_logits_kernel<GRAD, 8, 8, 2, KD>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -645,6 +606,11 @@ hipError_t launch_grad(const VocabArgs& a, hipStream_t s) {
   }
   return hipGetLastError();
 }
+
+// Workgroups of entries, a CU, up to which they go in the logits' launch; there a tile's registers and LDS leave room for
+// one on a CU.  16 rows of 16 entries against 20000 of 4096, with the gradient: 70 us, 79 with a launch for them; 64 of 64
+// 90 and 100; 256 of 64 184 either way; 1024 of 64 against 128256 1911 and 1900.
+constexpr int64_t kEntriesAhead = 4;
 
 // Room of a distillation's entries behind the pieces'.
 struct Entries {
@@ -666,6 +632,8 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   const Entries en = entries(pc.total, a.T, a.k);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
   if (ws_bytes < (kd ? en.total : pc.total)) return DSV_ERR_SIZE;
+  // the first launch's workgroups
+  if (kd && (int64_t)a.T * entry_groups(a.k) + (int64_t)((a.T + 31) / 32) * (pc.width / pc.tw) > INT32_MAX) return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
   char* b = static_cast<char*>(ws);
   a.P = a.grad ? b + pc.p : nullptr;
@@ -683,9 +651,6 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.exponent = reinterpret_cast<double*>(b + en.exponent);
     a.base = reinterpret_cast<double*>(b + en.base);
     a.share = reinterpret_cast<float*>(b + en.share);
-    if (bf) hipLaunchKernelGGL(vocab_teacher_kernel<uint16_t>, dim3((unsigned)a.T), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(vocab_teacher_kernel<float>, dim3((unsigned)a.T), dim3(256), 0, s, a);
-    if (hipGetLastError() != hipSuccess) return DSV_ERR_DEVICE;
   }
   for (int i = 0; i < pc.n; ++i) {
     a.v0 = i * pc.width;
@@ -694,7 +659,16 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.first = i == 0;
     a.last = i + 1 == pc.n;
     a.split = pc.split;
-    hipError_t e = !bf ? launch_vocab_f32_logits(a, cus, s) : a.grad ? launch_logits<true>(a, cus, s) : launch_logits<false>(a, cus, s);
+    const int64_t n_entry = kd && a.first ? (int64_t)a.T * entry_groups(a.k) : 0;
+    // ahead of the tiles, or on their own
+    const bool apart = n_entry > kEntriesAhead * cus;
+    a.n_entry = apart ? 0 : (int32_t)n_entry;
+    if (apart && bf) hipLaunchKernelGGL(vocab_entry_kernel<uint16_t>, dim3((unsigned)n_entry), dim3(256), 0, s, a);
+    else if (apart) hipLaunchKernelGGL(vocab_entry_kernel<float>, dim3((unsigned)n_entry), dim3(256), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return DSV_ERR_DEVICE;
+    hipError_t e = !bf  ? launch_vocab_f32_logits(a, cus, s)
+                   : kd ? (a.grad ? launch_logits<true, true>(a, cus, s) : launch_logits<false, true>(a, cus, s))
+                        : (a.grad ? launch_logits<true, false>(a, cus, s) : launch_logits<false, false>(a, cus, s));
     if (e != hipSuccess) return DSV_ERR_DEVICE;
     const dim3 rows((unsigned)a.T);
     if (kd && bf) hipLaunchKernelGGL((vocab_fold_kernel<uint16_t, true>), rows, dim3(256), 0, s, a);

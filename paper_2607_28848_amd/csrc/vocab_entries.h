@@ -1,0 +1,68 @@
+// vocab_entries.h -- the entries' logits of a distillation, beside the tiles of the logits' launch.
+#pragma once
+
+#include "device_common.h"
+#include "vocab.h"
+
+namespace dsv {
+namespace {
+
+// Eight values from p on.
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+  }
+}
+
+// The student's exponents at a teacher's tokens: products of a row with the head's rows in 64 bits from 8 products on,
+// times c.  The student's terms of the entries are kept out of P and formed from these, so that where student and teacher
+// agree their difference, not bf16's rounding of both, is what reaches dX.  A workgroup of four waves takes kEntryGroup
+// entries of a row, a wave four of them side by side.  They go in the launch of the first piece's logits, ahead of its
+// tiles, which they do not wait for (16 rows of 4096, 20 entries: 18 us in a launch of their own).
+template <typename T>
+__device__ __forceinline__ void entry_exponents(const VocabArgs& a, int block) {
+  const int groups = entry_groups(a.k);
+  const int64_t row = block / groups;
+  const int lane = threadIdx.x & 63, j0 = kEntryGroup * (block % groups) + 4 * (int)(threadIdx.x >> 6);
+  const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+  const T* w[4];
+  bool is[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int id = j0 + e < a.k ? a.ids[row * a.k + j0 + e] : -1;
+    is[e] = (uint32_t)id < (uint32_t)a.V;
+    w[e] = static_cast<const T*>(a.W) + (is[e] ? id : 0) * a.ldw;
+  }
+  double z[4] = {0., 0., 0., 0.};
+#pragma unroll 2
+  for (int at = 8 * lane; at < a.K; at += 512) {
+    float xs[8], ws[4][8];
+    load8(x + at, xs);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) load8(w[e] + at, ws[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += xs[i] * ws[e][i];
+      z[e] += part;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) z[e] += __shfl_xor(z[e], d);
+    if (lane == e && j0 + e < a.k) a.exponent[row * a.k + j0 + e] = is[e] ? z[e] * (a.inv_tau * 1.4426950408889634) : -INFINITY;
+  }
+}
+
+}  // namespace
+}  // namespace dsv

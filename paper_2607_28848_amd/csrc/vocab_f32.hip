@@ -12,6 +12,7 @@
 #include "device_common.h"
 #include "gemm_tile.h"
 #include "vocab.h"
+#include "vocab_entries.h"
 
 namespace dsv {
 namespace {
@@ -126,7 +127,7 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int FM>
+template <int FM, bool KD>
 __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   constexpr int WM = 16 * FM, TM = 2 * WM;
   __shared__ __attribute__((aligned(1024))) char b0[kStage];
@@ -134,7 +135,12 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   __shared__ __attribute__((aligned(1024))) char b2[kStage];
   __shared__ float red[2][2][TM];
   // the row tiles of a column tile one after the other: they share the head's rows in L2
-  const int n_m = (a.T + TM - 1) / TM, lin = tile_of(blockIdx.x, gridDim.x);
+  const int ahead = KD ? a.n_entry : 0;
+  if (KD && (int)blockIdx.x < ahead) {
+    entry_exponents<float>(a, blockIdx.x);
+    return;
+  }
+  const int n_m = (a.T + TM - 1) / TM, lin = tile_of(blockIdx.x - ahead, gridDim.x - ahead);
   const int mt = lin % n_m, nt = lin / n_m;
   const int m0 = TM * mt, n0 = 128 * nt, cols = min(128, a.vn - n0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l15 = lane & 15;
@@ -166,7 +172,7 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
     const float have = !a.first && in ? a.ref[row] : 0.f;
     ref[i] = tile_reference(m, have, a.first);
     const float base = ref[i] == -INFINITY ? 0.f : ref[i];
-    const int t = in && a.target ? a.target[row] - a.v0 - n0 - c0 : -1;
+    const int t = !KD && in ? a.target[row] - a.v0 - n0 - c0 : -1;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -237,9 +243,11 @@ __global__ __launch_bounds__(256) void vocab_f32_grad_kernel(VocabArgs a) {
 // Tiles of 64 rows fewer than the CUs are taken as tiles of 32 (64 rows against 5003 of 512: 19 us, 27 else).
 hipError_t launch_vocab_f32_logits(const VocabArgs& a, int cus, hipStream_t s) {
   const int tm = (int64_t)a.n_ct * ((a.T + 63) / 64) <= cus ? 32 : vocab_f32_rows(a.T);
-  const dim3 grid((unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm)));
-  if (tm == 32) hipLaunchKernelGGL(vocab_f32_logits_kernel<1>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(vocab_f32_logits_kernel<2>, grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm)) + a.n_entry);
+  if (a.k > 0 && tm == 32) hipLaunchKernelGGL((vocab_f32_logits_kernel<1, true>), grid, dim3(256), 0, s, a);
+  else if (a.k > 0) hipLaunchKernelGGL((vocab_f32_logits_kernel<2, true>), grid, dim3(256), 0, s, a);
+  else if (tm == 32) hipLaunchKernelGGL((vocab_f32_logits_kernel<1, false>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((vocab_f32_logits_kernel<2, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
