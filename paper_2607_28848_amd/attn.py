@@ -17,12 +17,12 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
-import struct
 
 import numpy as np
 
 from . import dsv
 from .dsv import DsvError, _check, _ptr, _stream_handle, torch  # noqa: F401
+from . import _marshal  # noqa: E402  (its libraries are torch's, loaded by now)
 
 _lib = dsv.lib_handle()
 _vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -51,9 +51,9 @@ _lib.dsv_attn_bwd.argtypes = [_vp, ctypes.c_int, ctypes.c_double] + [_viewp] * 4
 _lib.dsv_attn_bwd.restype = ctypes.c_int
 
 # The calls below pass their views as packed bytes, read during the call only: a decode step's attention takes the GPU
-# 10 us, and marshalling structures takes the host as long.
-_VIEW_PACK = struct.Struct("@Pqq").pack
-assert len(_VIEW_PACK(0, 0, 0)) == ctypes.sizeof(View)
+# 10 us, and marshalling structures takes the host as long.  _view(t, rows, heads, d, dtype, name): the bytes.
+_view = _marshal.view
+assert ctypes.sizeof(View) == 24
 _head = (ctypes.c_int, _vp, ctypes.c_int, ctypes.c_double)
 _fwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 6, _sz, _vp)(("dsv_attn_fwd", _lib))
 _bwd = ctypes.CFUNCTYPE(*_head, *[_vp] * 10, _sz, _vp)(("dsv_attn_bwd", _lib))
@@ -68,18 +68,8 @@ def on(stream):
 def here(*tensors):
     """ValueError unless the tensors (None: not given) are on one device, the current one where it is a GPU: a call's
     kernels run there."""
-    at = None
-    for t in tensors:
-        if t is None:
-            continue
-        d = t.get_device()  # -1: no GPU's
-        if d < 0 and t.is_meta:
-            raise ValueError("a tensor of the call has no memory")
-        if at is None:
-            at = d
-        elif d != at:
-            raise ValueError("the tensors of a call are on several devices: %s" % sorted({str(t.device) for t in tensors if t is not None}))
-    if at is not None and at >= 0 and at != torch.cuda.current_device():
+    at = _marshal.where(*tensors)
+    if at >= 0 and at != torch.cuda.current_device():
         raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (at, torch.cuda.current_device()))
 
 
@@ -157,23 +147,6 @@ def workspace_bytes(plan: Plan, dtype) -> int:
     n = _sz(0)
     _check(_lib.dsv_attn_workspace(plan.handle, _code(dtype), ctypes.byref(n)), "dsv_attn_workspace")
     return int(n.value)
-
-
-def _view(t, rows: int, heads: int, d: int, dtype, name: str) -> bytes:
-    if t.dtype is not dtype:
-        raise TypeError("%s is %s, the call's tensors are %s" % (name, t.dtype, dtype))
-    if t.shape != (rows, heads, d):
-        if t.shape != (rows, heads * d):
-            raise ValueError("%s must be [%d][%d][%d], got %s" % (name, rows, heads, d, tuple(t.shape)))
-        t = t.unflatten(1, (heads, d))
-    row, head, one = t.stride()
-    if one != 1 and rows:
-        raise ValueError("%s: the elements of a head must be contiguous" % name)
-    # the library takes a stride of 0 for the dense one
-    if (row == 0 and rows > 1) or (head == 0 and heads > 1 and rows > 0):
-        raise ValueError("%s is broadcast (a stride of 0): make it contiguous" % name)
-    # a stride of a dimension of one is arbitrary: the dense one then
-    return _VIEW_PACK(t.data_ptr(), row if rows > 1 else 0, head if heads > 1 and rows > 0 else 0)
 
 
 def _dense(t, shape, name: str):

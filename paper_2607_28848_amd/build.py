@@ -1,4 +1,4 @@
-"""Build libdsv.so (the HIP library behind include/dsv.h) for gfx950, in-tree.
+"""Build libdsv.so (the HIP library behind include/dsv.h) for gfx950 and _marshal.so (the bindings' checks of tensors), in-tree.
 
     python -m paper_2607_28848_amd.build              # the library
     python -m paper_2607_28848_amd.build --host-asan  # + host-sanitized variant
@@ -22,6 +22,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdsv.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["plan.cpp", "attn_plan.cpp", "api.cpp", "gemm_bf16.hip", "gemm_part.hip", "kernels_bf16.hip", "kernels_f32.hip",
            "optim.hip", "dropout.hip", "scratch.hip", "attn.hip", "attn_f32.hip", "rope.hip", "vocab.hip", "vocab_f32.hip"]
 HOST_SOURCES = [s for s in SOURCES if s.endswith(".cpp")]
@@ -42,7 +43,7 @@ FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source into libdsv.so (always recompiles; the sources side by side)."""
+    """Compile every source into libdsv.so, and _marshal.so (always recompiles; the sources side by side)."""
     obj_dir = os.path.join(PKG, "_build", "obj%d" % os.getpid())
     os.makedirs(obj_dir, exist_ok=True)
     objs = [os.path.join(obj_dir, s + ".o") for s in SOURCES]
@@ -50,8 +51,10 @@ def build(verbose: bool = False) -> str:
     flags = [f for f in FLAGS if f != "-shared"]
     try:
         with ThreadPoolExecutor(max_workers=min(len(objs), 8)) as ex:
+            module = ex.submit(build_marshal, verbose)
             outs = list(ex.map(lambda so: _run([HIPCC] + flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
                                zip(SOURCES, objs)))
+            outs.append(module.result())
         outs.append(_run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs, verbose))
         os.replace(tmp, LIB)
     finally:
@@ -60,6 +63,25 @@ def build(verbose: bool = False) -> str:
     if verbose and out:
         print(out, flush=True)
     return LIB
+
+
+def build_marshal(verbose: bool = False) -> str:
+    """Compile csrc/marshal.cpp against the installed torch into _marshal.so."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = MARSHAL + ".tmp%d" % os.getpid()
+    try:
+        out = _run(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+                   + [x for p in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]] for x in ("-isystem", p)]
+                   + [os.path.join(CSRC, "marshal.cpp"), "-o", tmp] + ["-L" + p for p in cpp_extension.library_paths()]
+                   + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+        os.replace(tmp, MARSHAL)
+    finally:
+        if os.path.exists(tmp):
+            os.unlink(tmp)
+    return out
 
 
 def _run(cmd, verbose):

@@ -15,7 +15,7 @@ import ctypes
 import struct
 
 from . import dsv
-from .attn import View, _code, _view, here, int32, made
+from .attn import View, _code, _marshal, _view, here, int32, made
 from .dsv import OK, _check, _stream_handle, torch
 
 _lib = dsv.lib_handle()
@@ -50,13 +50,7 @@ def frequencies(rotated: int, theta: float = 10000.0, device=None):
     return theta ** (-torch.arange(0, rotated, 2, dtype=torch.float64, device=device) / max(rotated, 1))
 
 
-def _vec(t, n: int, dtype, name: str):
-    """The address of a vector, 0 for none."""
-    if t is None:
-        return 0
-    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of %d elements" % (name, dtype, n))
-    return t.data_ptr()
+_vec = _marshal.vec  # (t, n, dtype, name): the address of a vector, 0 for None
 
 
 def _heads(t, name: str):
