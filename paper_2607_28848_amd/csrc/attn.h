@@ -75,7 +75,9 @@ struct AttnKeys {
 
 // fp32 mode: tiles of kAttnF32Rows.  windowed: the plan has a window.
 hipError_t launch_attn_f32_fwd(const AttnArgs& a, bool windowed, hipStream_t s);
-hipError_t launch_attn_f32_dq(const AttnArgs& a, bool windowed, hipStream_t s);  // dQ, and delta for the next launch
-hipError_t launch_attn_f32_dk(const AttnArgs& a, bool windowed, hipStream_t s);  // dK, dV
+hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s);  // dQ, and delta for the next launch
+hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s);  // dK, dV
+// Plans with a window: dQ, dK and dV; a's items are the key tiles'.
+hipError_t launch_attn_f32_grad(AttnArgs a, const int32_t* dq_items, int32_t n_dq, hipStream_t s);
 
 }  // namespace dsv

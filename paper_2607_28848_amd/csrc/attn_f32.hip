@@ -196,14 +196,12 @@ __global__ __launch_bounds__(256) void attn_f32_fwd_kernel(AttnArgs a) {
   }
 }
 
-// dQ of 16 queries of one head, and delta = do . o for the launch of dK and dV.
-template <int D, bool WIN>
-__global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
-  constexpr int NW = 4;
-  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
-  const int item = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
-  const Seq s(a, a.items[2 * item]);
-  const int qt = a.items[2 * item + 1];
+// dQ of 16 queries of one head, and delta = do . o for the launch of dK and dV (none where a.delta is null).
+template <int D, bool WIN, int NW>
+__device__ __forceinline__ void dq_tile(const AttnArgs& a, const int32_t* items, int block, float* red) {
+  const int item = block / a.hq, h = block % a.hq;
+  const Seq s(a, items[2 * item]);
+  const int qt = items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
   const int hk = h / a.group, q = qt + l15, off = s.kl - s.ql;
   const bool in = q < s.ql;
@@ -217,7 +215,7 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
     for (int c = 0; c < D / 4; ++c) dot += dv[c] * ov[c];
   }
   const float delta = quad_sum(dot);
-  if (in && wave == 0 && lane < 16) a.delta[h * a.train_q + s.cq + q] = delta;
+  if (in && wave == 0 && lane < 16 && a.delta) a.delta[h * a.train_q + s.cq + q] = delta;
   const float lse = in ? exp_from(a.lse[(int64_t)h * a.n_q + s.q0 + q]) : 0.f;
   f32x4 acc[D / 16];
   clear<D>(acc);
@@ -252,14 +250,20 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
   }
 }
 
+template <int D>
+__global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
+  constexpr int NW = 4;
+  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
+  dq_tile<D, false, NW>(a, a.items, blockIdx.x, red);
+}
+
 // dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
 // heads (so the sums over them need no atomics), or of one of a.parts ranges of them, whose sums go to the workspace
 // (32 us whole, 10.3 and 4.0 for the join in four parts: the first batch above).
-template <int D, bool WIN>
-__global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
-  constexpr int NW = 8;
-  __shared__ __attribute__((aligned(16))) float red[NW * 16 * (D + 4)];
-  const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts, item = tile / a.hkv, g = tile % a.hkv;
+// WIN: in one launch with dq_tile, so delta is formed here as it is there; the parts are ranges of all the tile's steps.
+template <int D, bool WIN, int NW>
+__device__ __forceinline__ void dk_tile(const AttnArgs& a, int block, float* red) {
+  const int part = block % a.parts, tile = block / a.parts, item = tile / a.hkv, g = tile % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
@@ -274,23 +278,33 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
   // the keys' last query: with a window that of the last key, but the sinks are seen to the end
   const int q_end = WIN && k0 >= a.sinks ? (int)min((int64_t)s.ql, (int64_t)min(k0 + 16, s.kl) - 1 - off + a.window) : s.ql;
   const int per_head = q_first < q_end ? (q_end - q_first + 15) / 16 : 0;
-  const int h0 = part * a.group / a.parts, h1 = (part + 1) * a.group / a.parts;
-  for (int n = wave; n < per_head * (h1 - h0); n += NW) {
-    const int h = g * a.group + h0 + n / per_head, qt = q_first + n % per_head * 16;
+  const int64_t all = WIN ? (int64_t)per_head * a.group : a.group;
+  const int step = WIN ? 1 : per_head, n0 = (int)(part * all / a.parts) * step, n1 = (int)((part + 1) * all / a.parts) * step;
+  for (int n = n0 + wave; n < n1; n += NW) {
+    const int h = g * a.group + n / per_head, qt = q_first + n % per_head * 16;
     float qv[D / 4], ov[D / 4], qc[4][D / 16], oc[4][D / 16], lse[4], delta[4];
     const auto qr = rows_of<D>(a.Q, (int64_t)s.q0 + qt, h, s.ql - qt);
     const auto dr = rows_of<D>(a.dO, (int64_t)s.cq + qt, h, s.ql - qt);
     load_quarter<D>(qr, a.Q.row, qv);
     load_quarter<D>(dr, a.dO.row, ov);
+    float mine = 0.f;  // do . o of row l % 16
+    if constexpr (WIN) {
+      float rows[D / 4];
+      load_quarter<D>(rows_of<D>(a.O, (int64_t)s.q0 + qt, h, s.ql - qt), a.O.row, rows);
+#pragma unroll
+      for (int c = 0; c < D / 4; ++c) mine += ov[c] * rows[c];
+      mine = quad_sum(mine);
+    }
     load_columns<D>(dr, a.dO.row, oc);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int q = min(qt + 4 * (lane >> 4) + v, s.ql - 1);
       lse[v] = a.lse[(int64_t)h * a.n_q + s.q0 + q];
-      delta[v] = a.delta[h * a.train_q + s.cq + q];
+      delta[v] = WIN ? __shfl(mine, 4 * (lane >> 4) + v) : a.delta[h * a.train_q + s.cq + q];
     }
     const f32x4 x = dot_tile<D>(qv, kv);
-    __builtin_amdgcn_sched_barrier(0);  // Q's columns take the registers of its rows (with heads of 128 both do not fit)
+    // Q's columns take the registers of its rows (with heads of 128 both do not fit)
+    if constexpr (!WIN || D == 128) __builtin_amdgcn_sched_barrier(0);
     load_columns<D>(qr, a.Q.row, qc);
     const f32x4 dp = dot_tile<D>(ov, vv);
     f32x4 p, ds;
@@ -316,13 +330,29 @@ __global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
       const int r = i / (D / 4), c = 4 * (i % (D / 4));
       const f32x4 x = gather<D, NW>(red, r, c);
       if (a.parts > 1)
-        *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)blockIdx.x * 2 + half) * 16 + r) * D + c) = x;
+        *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)block * 2 + half) * 16 + r) * D + c) = x;
       else if (k0 + r < s.kl)
         *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) = x;
     }
   };
   put(dk, a.dK, 0);
   put(dv, a.dV, 1);
+}
+
+template <int D>
+__global__ __launch_bounds__(512) void attn_f32_dk_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) float red[8 * 16 * (D + 4)];
+  dk_tile<D, false, 8>(a, blockIdx.x, red);
+}
+
+// Both gradients of a plan with a window: a.first_groups workgroups for dK and dV, then those of dQ (a.first_join's items).
+// The key tiles are short there but for the sinks', and two launches would leave most of the card to the other's latency:
+// three samples of 357 rows, 8 heads on 2 of 64, window 101: 13.6 and 21 us one after the other.
+template <int D>
+__global__ __launch_bounds__(256) void attn_f32_grad_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) float red[4 * 16 * (D + 4)];
+  if ((int)blockIdx.x < a.first_groups) dk_tile<D, true, 4>(a, blockIdx.x, red);
+  else dq_tile<D, true, 4>(a, a.first_join, blockIdx.x - a.first_groups, red);
 }
 
 // dK and dV of 16 keys from the parts' sums, in order: one workgroup a tile and gradient.
@@ -354,29 +384,46 @@ hipError_t launch_attn_f32_fwd(const AttnArgs& a, bool windowed, hipStream_t s) 
   return hipGetLastError();
 }
 
-hipError_t launch_attn_f32_dq(const AttnArgs& a, bool windowed, hipStream_t s) {
+hipError_t launch_attn_f32_dq(const AttnArgs& a, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)(a.n_items * (int64_t)a.hq));
-  if (windowed && a.d == 64) hipLaunchKernelGGL((attn_f32_dq_kernel<64, true>), grid, dim3(256), 0, s, a);
-  else if (windowed) hipLaunchKernelGGL((attn_f32_dq_kernel<128, true>), grid, dim3(256), 0, s, a);
-  else if (a.d == 64) hipLaunchKernelGGL((attn_f32_dq_kernel<64, false>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attn_f32_dq_kernel<128, false>), grid, dim3(256), 0, s, a);
+  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dq_kernel<64>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(attn_f32_dq_kernel<128>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_attn_f32_dk(const AttnArgs& a, bool windowed, hipStream_t s) {
-  if (a.n_items <= 0) return hipSuccess;
-  const int64_t tiles = a.n_items * (int64_t)a.hkv;
-  const dim3 grid((unsigned)(tiles * a.parts));
-  if (windowed && a.d == 64) hipLaunchKernelGGL((attn_f32_dk_kernel<64, true>), grid, dim3(512), 0, s, a);
-  else if (windowed) hipLaunchKernelGGL((attn_f32_dk_kernel<128, true>), grid, dim3(512), 0, s, a);
-  else if (a.d == 64) hipLaunchKernelGGL((attn_f32_dk_kernel<64, false>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((attn_f32_dk_kernel<128, false>), grid, dim3(512), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
+namespace {
+
+// The join of dK's and dV's parts, where there are some.
+hipError_t join_parts(const AttnArgs& a, int64_t tiles, hipStream_t s) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1 || tiles == 0) return e;
   if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_join_kernel<64>, dim3((unsigned)(2 * tiles)), dim3(256), 0, s, a);
   else hipLaunchKernelGGL(attn_f32_dk_join_kernel<128>, dim3((unsigned)(2 * tiles)), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s) {
+  if (a.n_items <= 0) return hipSuccess;
+  const int64_t tiles = a.n_items * (int64_t)a.hkv;
+  const dim3 grid((unsigned)(tiles * a.parts));
+  if (a.d == 64) hipLaunchKernelGGL(attn_f32_dk_kernel<64>, grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL(attn_f32_dk_kernel<128>, grid, dim3(512), 0, s, a);
+  return join_parts(a, tiles, s);
+}
+
+hipError_t launch_attn_f32_grad(AttnArgs a, const int32_t* dq_items, int32_t n_dq, hipStream_t s) {
+  const int64_t tiles = a.n_items * (int64_t)a.hkv;
+  a.first_groups = (int32_t)(tiles * a.parts);
+  a.first_join = dq_items;
+  a.delta = nullptr;
+  const dim3 grid((unsigned)(a.first_groups + (int64_t)n_dq * a.hq));
+  if (grid.x == 0) return hipSuccess;
+  if (a.d == 64) hipLaunchKernelGGL(attn_f32_grad_kernel<64>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(attn_f32_grad_kernel<128>, grid, dim3(256), 0, s, a);
+  return join_parts(a, tiles, s);
 }
 
 }  // namespace dsv
