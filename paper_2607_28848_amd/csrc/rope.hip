@@ -17,6 +17,14 @@
 namespace dsv {
 namespace {
 
+// The backward of the queries or the keys.
+struct RopeBack {
+  int32_t heads, split, groups;  // waves a row, workgroups
+  const float* weight;
+  AttnView dy, x, dx;
+  float* dw;  // nullptr: not wanted
+};
+
 struct RopeArgs {
   int32_t n;            // rows of the forward's tensors
   int32_t hq, hkv, hv;  // hv: heads of V that are copied (0: none)
@@ -32,10 +40,8 @@ struct RopeArgs {
   // backward
   int32_t n_rows;
   const int32_t* rows;  // nullptr: row i
-  AttnView dQ, dK, dQo, dKo;
-  float* part;          // [groups][2][D] sums of the weights' gradients (nullptr: none)
-  int32_t groups;
-  float *dqw, *dkw;
+  RopeBack q, k;
+  float* part;          // [groups of both][D] sums of the weights' gradients (nullptr: none)
 };
 
 template <typename T>
@@ -133,14 +139,15 @@ __device__ __forceinline__ void row_turns(const RopeArgs& a, int pos, const Lane
   }
 }
 
-// The lane's pairs turned: x[0 .. 8) and x[8 .. 16) are its chunks.
-template <bool NEXT>
+// The lane's pairs turned (BACK: the other way): x[0 .. 8) and x[8 .. 16) are its chunks.
+template <bool NEXT, bool BACK = false>
 __device__ __forceinline__ void turn(float (&x)[16], const float (&c)[8], const float (&s)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int a = NEXT ? 2 * i : i, b = NEXT ? 2 * i + 1 : 8 + i;
     const float u = x[a], v = x[b];
-    x[a] = u * c[i] - v * s[i], x[b] = v * c[i] + u * s[i];
+    if constexpr (BACK) x[a] = u * c[i] + v * s[i], x[b] = v * c[i] - u * s[i];
+    else x[a] = u * c[i] - v * s[i], x[b] = v * c[i] + u * s[i];
   }
 }
 
@@ -205,52 +212,50 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs a) {
   }
 }
 
-// Gradient rows: a wave takes every (4 groups / split)-th row and, of its heads, every split-th wave's share, queries
-// first; the weights' gradients stay in registers over its rows.
+// Gradient rows of the queries (the first a.q.groups workgroups) or of the keys: a wave takes every
+// (4 groups / split)-th row and, of its heads, every split-th wave's share; the weight's gradient stays in registers over
+// its rows.  With queries and keys in one wave the two sums took 155 registers, three waves a SIMD: 2048 rows of 8 + 2
+// heads of 64 11.8 us with the weights' launch, 8.2 so; 16000 of 24 + 4 45.7 and 39.8 (4.3 TB/s).
 template <typename T, int D, bool NEXT>
-__global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs a) {
+__global__ __launch_bounds__(256, 4) void rope_bwd_kernel(RopeArgs a) {
   constexpr int LPH = Lane<D>::LPH, HPW = Lane<D>::HPW;
   __shared__ __attribute__((aligned(16))) float cs[4][2][64];
   __shared__ __attribute__((aligned(16))) float red[4 * HPW][D];
+  const bool is_q = (int)blockIdx.x < a.q.groups;
+  const RopeBack& k = is_q ? a.q : a.k;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
-  const int part = (int)(w % a.split);
-  const int64_t step = (int64_t)a.groups * 4 / a.split;  // groups * 4 is a multiple of split
+  const int64_t w = (int64_t)(blockIdx.x - (is_q ? 0 : a.q.groups)) * 4 + wave;
+  const int part = (int)(w % k.split);
+  const int64_t step = (int64_t)k.groups * 4 / k.split;  // groups * 4 is a multiple of split
   const Lane<D> at(a.rot, NEXT);
-  const int qb = (a.hq + HPW - 1) / HPW, kb = (a.hkv + HPW - 1) / HPW;
-  float dw[2][16];
+  float dw[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0.f;
-  for (int64_t i = w / a.split; i < a.n_rows; i += step) {
+  for (int i = 0; i < 16; ++i) dw[i] = 0.f;
+  for (int64_t i = w / k.split; i < a.n_rows; i += step) {
     const int row = a.rows ? a.rows[i] : (int)i;
     const bool in = (uint32_t)row < (uint32_t)a.n;
     float c[8], s[8];
     row_turns<D>(a, a.rot && in ? a.pos[row] : 0, at, cs[wave], c, s);
-    auto head = [&](int h, int heads, const AttnView& dy, const AttnView& x_of, const AttnView& dx, const float* weight,
-                    float (&sums)[16]) {
-      if (h >= heads) return;
+    for (int h = part * HPW + at.g; h < k.heads; h += k.split * HPW) {
       float g[16], x[16];
-      Chunk<T> p, q;
-      const T* from = element<const T>(dy, i, h);
+      Chunk<T> p, q, px, qx;
+      const T* from = element<const T>(k.dy, i, h);
       p.load(from + at.a), q.load(from + at.b);
-      p.get(g), q.get(g + 8);
-      if (at.turns) {
-        float back[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) back[e] = -s[e];
-        turn<NEXT>(g, c, back);
+      if (k.weight && in) {
+        const T* seen = element<const T>(k.x, row, h);
+        px.load(seen + at.a), qx.load(seen + at.b);
       }
-      if (weight && in) {
-        const T* seen = element<const T>(x_of, row, h);
-        p.load(seen + at.a), q.load(seen + at.b);
-        p.get(x), q.get(x + 8);
+      p.get(g), q.get(g + 8);
+      if (at.turns) turn<NEXT, true>(g, c, s);
+      if (k.weight && in) {
+        px.get(x), qx.get(x + 8);
         float wt[16], dot = 0.f;
-        weight_of<D>(weight, at, wt);
+        weight_of<D>(k.weight, at, wt);
         const float r = __builtin_amdgcn_rsqf(head_sum<LPH>(square_sum(x)) * (1.f / D) + a.eps);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           x[e] *= r;
-          sums[e] += g[e] * x[e];
+          dw[e] += g[e] * x[e];
           g[e] *= wt[e];
           dot += g[e] * x[e];
         }
@@ -261,48 +266,44 @@ __global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs a) {
       if (!in)
 #pragma unroll
         for (int e = 0; e < 16; ++e) g[e] = 0.f;
-      T* to = element<T>(dx, i, h);
+      T* to = element<T>(k.dx, i, h);
       p.set(g), q.set(g + 8);
       p.store(to + at.a), q.store(to + at.b);
-    };
-    for (int b = part; b < qb + kb; b += a.split) {
-      if (b < qb) head(b * HPW + at.g, a.hq, a.dQ, a.Q, a.dQo, a.qw, dw[0]);
-      else head((b - qb) * HPW + at.g, a.hkv, a.dK, a.K, a.dKo, a.kw, dw[1]);
     }
   }
-  if (!a.part) return;
+  if (!a.part || !k.dw) return;
+  Chunk<float> p, q;
+  p.set(dw), q.set(dw + 8);
+  p.store(&red[wave * HPW + at.g][at.a]), q.store(&red[wave * HPW + at.g][at.b]);
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float x = 0.f;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    __syncthreads();
-    Chunk<float> p, q;
-    p.set(dw[k]), q.set(dw[k] + 8);
-    p.store(&red[wave * HPW + at.g][at.a]), q.store(&red[wave * HPW + at.g][at.b]);
-    __syncthreads();
-    if (threadIdx.x < D) {
-      float x = 0.f;
-#pragma unroll
-      for (int g = 0; g < 4 * HPW; ++g) x += red[g][threadIdx.x];
-      a.part[((int64_t)blockIdx.x * 2 + k) * D + threadIdx.x] = x;
-    }
+    for (int g = 0; g < 4 * HPW; ++g) x += red[g][threadIdx.x];
+    a.part[(int64_t)blockIdx.x * D + threadIdx.x] = x;
   }
 }
 
-// The workgroups' sums of 16 columns added in order, in 64 bits: 16 ranges of the workgroups, then the ranges.
+// The workgroups' sums of 16 columns of a weight's gradient (the queries' first) added in order, in 64 bits: 16 ranges of
+// the workgroups, then the ranges.
 template <int D>
 __global__ __launch_bounds__(256) void rope_weight_kernel(RopeArgs a) {
   __shared__ double red[16][17];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), range = threadIdx.x >> 4;
+  const bool is_q = blockIdx.x < D / 16;
+  const RopeBack& k = is_q ? a.q : a.k;
+  if (!k.dw) return;
+  const int col = blockIdx.x % (D / 16) * 16 + (threadIdx.x & 15), range = threadIdx.x >> 4;
+  const float* part = a.part + (int64_t)(is_q ? 0 : a.q.groups) * D + col;
   double x = 0.;
 #pragma unroll 16
-  for (int g = range; g < a.groups; g += 16) x += (double)a.part[(int64_t)g * 2 * D + col];
+  for (int g = range; g < k.groups; g += 16) x += (double)part[(int64_t)g * D];
   red[range][threadIdx.x & 15] = x;
   __syncthreads();
   if (threadIdx.x >= 16) return;
   x = 0.;
 #pragma unroll
   for (int r = 0; r < 16; ++r) x += red[r][threadIdx.x];
-  float* const to = col < D ? a.dqw : a.dkw;
-  if (to) to[col % D] = (float)x;
+  k.dw[col] = (float)x;
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -318,17 +319,23 @@ int split_of(int64_t rows, int blocks, int64_t waves) {
 
 int heads_a_wave(int d) { return 64 / (d / 16); }
 
-int bwd_blocks(const dsv_rope& r) {
-  const int hpw = heads_a_wave(r.head_dim);
-  return (r.heads_q + hpw - 1) / hpw + (r.heads_kv + hpw - 1) / hpw;
-}
-
-// Workgroups of the backward: a number of waves that the split divides.
-int bwd_groups(const dsv_rope& r, int32_t n_rows, int* split) {
-  *split = split_of(n_rows, bwd_blocks(r), 4 * kBwdGroups);
-  const int64_t waves = std::min<int64_t>((int64_t)n_rows * *split, 4 * kBwdGroups);
+// Workgroups of the backward of `heads` heads, at most `most`: a number of waves that the split divides.
+int bwd_groups(int32_t heads, int d, int32_t n_rows, int most, int* split) {
+  *split = 1;
+  if (heads == 0) return 0;
+  const int hpw = heads_a_wave(d);
+  *split = split_of(n_rows, (heads + hpw - 1) / hpw, 4 * most);
+  const int64_t waves = std::min<int64_t>((int64_t)n_rows * *split, 4 * most);
   const int64_t per = std::max(1, *split / 4);  // groups of four waves that one row takes
   return (int)std::max<int64_t>(per, (waves + 4 * per - 1) / (4 * per) * per);
+}
+
+// Of both kinds, with the workgroups divided as the heads are.
+void bwd_launch(const dsv_rope& r, int32_t n_rows, RopeBack* q, RopeBack* k) {
+  const int hpw = heads_a_wave(r.head_dim), qb = (r.heads_q + hpw - 1) / hpw, kb = (r.heads_kv + hpw - 1) / hpw;
+  const int most_q = std::max(1, kBwdGroups * qb / (qb + kb)), most_k = std::max(1, kBwdGroups * kb / (qb + kb));
+  q->groups = bwd_groups(r.heads_q, r.head_dim, n_rows, most_q, &q->split);
+  k->groups = bwd_groups(r.heads_kv, r.head_dim, n_rows, most_k, &k->split);
 }
 
 int check(const dsv_rope* r) {
@@ -370,8 +377,8 @@ hipError_t launch_fwd(const RopeArgs& a, int d, int64_t groups, hipStream_t s) {
 
 template <typename T, bool NEXT>
 hipError_t launch_bwd(const RopeArgs& a, int d, hipStream_t s) {
-  if (d == 64) hipLaunchKernelGGL((rope_bwd_kernel<T, 64, NEXT>), dim3((unsigned)a.groups), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((rope_bwd_kernel<T, 128, NEXT>), dim3((unsigned)a.groups), dim3(256), 0, s, a);
+  if (d == 64) hipLaunchKernelGGL((rope_bwd_kernel<T, 64, NEXT>), dim3((unsigned)(a.q.groups + a.k.groups)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_bwd_kernel<T, 128, NEXT>), dim3((unsigned)(a.q.groups + a.k.groups)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -417,8 +424,9 @@ extern "C" int dsv_rope_workspace(const dsv_rope* r, int32_t n_rows, size_t* byt
   if (!bytes || n_rows < 0) return DSV_ERR_ARG;
   const int rc = check(r);
   if (rc != DSV_OK) return rc;
-  int split;
-  *bytes = std::max<size_t>(256, (size_t)bwd_groups(*r, n_rows, &split) * 2 * r->head_dim * sizeof(float));
+  RopeBack q, k;
+  bwd_launch(*r, n_rows, &q, &k);
+  *bytes = std::max<size_t>(256, (size_t)(q.groups + k.groups) * r->head_dim * sizeof(float));
   return DSV_OK;
 }
 
@@ -436,25 +444,27 @@ extern "C" int dsv_rope_bwd(dsv_dtype dt, const dsv_rope* r, int32_t n_rows, con
   RopeArgs a = common(*r);
   const int32_t d = r->head_dim;
   if (a.hq > 0) {
-    if ((rc = view(dQ, n_rows, a.hq, d, false, &a.dQ)) != DSV_OK) return rc;
-    if ((rc = view(dQ_out, n_rows, a.hq, d, true, &a.dQo)) != DSV_OK) return rc;
-    if (a.qw && (rc = view(Q, r->n, a.hq, d, false, &a.Q)) != DSV_OK) return rc;
+    if ((rc = view(dQ, n_rows, a.hq, d, false, &a.q.dy)) != DSV_OK) return rc;
+    if ((rc = view(dQ_out, n_rows, a.hq, d, true, &a.q.dx)) != DSV_OK) return rc;
+    if (a.qw && (rc = view(Q, r->n, a.hq, d, false, &a.q.x)) != DSV_OK) return rc;
   }
   if (a.hkv > 0) {
-    if ((rc = view(dK, n_rows, a.hkv, d, false, &a.dK)) != DSV_OK) return rc;
-    if ((rc = view(dK_out, n_rows, a.hkv, d, true, &a.dKo)) != DSV_OK) return rc;
-    if (a.kw && (rc = view(K, r->n, a.hkv, d, false, &a.K)) != DSV_OK) return rc;
+    if ((rc = view(dK, n_rows, a.hkv, d, false, &a.k.dy)) != DSV_OK) return rc;
+    if ((rc = view(dK_out, n_rows, a.hkv, d, true, &a.k.dx)) != DSV_OK) return rc;
+    if (a.kw && (rc = view(K, r->n, a.hkv, d, false, &a.k.x)) != DSV_OK) return rc;
   }
-  a.groups = bwd_groups(*r, n_rows, &a.split);
+  bwd_launch(*r, n_rows, &a.q, &a.k);
+  a.q.heads = a.hq, a.k.heads = a.hkv;
+  a.q.weight = a.qw, a.k.weight = a.kw;
+  a.q.dw = dq_weight, a.k.dw = dk_weight;
   const bool sums = dq_weight || dk_weight;
   if (sums) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
-    if (ws_bytes < (size_t)a.groups * 2 * d * sizeof(float)) return DSV_ERR_SIZE;
+    if (ws_bytes < (size_t)(a.q.groups + a.k.groups) * d * sizeof(float)) return DSV_ERR_SIZE;
     a.part = static_cast<float*>(ws);
   }
   if (n_rows == 0 && !sums) return DSV_OK;
   a.n_rows = n_rows, a.rows = rows;
-  a.dqw = dq_weight, a.dkw = dk_weight;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t e =
       dt == DSV_BF16 ? (r->interleaved ? launch_bwd<uint16_t, true>(a, d, s) : launch_bwd<uint16_t, false>(a, d, s))
