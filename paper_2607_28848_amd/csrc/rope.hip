@@ -307,10 +307,13 @@ __global__ __launch_bounds__(256) void rope_weight_kernel(RopeArgs a) {
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
-constexpr int kFwdWaves = 4096;  // waves a launch should have before a row's heads stay in one
+// Of a row's blocks of heads a forward wave takes three in bf16 (6 KiB) and one in fp32 (4 KiB), or one where that makes
+// fewer waves than this.  16384 rows of 64 + 8 heads of 128 and the values, bf16, one, two or three blocks, or all ten a wave:
+// 136, 127, 127 and 143 us; fp32 239, 248, 254 and 268.  6144 rows of 32 + 8: 35.8, 34.3, 33.9 and 36.5; fp32 54, 57, 59, 60.
+constexpr int kFwdWaves = 4096;
 constexpr int kBwdGroups = 1024;
 
-// Waves that share a row: a power of two, so that the backward's four waves a group divide evenly.
+// Waves that share a gradient row: a power of two, so that four waves a group divide evenly.
 int split_of(int64_t rows, int blocks, int64_t waves) {
   int s = 1;
   while (s < blocks && rows * s < waves && s < 64) s *= 2;
@@ -412,7 +415,8 @@ extern "C" int dsv_rope_fwd(dsv_dtype dt, const dsv_rope* r, const dsv_attn_view
   if (r->n == 0) return DSV_OK;
   a.slots = slots, a.n_slots = n_slots;
   const int hpw = heads_a_wave(d);
-  a.split = split_of(r->n, (a.hq + a.hkv + a.hv + hpw - 1) / hpw, kFwdWaves);
+  const int blocks = (a.hq + a.hkv + a.hv + hpw - 1) / hpw, shared = dt == DSV_BF16 ? (blocks + 2) / 3 : blocks;
+  a.split = (int64_t)r->n * shared < kFwdWaves ? blocks : shared;
   const int64_t groups = ((int64_t)r->n * a.split + 3) / 4;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (dt == DSV_BF16)
