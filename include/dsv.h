@@ -647,11 +647,15 @@ int dsv_attn_build(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_
  * dsv_attn_build_window -- the same for attention that looks back over a window, with a
  * few first keys that stay visible (sinks): query i of a sequence, which stands at key
  * p = i + k_len - q_len, sees the keys j <= p with j > p - window or j < sinks.
- * window >= 1 (1: its own key), sinks >= 0, else DSV_ERR_RANGE.  Every call takes the
+ * window >= 1 (1: its own key), sinks >= 0, else DSV_ERR_RANGE; where the window hides a
+ * key, k_len at most 2^31 - 1025, else DSV_ERR_SIZE.  Every call takes the
  * plan like any other; only blocks of keys that some query of a tile sees are read, so a
  * decode token costs window + sinks keys, whatever its cache holds.  A cache that keeps
  * the sinks' and the last keys alone serves as well: positions count within the sequence's
  * key rows.  A window that hides no key of the batch gives dsv_attn_build's plan.
+ * Keys that no query of a sequence sees are not part of any sum, whatever they hold, and
+ * have gradients of 0; one that other queries of a sequence see adds 0 v to a query's sums,
+ * as in dsv_attn_fwd.
  */
 int dsv_attn_build_window(const dsv_attn_seq* seqs, int32_t n_seqs, int32_t n_q, int32_t n_kv, int32_t heads_q,
                           int32_t heads_kv, int32_t head_dim, int32_t window, int32_t sinks, size_t* meta_bytes,
@@ -754,7 +758,8 @@ int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const 
  * different temperatures alike is the caller's, in weight).  An id outside [0, V) is no
  * entry (padding); a teacher logit of -infinity is an entry of q = 0.  A row without an
  * entry of q > 0 has loss 0 and dx zeros, whatever it holds.  The same id twice: two
- * entries, each with its q.  The cross entropy's conventions hold else: the logits are
+ * entries, each with its q (so the loss can be below 0 there).  Teacher logits are finite or
+ * -infinity; others give NaN.  The cross entropy's conventions hold else: the logits are
  * never held whole, shapes, strides, alignment, Wt, and its workspace but for the entries'
  * room.  The student's terms at the teacher's ids are formed apart in fp32 or more, so in
  * bf16 mode dX keeps its accuracy where student and teacher agree; the others are rounded

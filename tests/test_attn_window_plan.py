@@ -65,7 +65,14 @@ def test_a_decode_token_costs_its_window():
 def test_the_widest_numbers():
     """Sequences, windows and sinks at the ends of 32 bits: sums of them do not wrap."""
     m = 2 ** 31 - 1
-    for w, s, q in ((1, 0, 1), (m, m, 40), (m - 1, 0, 40), (m - 1, 0, 1), (1, m - 2, 40), (1, m - 2, 1), (1000, 1000, 40)):
-        p = attn.Plan([(0, 2, 0, 100000, 1), (2, q, 0, m, 0)], 43, m, 1, 1, 64, window=w, sinks=s)
-        assert attn.workspace_bytes(p, attn.torch.bfloat16) > 0
-        del p
+    for k in (m, m - 1024):
+        for w, s, q in ((1, 0, 1), (m, m, 40), (k - 1, 0, 40), (k - 1, 0, 1), (1, k - 2, 40), (1, k - 2, 1), (1000, 1000, 40),
+                        (1, m, 1), (k - 33, 33, 1)):
+            hides = k > w and s < k - w
+            try:
+                p = attn.Plan([(0, 2, 0, 100000, 1), (2, q, 0, k, 0)], 43, m, 1, 1, 64, window=w, sinks=s)
+            except dsv.DsvError as e:
+                assert hides and k == m and e.status == dsv.ERR_SIZE
+            else:
+                assert (not hides or k < m) and attn.workspace_bytes(p, attn.torch.bfloat16) > 0
+                del p
