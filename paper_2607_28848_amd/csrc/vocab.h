@@ -22,9 +22,10 @@ struct VocabArgs {
   int32_t v0, vn;
   int32_t tw, n_ct;       // width and number of the piece's column tiles
   int32_t first, last;    // the piece is the first / the last
-  int32_t grad;
+  int32_t grad;           // the gradient is wanted
+  int32_t keep;           // P is kept
   // Exponents are base 2: a row's reference r stands for 2^r.
-  void* P;                // [T][ldp] 2^(z log2 e - reference) of the piece, the target's left out (grad)
+  void* P;                // [T][ldp] 2^(z log2 e - reference) of the piece, the target's left out (keep)
   int64_t ldp;
   float2* stats;          // [T][ld_stats] per column tile: reference, sum of its P
   int64_t ld_stats;

@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     }
   }
   T* P = static_cast<T*>(a.P) + (int64_t)row * a.ldp;
-  if (a.grad && __syncthreads_or(moved)) {
+  if (a.keep && __syncthreads_or(moved)) {
     constexpr int E = 16 / sizeof(T);
     for (int64_t c = threadIdx.x * E; c < (int64_t)a.n_ct * a.tw; c += 256 * E) {
       const float r = st[c / a.tw].x;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     __syncthreads();
     double put = 0.;  // what comes into the sum: all of it that is to, in the last piece
     float out = 0.f;
-    for (int j = threadIdx.x; a.grad && j < a.k; j += 256) {
+    for (int j = threadIdx.x; a.keep && j < a.k; j += 256) {
       const double x = a.exponent[(int64_t)row * a.k + j];
       if (x == -INFINITY) continue;  // none, or one that another entry stands for
       const int at = a.ids[(int64_t)row * a.k + j] - a.v0;
@@ -390,12 +390,12 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
       }
       if (F32 && a.last) put += exp2(x - ref);
     }
-    if (F32 && a.grad) {
+    if (F32) {
       out = block_sum<4>(out, red);
       if (a.last) put = block_sum<4>(put, red64);
     }
     if (threadIdx.x == 0) {
-      const float rest = F32 && a.grad ? others - out : others;
+      const float rest = F32 ? others - out : others;
       const double total = (rest < 0.f ? 0.f : rest) + put;  // a NaN stays one
       a.others[row] = (float)total;
       if (a.last && a.loss)
@@ -513,14 +513,16 @@ int logits_tile(int32_t T, int64_t width, int cus) {
 
 constexpr int64_t kPieceBytes = 256 << 20;  // of P: the size of the last-level cache
 
-Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool grad, int cus) {
+// kd: a distillation, whose sums in fp32 need P for the losses alone as well (vocab_fold).
+Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool grad, bool kd, int cus) {
   Pieces r{};
   const bool bf = dt == DSV_BF16;
   const int64_t size = bf ? 2 : 4;
   r.tw = bf ? 256 : 128;
   int64_t width = (V + r.tw - 1) / r.tw * r.tw;
   r.split = 1;
-  if (grad) {
+  const bool keep = grad || (kd && !bf);
+  if (keep) {
     // P within its room; 32-bit offsets of the second product's reads of W and of a tile's (up to 256) rows of P
     const int64_t most = std::min({kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 30) / (size * ldw),
                                    (((int64_t)1 << 31) - 1) / (size * 256)}) / r.tw * r.tw;
@@ -551,7 +553,7 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
     at += align256(bytes);
     return o;
   };
-  r.p = room(grad ? (size_t)T * r.width * size : 0);
+  r.p = room(keep ? (size_t)T * r.width * size : 0);
   r.stats = room((size_t)T * (r.width / r.tw) * sizeof(float2));
   r.rows = room((size_t)T * 4 * sizeof(float));
   r.o = room(grad ? (size_t)r.split * T * K * sizeof(float) : 0);
@@ -628,7 +630,8 @@ Entries entries(size_t from, int32_t T, int32_t k) {
 int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   const bool bf = dt == DSV_BF16, kd = a.k > 0;
   const int cus = device_cus();
-  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, cus);
+  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, kd, cus);
+  a.keep = a.grad || (kd && !bf);
   const Entries en = entries(pc.total, a.T, a.k);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
   if (ws_bytes < (kd ? en.total : pc.total)) return DSV_ERR_SIZE;
@@ -636,7 +639,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   if (kd && (int64_t)a.T * entry_groups(a.k) + (int64_t)((a.T + 31) / 32) * (pc.width / pc.tw) > INT32_MAX) return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
   char* b = static_cast<char*>(ws);
-  a.P = a.grad ? b + pc.p : nullptr;
+  a.P = a.keep ? b + pc.p : nullptr;
   a.ldp = pc.width;
   a.stats = reinterpret_cast<float2*>(b + pc.stats);
   a.ld_stats = pc.width / pc.tw;
@@ -700,7 +703,7 @@ extern "C" int dsv_vocab_workspace(dsv_dtype dt, int32_t T, int32_t K, int32_t V
   int64_t w = 0;
   const int rc = check_shape(dt, T, K, V, ldw, &w);
   if (rc != DSV_OK) return rc;
-  *bytes = pieces(dt, T, K, V, w, grad != 0, device_cus()).total;
+  *bytes = pieces(dt, T, K, V, w, grad != 0, false, device_cus()).total;
   return DSV_OK;
 }
 
@@ -765,7 +768,7 @@ extern "C" int dsv_vocab_distill_workspace(dsv_dtype dt, int32_t T, int32_t K, i
   const int rc = check_shape(dt, T, K, V, ldw, &w);
   if (rc != DSV_OK) return rc;
   if (k < 1 || k > kMaxEntries) return DSV_ERR_SIZE;
-  *bytes = entries(pieces(dt, T, K, V, w, grad != 0, device_cus()).total, T, k).total;
+  *bytes = entries(pieces(dt, T, K, V, w, grad != 0, true, device_cus()).total, T, k).total;
   return DSV_OK;
 }
 

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
         sum += e;
         acc[i][j][v] = e;
       }
-      if (a.grad && in)
+      if (a.keep && in)
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.P) + (int64_t)row * a.ldp + n0 + c0 + 16 * j) = acc[i][j];
     }
     sum = quad_sum(sum);

@@ -149,6 +149,31 @@ def test_agreement_keeps_its_accuracy():
     assert bool((dx.double().abs() <= bound * 1.01).all())
 
 
+def test_sure_students_in_fp32():
+    """Rows whose mass is at their entries' tokens: those terms are not the products' (whose K-long fp32 sums err by up to
+    m) but formed apart, so m bounds the other terms alone; 64 e and 8 e of the loss are left for sums and logarithms.  The
+    losses alone and those beside the gradient are the same bits."""
+    from paper_2607_28848_amd import vocab
+    T, K, V, k = 50, 1024, 3000, 6
+    X, W, ids, teacher, _ = make(T, K, V, k, F32, seed=12)
+    X += 3.0 * W[ids[:, 0].long()] + 2.0 * W[ids[:, 1].long()]
+    loss = vocab.distill(X, W, ids, teacher)
+    again, _ = vocab.distill_grad(X, W, ids, teacher)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, again)
+    (want, _), _ = oracle(X, W, ids, teacher, 1.0, None)
+    z = X.cpu().double() @ W.cpu().double().t()
+    p = torch.softmax(z, 1)
+    rest = 1 - torch.zeros_like(p).scatter(1, ids.cpu().long(), 1.0).mul(p).sum(1)
+    m = ((K + 4) * (X.abs().cpu().double() @ W.abs().cpu().double().t()) + 4 * z.abs()).amax(1) * E32
+    assert float(rest.median()) < 0.2
+    bound = 1.05 * (rest * (2 * m + (V + 40) * E32) + (64 + 8 * want.abs()) * E32)
+    # what 8 products in fp32 leave of an entry's own logit
+    bound += 8 * E32 * (X.abs().cpu().double() @ W.abs().cpu().double().t()).gather(1, ids.cpu().long()).amax(1) / 8
+    off = (loss.cpu().double() - want).abs()
+    assert float((off / bound).max()) <= 1, float((off / bound).max())
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("std", [1e-3, 40.0])
 def test_flat_and_sure_students(dtype, std):
