@@ -30,7 +30,8 @@ struct AttnArgs {
   float* lse2;           // bf16: lse of the compact rows, base 2
   // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
   // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
-  // Query tiles: [slot][hq][kAttnBwdRows][D].  Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].  fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
+  // Query tiles: [slot][hq][kAttnBwdRows][D].  Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].
+  // fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
   float* part_o;
   float* part_ml;
   // A join's first part (forward tiles, dQ): its sums, items and workgroups; the rest is as above.

@@ -275,6 +275,8 @@ __device__ __forceinline__ void store_sums(float* p, const f32x16 (&acc)[D / 32]
 // the other's products.  With heads of 64 the exponentials (one for 256 operations, a quarter of the vector rate) take
 // as long as the products.  16384 queries, 32 heads of 128 on 8: 1.90 ms (1155 TFLOP/s; a large bf16 product reaches
 // 1290 on the same card).  Nine prompts of about 700, 24 heads of 64 on 4: 36 us (570 TFLOP/s).
+// WIN: the plan has a window.  32768 queries behind 4096 and 4 sinks, 32 heads of 128 on 8: 2.00 ms (1030 TFLOP/s of the pairs
+// that are seen; 67 steps walked for 64).
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 // own (no barrier until the end), then the four waves' sums are added.  Every key is read once for all of
 // its head's queries: the stream of K and V is what bounds it where there are many keys (64 sequences of about 2600,
 // 8 heads of 128: 577 MB in 105 us, 5.5 TB/s), and the loads' latency one after the other where there are few (8 of
-// about 400: 10 us for 12 MB).
+// about 400: 10 us for 12 MB).  With a window the same: 64 caches of about 12000 behind 4096, 1.07 GB in 181 us, 5.9 TB/s.
 template <int D, bool WIN>
 __global__ __launch_bounds__(256) void attn_split_kernel(AttnArgs a) {
   constexpr int TK = 32, TILE = TK * 2 * D, LDO = D + 4;
@@ -565,7 +567,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dQ of 128 queries of one head over the keys they see, 32 queries a wave, 64 keys a step, in three products: the scores
 // again (p = 2^(c s - lse) needs no maximum), dO V^T, and ds K.  It also leaves delta = do . o and the base-2 lse of its
 // rows for attn_dk, which runs after it.  Bound as attn_fwd is (three fragments of LDS for three matrix instructions),
-// matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.45 ms (412 GFLOP, 920 TFLOP/s).
+// matrix core 49% busy: four samples of 2048, 64 heads of 128 on 8, 0.45 ms (412 GFLOP, 920 TFLOP/s).  Two of 8192 behind a
+// window of 1024, 32 heads on 8: 0.46 ms (850 TFLOP/s).
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int TK = 64, TILE = TK * 2 * D;
@@ -693,7 +696,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // Four products of 2 D operations a score (attn_dq: three), because dQ's sums run along the other axis and would need
 // atomics here.  The matrix core is 45% busy: 64 queries against 128 keys read 272 KB of LDS, 2200 cycles beside 2048 of
 // products, and two waves a SIMD overlap them in part.  Four samples of 2048, 64 heads of 128 on
-// 8: 0.65 ms (550 GFLOP, 845 TFLOP/s); two of 1024, 32 heads on 8: 72 us and 8 for the join.
+// 8: 0.65 ms (550 GFLOP, 845 TFLOP/s); two of 1024, 32 heads on 8: 72 us and 8 for the join.  Two of 8192 behind a window of
+// 1024: 0.75 ms (690 TFLOP/s; 18 steps for 16, and the sinks' tiles, 11% of the steps).  Waves without a visible pair in a step
+// could leave it out: no gain, since the others of the workgroup are waited for.
 template <int D, bool WIN>
 __global__ __launch_bounds__(512) void attn_dk_kernel(AttnArgs a) {
   constexpr int TQ = 64, TILE = TQ * 2 * D, PB = 4 * 64 * TQ, ST = 2 * TILE + PB;

@@ -4,6 +4,10 @@
 // chunks l and l + rotated / 16, or 2 l and 2 l + 1 where neighbours turn together, so both elements of a pair lie in
 // one lane and in both orders the lane's pairs are i = 8 l .. 8 l + 7.  A wave takes 64 / (D / 16) heads of one row at a
 // time.  The row's cosines and sines are formed once a wave, one angle a lane, and go to the lanes through LDS.
+//
+// Memory's rate bounds both directions: 16384 rows of 64 + 8 heads of 128 and the values, bf16, 127 us (5.3 TB/s); 6144 of 32 + 8
+// 34 us (4.4 TB/s); 8192 rows of gradients of 32 + 8 63 us (4.0 TB/s).  A few rows cost a launch: 8 rows 3.3 us.  Loading the
+// next heads before the present ones are turned was slower (44 us for the 6144 rows: more registers, fewer waves).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

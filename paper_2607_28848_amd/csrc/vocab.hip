@@ -435,6 +435,7 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(VocabArgs a) {
   }
 }
 
+// One read of the entries' head rows bounds it: 1024 rows of 8192, 64 entries, 134 us for 1.07 GB.
 // dx = weight / temperature (sum of the terms kept in P over their total + sum_j (p_j - share_j) W_j), 1024 columns a
 // workgroup.
 template <typename T>
