@@ -167,6 +167,7 @@ def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse=None, worksp
     needs; without one it is made if want_lse, which stands for "where O is made" if None, else it is not written and
     None is returned for it (inference)."""
     hq, hkv, d = plan.heads_q, plan.heads_kv, plan.head_dim
+    here(plan.meta, Q, K, V, O, lse, workspace)
     make_lse = lse is None and (O is None if want_lse is None else want_lse)
     if O is None or make_lse:
         with on(stream):
@@ -190,6 +191,7 @@ def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, 
     hq, hkv, d, nq, nk = plan.heads_q, plan.heads_kv, plan.head_dim, plan.train_q, plan.train_k
     if lse is None and nq > 0:
         raise ValueError("lse is None: the forward returns it with lse=... or want_lse=True")
+    here(plan.meta, Q, K, V, O, lse, dO, dQ, dK, dV, workspace)
     if dQ is None or dK is None or dV is None:
         with on(stream):
             dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)
