@@ -38,10 +38,13 @@ struct VocabArgs {
   const float* teacher;
   int32_t k;
   int32_t n_entry;        // workgroups of entry_exponents ahead of the launch's tiles
+  int32_t shares_ahead;   // they form the teacher's shares too; else the first fold does
   double inv_tau;
-  double* exponent;       // c z of the entry, -infinity where it is none or its token stands at an earlier one too
-  float* share;           // the teacher's probability of it
-  double* base;           // [T] sum of share (log2 share - c z)
+  double* exponent;       // c z of the entry, -infinity where it is none; after the first fold also where its token stands
+                          // at an earlier one
+  float* share;           // the teacher's probability of it; below 0 (or -0) until the first fold where its token stands earlier
+  double* log_share;      // its logarithm, base 2
+  double* base;           // [T] sum of share (log_share - c z)
   // second product: contraction in `split` ranges of split_len columns, each with its own sums
   float* O;               // [split][T][K]
   int32_t split, split_len;

@@ -255,55 +255,11 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a) {
   entry_exponents<T>(a, blockIdx.x);
 }
 
-// The teacher's shares of a row's entries (its softmax over them, in 64 bits), what the loss takes from them, and each
-// token's exponent at its first entry alone.
-__device__ __forceinline__ void teacher_row(const VocabArgs& a, int64_t row, double* red) {
-  __shared__ int32_t ids[kMaxEntries];
-  const double c = a.inv_tau * kLog2e;
-  const float* teacher = a.teacher + row * a.k;
-  double* exponent = a.exponent + row * a.k;
-  // an entry's logit, -infinity where it is none
-  auto logit = [&](int j) { return ids[j] < 0 ? -INFINITY : teacher[j] * c; };
-  double top = -INFINITY;
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    const int id = a.ids[row * a.k + j];
-    ids[j] = (uint32_t)id < (uint32_t)a.V ? id : -1;
-    top = fmax(top, logit(j));
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
-  __syncthreads();
-  auto term = [&](int j) { const double t = logit(j); return t == -INFINITY ? 0. : exp2(t - top); };
-  double mass = 0.;
-  for (int j = threadIdx.x; j < a.k; j += 256) mass += term(j);
-  mass = block_sum<4>(mass, red);
-  __syncthreads();
-  double sum = 0.;
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    const double e = term(j), q = e == 0. ? 0. : e / mass;
-    a.share[row * a.k + j] = (float)q;
-    if (q != 0.) sum += q * ((logit(j) - top - log2(mass)) - exponent[j]);
-    bool again = false;
-    for (int i = 0; i < j; ++i) again |= ids[i] == ids[j];
-    if (again) exponent[j] = -INFINITY;
-  }
-  sum = block_sum<4>(sum, red);
-  if (threadIdx.x == 0) {
-    a.base[row] = sum;
-    a.term[row] = mass == 0. ? 0.f : 1.f;
-  }
-}
-
 // One row: the piece's sums into the row's, at the larger of the references; the terms of tiles at another
 // reference are brought to the row's.  After the last piece the target's logit, its term and the loss, in 64 bits: the
 // logarithm and the logit nearly cancel for a sure row, and there is one of each per row (one row against 128256 of
 // 4096: the loss is off by 8e-7 in the root mean square with the logit from the products, whose sums are fp32).
-// KD (distillation): no target; the first piece turns the teacher's logits into its shares, and the entries' terms come out
-// of P.  Where P holds the terms as they were summed (fp32), the entries' are taken out of the sum as well and the ones
+// KD (distillation): no target, and the entries' terms come out of P.  Where P holds the terms as they were summed (fp32), the entries' are taken out of the sum as well and the ones
 // of entry_exponents put in: a sure row's total and its largest term then have the same error, which drops out of p - q
 // (333 rows against 5003 of 512: dX off by 2.6e-6 in the root mean square with the products' own terms in the sum).
 template <typename T, bool KD>
@@ -376,7 +332,22 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   }
   if constexpr (KD) {
     constexpr bool F32 = sizeof(T) == 4;
-    if (a.first) teacher_row(a, row, red64);
+    if (a.first && !a.shares_ahead) teacher_shares(a, row);  // an entry's are its thread's own in what follows
+    if (a.first) {
+      // what the loss takes from the entries, and each token's exponent at its first entry alone
+      double sum = 0.;
+      for (int j = threadIdx.x; j < a.k; j += 256) {
+        const int64_t at = (int64_t)row * a.k + j;
+        const float share = a.share[at];
+        if (share != 0.f) sum += fabs(share) * (a.log_share[at] - a.exponent[at]);
+        if (__float_as_uint(share) >> 31) {
+          a.share[at] = -share;
+          a.exponent[at] = -INFINITY;
+        }
+      }
+      sum = block_sum<4>(sum, red64);
+      if (threadIdx.x == 0) a.base[row] = sum;
+    }
     __syncthreads();
     double put = 0.;  // what comes into the sum: all of it that is to, in the last piece
     float out = 0.f;
@@ -613,16 +584,20 @@ hipError_t launch_grad(const VocabArgs& a, hipStream_t s) {
 // Workgroups of entries, a CU, up to which they go in the logits' launch; there a tile's registers and LDS leave room for
 // one on a CU.  16 rows of 16 entries against 20000 of 4096, with the gradient: 70 us, 79 with a launch for them; 64 of 64
 // 90 and 100; 256 of 64 184 either way; 1024 of 64 against 128256 1911 and 1900.
+// The teacher's shares take a workgroup about as long again, so beside the tiles they pay up to one a CU: 20 rows of 2080, 2
+// entries, against 33025 64.0 us, 66.2 in the fold; 98 of 1400, 10 against 36960 80.7 and 83.2; 333 in fp32 65.2 and 64.3; 505 of
+// 1176, 31 against 18096 121.6 and 108.8.
 constexpr int64_t kEntriesAhead = 4;
 
 // Room of a distillation's entries behind the pieces'.
 struct Entries {
-  size_t exponent, base, share, total;
+  size_t exponent, log_share, base, share, total;
 };
 Entries entries(size_t from, int32_t T, int32_t k) {
   Entries e{};
   e.exponent = align256(from);
-  e.base = align256(e.exponent + (size_t)T * k * sizeof(double));
+  e.log_share = align256(e.exponent + (size_t)T * k * sizeof(double));
+  e.base = align256(e.log_share + (size_t)T * k * sizeof(double));
   e.share = align256(e.base + (size_t)T * sizeof(double));
   e.total = align256(e.share + (size_t)T * k * sizeof(float));
   return e;
@@ -653,6 +628,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   a.split_len = pc.split_len;
   if (kd) {
     a.exponent = reinterpret_cast<double*>(b + en.exponent);
+    a.log_share = reinterpret_cast<double*>(b + en.log_share);
     a.base = reinterpret_cast<double*>(b + en.base);
     a.share = reinterpret_cast<float*>(b + en.share);
   }
@@ -667,6 +643,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     // ahead of the tiles, or on their own
     const bool apart = n_entry > kEntriesAhead * cus;
     a.n_entry = apart ? 0 : (int32_t)n_entry;
+    a.shares_ahead = n_entry <= cus;
     if (apart && bf) hipLaunchKernelGGL(vocab_entry_kernel<uint16_t>, dim3((unsigned)n_entry), dim3(256), 0, s, a);
     else if (apart) hipLaunchKernelGGL(vocab_entry_kernel<float>, dim3((unsigned)n_entry), dim3(256), 0, s, a);
     if (hipGetLastError() != hipSuccess) return DSV_ERR_DEVICE;

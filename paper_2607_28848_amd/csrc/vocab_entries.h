@@ -22,11 +22,54 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
   }
 }
 
+// A sum over a workgroup of four waves.
+__device__ __forceinline__ double sum_of_four(double x, double* red) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
+}
+
+// The teacher's shares of a row's entries: its softmax over them, in 64 bits.
+__device__ __forceinline__ void teacher_shares(const VocabArgs& a, int64_t row) {
+  __shared__ double red[4];
+  __shared__ int32_t ids[kMaxEntries];
+  const double c = a.inv_tau * 1.4426950408889634;
+  // an entry's logit, -infinity where it is none
+  auto logit = [&](int j) { return (uint32_t)ids[j] < (uint32_t)a.V ? a.teacher[row * a.k + j] * c : -INFINITY; };
+  double top = -INFINITY;
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    ids[j] = a.ids[row * a.k + j];
+    top = fmax(top, logit(j));
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+  auto term = [&](double t) { return t == -INFINITY ? 0. : exp2(t - top); };
+  double mass = 0.;
+  for (int j = threadIdx.x; j < a.k; j += 256) mass += term(logit(j));
+  mass = sum_of_four(mass, red);
+  const double log_mass = log2(mass);
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    const double t = logit(j), x = term(t), q = x == 0. ? 0. : x / mass;
+    bool again = false;  // the token stands at an earlier entry too
+    for (int i = 0; i < j; ++i) again |= ids[i] == ids[j];
+    a.share[row * a.k + j] = (float)(again ? -q : q);
+    a.log_share[row * a.k + j] = t - top - log_mass;
+  }
+  if (threadIdx.x == 0) a.term[row] = mass == 0. ? 0.f : 1.f;
+}
+
 // The student's exponents at a teacher's tokens: products of a row with the head's rows in 64 bits from 8 products on,
 // times c.  The student's terms of the entries are kept out of P and formed from these, so that where student and teacher
 // agree their difference, not bf16's rounding of both, is what reaches dX.  A workgroup of four waves takes kEntryGroup
 // entries of a row, a wave four of them side by side.  They go in the launch of the first piece's logits, ahead of its
-// tiles, which they do not wait for (16 rows of 4096, 20 entries: 18 us in a launch of their own).
+// tiles, which they do not wait for (16 rows of 4096, 20 entries: 18 us in a launch of their own).  A row's first group
+// forms the teacher's shares as well where they are few (a.shares_ahead).
 template <typename T>
 __device__ __forceinline__ void entry_exponents(const VocabArgs& a, int block) {
   const int groups = entry_groups(a.k);
@@ -62,6 +105,7 @@ __device__ __forceinline__ void entry_exponents(const VocabArgs& a, int block) {
     for (int d = 32; d > 0; d >>= 1) z[e] += __shfl_xor(z[e], d);
     if (lane == e && j0 + e < a.k) a.exponent[row * a.k + j0 + e] = is[e] ? z[e] * (a.inv_tau * 1.4426950408889634) : -INFINITY;
   }
+  if (a.shares_ahead && block % groups == 0) teacher_shares(a, row);
 }
 
 }  // namespace
