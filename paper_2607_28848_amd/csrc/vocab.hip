@@ -249,10 +249,11 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
   return x;
 }
 
-// entry_exponents in a launch of its own.
+// entry_exponents in a launch of its own, where they are many, and without the shares' code, whose registers cost it waves
+// (1024 rows of 8192, 64 entries: 156 us with it, 128 without).
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a) {
-  entry_exponents<T>(a, blockIdx.x);
+  entry_exponents<T, false>(a, blockIdx.x);
 }
 
 // One row: the piece's sums into the row's, at the larger of the references; the terms of tiles at another

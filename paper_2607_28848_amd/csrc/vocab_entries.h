@@ -70,7 +70,7 @@ __device__ __forceinline__ void teacher_shares(const VocabArgs& a, int64_t row) 
 // entries of a row, a wave four of them side by side.  They go in the launch of the first piece's logits, ahead of its
 // tiles, which they do not wait for (16 rows of 4096, 20 entries: 18 us in a launch of their own).  A row's first group
 // forms the teacher's shares as well where they are few (a.shares_ahead).
-template <typename T>
+template <typename T, bool SHARES = true>
 __device__ __forceinline__ void entry_exponents(const VocabArgs& a, int block) {
   const int groups = entry_groups(a.k);
   const int64_t row = block / groups;
@@ -105,7 +105,9 @@ __device__ __forceinline__ void entry_exponents(const VocabArgs& a, int block) {
     for (int d = 32; d > 0; d >>= 1) z[e] += __shfl_xor(z[e], d);
     if (lane == e && j0 + e < a.k) a.exponent[row * a.k + j0 + e] = is[e] ? z[e] * (a.inv_tau * 1.4426950408889634) : -INFINITY;
   }
-  if (a.shares_ahead && block % groups == 0) teacher_shares(a, row);
+  if constexpr (SHARES) {
+    if (a.shares_ahead && block % groups == 0) teacher_shares(a, row);
+  }
 }
 
 }  // namespace
