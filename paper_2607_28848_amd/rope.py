@@ -117,7 +117,7 @@ def fwd(Q, K, pos, freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=Fal
 def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
         dQ_out=None, dK_out=None, dq_weight=None, dk_weight=None, want_weights=None, workspace=None, stream=None):
     """dsv_rope_bwd; returns (dQ_out, dK_out, dq_weight, dk_weight).  Q, K: the forward's inputs, needed where there is a
-    weight.  The weights' gradients are fp32 and overwritten; one not given is made if want_weights, which stands for
+    weight; they or pos state the batch's rows, outside which a gradient row gets zeros (none given: any row from 0 on is one).  The weights' gradients are fp32 and overwritten; one not given is made if want_weights, which stands for
     "where its gradient's rows are made" if None, else it is not computed and None is returned for it."""
     if dQ is None and dK is None:
         raise ValueError("neither dQ nor dK")
@@ -128,7 +128,9 @@ def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=No
     hq, hkv, dt = 0 if dQ is None else dQ.shape[1], 0 if dK is None else _heads(dK, "dK")[1], like.dtype
     if (dQ is None or q_weight is None) and dq_weight is not None or (dK is None or k_weight is None) and dk_weight is not None:
         raise ValueError("the gradient of a weight that is not there")
-    n = m if pos is None and Q is None and K is None else (pos if pos is not None else Q if Q is not None else K).shape[0]
+    stated = next((t for t in (pos, Q, K) if t is not None), None)
+    # nothing of a batch's rows is read where nothing states their number: every row that 32 bits name is one
+    n = stated.shape[0] if stated is not None else m if rows is None else (1 << 31) - 1
     here(dQ, dK, pos, freq, rows, Q, K, q_weight, k_weight, dQ_out, dK_out, dq_weight, dk_weight, workspace)
     if hq and q_weight is not None and (dQ_out is None if want_weights is None else want_weights):
         dq_weight = made(dq_weight, (d,), torch.float32, dQ, stream)
