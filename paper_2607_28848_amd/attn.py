@@ -65,12 +65,24 @@ def on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def here(*tensors):
+class HostTensors(DsvError, ValueError):
+    """A call whose tensors are all in host memory, where its kernels would fault."""
+
+
+def here(*tensors) -> bool:
     """ValueError unless the tensors (None: not given) are on one device, the current one where it is a GPU: a call's
-    kernels run there."""
+    kernels run there.  Returns whether they are in host memory, for launchable()."""
     at = _marshal.where(*tensors)
     if at >= 0 and at != torch.cuda.current_device():
         raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (at, torch.cuda.current_device()))
+    return at < 0
+
+
+def launchable(host: bool, work: bool, what: str):
+    """HostTensors for a call that has something to do on tensors in host memory.  Without a GPU nothing can be launched,
+    and the library gives its own answer."""
+    if host and work and torch.cuda.is_available():
+        raise HostTensors(dsv.ERR_ARG, what + ": the tensors are in host memory")
 
 
 def made(given, shape, dtype, like, stream):

@@ -15,7 +15,7 @@ import ctypes
 import struct
 
 from . import dsv
-from .attn import View, _code, _marshal, _view, here, int32, made
+from .attn import View, _code, _marshal, _view, here, int32, launchable, made
 from .dsv import OK, _check, _stream_handle, torch
 
 _lib = dsv.lib_handle()
@@ -92,7 +92,7 @@ def fwd(Q, K, pos, freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=Fal
     hq, hkv, dt = 0 if Q is None else Q.shape[1], 0 if K is None else _heads(K, "K")[1], like.dtype
     if slots is not None and (K_out is None or (V is not None and V_out is None)):
         raise ValueError("slots need K_out, and V_out where V is given")
-    here(Q, K, V, pos, freq, q_weight, k_weight, slots, Q_out, K_out, V_out)
+    host = here(Q, K, V, pos, freq, q_weight, k_weight, slots, Q_out, K_out, V_out)
     if hq:
         Q_out = made(Q_out, (n, hq, d), dt, Q, stream)
     if hkv:
@@ -103,12 +103,15 @@ def fwd(Q, K, pos, freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=Fal
     if rows >= 1 << 31:
         int32(n_slots=rows)
     r = _rope(n, hq, hkv, d, pos, freq, q_weight if hq else None, k_weight if hkv else None, eps, interleaved)
-    rc = _fwd(_code(dt), r, None if Q is None else _view(Q, n, hq, d, dt, "Q"),
-              None if K is None else _view(K, n, hkv, d, dt, "K"), None if V is None else _view(V, n, hkv, d, dt, "V"),
-              None if slots is None else _vec(slots, n, torch.int32, "slots"), rows,
-              None if Q is None else _view(Q_out, n, hq, d, dt, "Q_out"),
-              None if K is None else _view(K_out, rows, hkv, d, dt, "K_out"),
-              None if V is None else _view(V_out, rows, hkv, d, dt, "V_out"), _stream_handle(stream))
+    args = (_code(dt), r, None if Q is None else _view(Q, n, hq, d, dt, "Q"),
+            None if K is None else _view(K, n, hkv, d, dt, "K"), None if V is None else _view(V, n, hkv, d, dt, "V"),
+            None if slots is None else _vec(slots, n, torch.int32, "slots"), rows,
+            None if Q is None else _view(Q_out, n, hq, d, dt, "Q_out"),
+            None if K is None else _view(K_out, rows, hkv, d, dt, "K_out"),
+            None if V is None else _view(V_out, rows, hkv, d, dt, "V_out"))
+    if host:
+        launchable(host, n > 0, "rope.fwd")
+    rc = _fwd(*args, _stream_handle(stream))
     if rc != OK:
         _check(rc, "dsv_rope_fwd")
     return (Q_out, K_out) if V is None else (Q_out, K_out, V_out)
@@ -131,7 +134,7 @@ def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=No
     stated = next((t for t in (pos, Q, K) if t is not None), None)
     # nothing of a batch's rows is read where nothing states their number: every row that 32 bits name is one
     n = stated.shape[0] if stated is not None else m if rows is None else (1 << 31) - 1
-    here(dQ, dK, pos, freq, rows, Q, K, q_weight, k_weight, dQ_out, dK_out, dq_weight, dk_weight, workspace)
+    host = here(dQ, dK, pos, freq, rows, Q, K, q_weight, k_weight, dQ_out, dK_out, dq_weight, dk_weight, workspace)
     if hq and q_weight is not None and (dQ_out is None if want_weights is None else want_weights):
         dq_weight = made(dq_weight, (d,), torch.float32, dQ, stream)
     if hkv and k_weight is not None and (dK_out is None if want_weights is None else want_weights):
@@ -149,12 +152,15 @@ def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=No
 
     if m >= 1 << 31:
         int32(n_rows=m)
-    rc = _bwd(_code(dt), r, m, None if rows is None else _vec(rows, m, torch.int32, "rows"), view(dQ, m, hq, "dQ"),
-              view(dK, m, hkv, "dK"), view(Q, n, hq, "Q") if hq and q_weight is not None else None,
-              view(K, n, hkv, "K") if hkv and k_weight is not None else None, view(dQ_out, m, hq, "dQ_out") if hq else None,
-              view(dK_out, m, hkv, "dK_out") if hkv else None, _vec(dq_weight, d, torch.float32, "dq_weight"),
-              _vec(dk_weight, d, torch.float32, "dk_weight"), None if workspace is None else workspace.data_ptr(),
-              0 if workspace is None else workspace.nbytes, _stream_handle(stream))
+    args = (_code(dt), r, m, None if rows is None else _vec(rows, m, torch.int32, "rows"), view(dQ, m, hq, "dQ"),
+            view(dK, m, hkv, "dK"), view(Q, n, hq, "Q") if hq and q_weight is not None else None,
+            view(K, n, hkv, "K") if hkv and k_weight is not None else None, view(dQ_out, m, hq, "dQ_out") if hq else None,
+            view(dK_out, m, hkv, "dK_out") if hkv else None, _vec(dq_weight, d, torch.float32, "dq_weight"),
+            _vec(dk_weight, d, torch.float32, "dk_weight"), None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.nbytes)
+    if host:
+        launchable(host, m > 0 or dq_weight is not None or dk_weight is not None, "rope.bwd")
+    rc = _bwd(*args, _stream_handle(stream))
     if rc != OK:
         _check(rc, "dsv_rope_bwd")
     return dQ_out if hq else None, dK_out if hkv else None, dq_weight, dk_weight

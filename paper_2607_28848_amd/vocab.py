@@ -13,7 +13,7 @@ from __future__ import annotations
 import ctypes
 
 from . import dsv
-from .attn import here, int32, on
+from .attn import here, int32, launchable, on
 from .dsv import _check, _ptr, _stream_handle, torch
 
 _lib = dsv.lib_handle()
@@ -144,11 +144,12 @@ def _distill_ws(given, like, T, K, V, k, grad, ldw, stream):
 def distill(X, W, ids, teacher, temperature=1.0, loss=None, workspace=None, stream=None):
     """dsv_vocab_distill: the divergence of softmax(X W^T / temperature) from the teacher of every row, fp32."""
     (T, K), V, k = X.shape, W.shape[0], ids.shape[-1]
-    here(X, W, ids, teacher, loss, workspace)
+    host = here(X, W, ids, teacher, loss, workspace)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     (x, ldx), (w, ldw) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W")
     i, t = _entries(ids, T, k, torch.int32, "ids"), _entries(teacher, T, k, torch.float32, "teacher")
     ws, n = _distill_ws(workspace, X, T, K, V, k, False, ldw, stream)
+    launchable(host, T > 0, "vocab.distill")
     _check(_lib.dsv_vocab_distill(_code(X.dtype), T, K, V, k, x, ldx, w, ldw, i, t, temperature,
                                   _vec(loss, T, torch.float32, "loss"), _ptr(ws), n, _stream_handle(stream)),
            "dsv_vocab_distill")
@@ -159,13 +160,14 @@ def distill_grad(X, W, ids, teacher, temperature=1.0, weight=None, Wt=None, loss
     """dsv_vocab_distill_grad; returns (loss, dX).  weight [T] fp32: the upstream gradient of each row's loss (ones if
     None).  Wt [K][V]: the head transposed, as loss_grad takes it."""
     (T, K), V, k = X.shape, W.shape[0], ids.shape[-1]
-    here(X, W, ids, teacher, weight, Wt, loss, dX, workspace)
+    host = here(X, W, ids, teacher, weight, Wt, loss, dX, workspace)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     dX = _new(dX, (T, K), X.dtype, X.device, stream)
     (x, ldx), (w, ldw), (dx, lddx) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W"), _mat(dX, T, K, X.dtype, "dX")
     wt, ldwt = _mat(Wt, K, V, X.dtype, "Wt") if Wt is not None else (None, 0)
     i, t = _entries(ids, T, k, torch.int32, "ids"), _entries(teacher, T, k, torch.float32, "teacher")
     ws, n = _distill_ws(workspace, X, T, K, V, k, True, ldw, stream)
+    launchable(host, T > 0, "vocab.distill_grad")
     _check(_lib.dsv_vocab_distill_grad(_code(X.dtype), T, K, V, k, x, ldx, w, ldw, wt, ldwt, i, t, temperature,
                                        _vec(weight, T, torch.float32, "weight"), _vec(loss, T, torch.float32, "loss"), dx, lddx,
                                        _ptr(ws), n, _stream_handle(stream)), "dsv_vocab_distill_grad")
