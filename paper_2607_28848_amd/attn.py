@@ -69,13 +69,21 @@ class HostTensors(DsvError, ValueError):
     """A call whose tensors are all in host memory, where its kernels would fault."""
 
 
-def here(*tensors) -> bool:
-    """ValueError unless the tensors (None: not given) are on one device, the current one where it is a GPU: a call's
-    kernels run there.  Returns whether they are in host memory, for launchable()."""
+def here(*tensors, stream=None) -> bool:
+    """ValueError unless the tensors (None: not given) are on one device and, where it is a GPU, on the call's: the stream's
+    own, whichever is current, and the current one without a stream.  Pinned host tensors may stand beside a GPU's.
+    Returns whether the tensors are in host memory that no GPU reads, for launchable()."""
     at = _marshal.where(*tensors)
-    if at >= 0 and at != torch.cuda.current_device():
-        raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (at, torch.cuda.current_device()))
-    return at < 0
+    if at >= 0:
+        # a stream that does not say its device is taken at its word; the default stream is the current device's
+        own = None if stream is None else getattr(stream, "device", None)
+        if stream is None or not stream.cuda_stream:
+            gpu = torch.cuda.current_device()
+        else:
+            gpu = at if own is None else own.index
+        if at != gpu:
+            raise ValueError("the tensors are on cuda:%d, the call's device is cuda:%d" % (at, gpu))
+    return at == -1
 
 
 def launchable(host: bool, work: bool, what: str):
@@ -179,7 +187,7 @@ def fwd(plan: Plan, Q, K, V, scale=None, O=None, lse=None, want_lse=None, worksp
     needs; without one it is made if want_lse, which stands for "where O is made" if None, else it is not written and
     None is returned for it (inference)."""
     hq, hkv, d = plan.heads_q, plan.heads_kv, plan.head_dim
-    here(plan.meta, Q, K, V, O, lse, workspace)
+    here(plan.meta, Q, K, V, O, lse, workspace, stream=stream)
     make_lse = lse is None and (O is None if want_lse is None else want_lse)
     if O is None or make_lse:
         with on(stream):
@@ -203,7 +211,7 @@ def bwd(plan: Plan, Q, K, V, O, lse, dO, scale=None, dQ=None, dK=None, dV=None, 
     hq, hkv, d, nq, nk = plan.heads_q, plan.heads_kv, plan.head_dim, plan.train_q, plan.train_k
     if lse is None and nq > 0:
         raise ValueError("lse is None: the forward returns it with lse=... or want_lse=True")
-    here(plan.meta, Q, K, V, O, lse, dO, dQ, dK, dV, workspace)
+    here(plan.meta, Q, K, V, O, lse, dO, dQ, dK, dV, workspace, stream=stream)
     if dQ is None or dK is None or dV is None:
         with on(stream):
             dQ, dK, dV = (t if t is not None else torch.empty((n, h, d), dtype=Q.dtype, device=Q.device)

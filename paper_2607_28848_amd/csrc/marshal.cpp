@@ -82,8 +82,9 @@ PyObject* vec(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// where(*tensors) -> the GPU that all tensors (None: not given) are on, -1 for host memory or none; ValueError where they
-// differ, or have no memory.
+// where(*tensors) -> the GPU that the tensors (None: not given) are on, -1 where all of them are in host memory; ValueError
+// where they differ, or have no memory.  Tensors without elements are anywhere, as is pinned host memory, which every GPU
+// reads and writes: -2 where there are no others.
 PyObject* where(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   const at::Tensor* first = nullptr;
@@ -92,6 +93,7 @@ PyObject* where(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!THPVariable_Check(a[i])) return PyErr_Format(PyExc_TypeError, "not a tensor: %R", a[i]);
     const at::Tensor& t = THPVariable_Unpack(a[i]);
     if (t.is_meta()) return PyErr_Format(PyExc_ValueError, "a tensor of the call has no memory");
+    if (t.numel() == 0 || (t.is_cpu() && t.is_pinned())) continue;
     if (!first) {
       first = &t;
     } else if (t.device() != first->device()) {
@@ -99,7 +101,7 @@ PyObject* where(PyObject*, PyObject* const* a, Py_ssize_t n) {
                           t.device().str().c_str());
     }
   }
-  return PyLong_FromLong(first && !first->is_cpu() ? first->device().index() : -1);
+  return PyLong_FromLong(!first ? -2 : first->is_cpu() ? -1 : first->device().index());
   END_HANDLE_TH_ERRORS
 }
 

@@ -92,7 +92,7 @@ def fwd(Q, K, pos, freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=Fal
     hq, hkv, dt = 0 if Q is None else Q.shape[1], 0 if K is None else _heads(K, "K")[1], like.dtype
     if slots is not None and (K_out is None or (V is not None and V_out is None)):
         raise ValueError("slots need K_out, and V_out where V is given")
-    host = here(Q, K, V, pos, freq, q_weight, k_weight, slots, Q_out, K_out, V_out)
+    host = here(Q, K, V, pos, freq, q_weight, k_weight, slots, Q_out, K_out, V_out, stream=stream)
     if hq:
         Q_out = made(Q_out, (n, hq, d), dt, Q, stream)
     if hkv:
@@ -134,7 +134,8 @@ def bwd(dQ, dK, pos, freq, rows=None, Q=None, K=None, q_weight=None, k_weight=No
     stated = next((t for t in (pos, Q, K) if t is not None), None)
     # nothing of a batch's rows is read where nothing states their number: every row that 32 bits name is one
     n = stated.shape[0] if stated is not None else m if rows is None else (1 << 31) - 1
-    host = here(dQ, dK, pos, freq, rows, Q, K, q_weight, k_weight, dQ_out, dK_out, dq_weight, dk_weight, workspace)
+    host = here(dQ, dK, pos, freq, rows, Q, K, q_weight, k_weight, dQ_out, dK_out, dq_weight, dk_weight, workspace,
+                stream=stream)
     if hq and q_weight is not None and (dQ_out is None if want_weights is None else want_weights):
         dq_weight = made(dq_weight, (d,), torch.float32, dQ, stream)
     if hkv and k_weight is not None and (dK_out is None if want_weights is None else want_weights):

@@ -144,7 +144,7 @@ def _distill_ws(given, like, T, K, V, k, grad, ldw, stream):
 def distill(X, W, ids, teacher, temperature=1.0, loss=None, workspace=None, stream=None):
     """dsv_vocab_distill: the divergence of softmax(X W^T / temperature) from the teacher of every row, fp32."""
     (T, K), V, k = X.shape, W.shape[0], ids.shape[-1]
-    host = here(X, W, ids, teacher, loss, workspace)
+    host = here(X, W, ids, teacher, loss, workspace, stream=stream)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     (x, ldx), (w, ldw) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W")
     i, t = _entries(ids, T, k, torch.int32, "ids"), _entries(teacher, T, k, torch.float32, "teacher")
@@ -160,7 +160,7 @@ def distill_grad(X, W, ids, teacher, temperature=1.0, weight=None, Wt=None, loss
     """dsv_vocab_distill_grad; returns (loss, dX).  weight [T] fp32: the upstream gradient of each row's loss (ones if
     None).  Wt [K][V]: the head transposed, as loss_grad takes it."""
     (T, K), V, k = X.shape, W.shape[0], ids.shape[-1]
-    host = here(X, W, ids, teacher, weight, Wt, loss, dX, workspace)
+    host = here(X, W, ids, teacher, weight, Wt, loss, dX, workspace, stream=stream)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     dX = _new(dX, (T, K), X.dtype, X.device, stream)
     (x, ldx), (w, ldw), (dx, lddx) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W"), _mat(dX, T, K, X.dtype, "dX")

@@ -14,6 +14,7 @@ STREAM = types.SimpleNamespace(cuda_stream=0)
 @pytest.fixture
 def given(monkeypatch):
     seen = []
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: False)  # the tensors are in host memory
     monkeypatch.setattr(rope, "_bwd", lambda dtype, r, n_rows, *rest: seen.append((struct.unpack_from("@i", r)[0], n_rows)) or 0)
     return seen
 
