@@ -93,9 +93,11 @@ def _new(given, shape, dtype, device, stream):
 def loss(X, W, target, loss=None, workspace=None, stream=None):
     """dsv_vocab_loss: -log softmax(X W^T)[target] of every row, fp32."""
     (T, K), V = X.shape, W.shape[0]
+    host = here(X, W, target, loss, workspace, stream=stream)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     (x, ldx), (w, ldw) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W")
     ws, n = _ws(workspace, X, T, K, V, False, ldw, stream)
+    launchable(host, T > 0, "vocab.loss")
     _check(_lib.dsv_vocab_loss(_code(X.dtype), T, K, V, x, ldx, w, ldw, _vec(target, T, torch.int32, "target"),
                                _vec(loss, T, torch.float32, "loss"), _ptr(ws), n, _stream_handle(stream)),
            "dsv_vocab_loss")
@@ -106,11 +108,13 @@ def loss_grad(X, W, target, weight=None, Wt=None, loss=None, dX=None, workspace=
     """dsv_vocab_loss_grad; returns (loss, dX).  weight [T] fp32: the upstream gradient of each row's loss (ones if
     None).  Wt [K][V]: the head transposed, kept by the caller (read for bf16 where V is a multiple of 8 below 2^22)."""
     (T, K), V = X.shape, W.shape[0]
+    host = here(X, W, target, weight, Wt, loss, dX, workspace, stream=stream)
     loss = _new(loss, (T,), torch.float32, X.device, stream)
     dX = _new(dX, (T, K), X.dtype, X.device, stream)
     (x, ldx), (w, ldw), (dx, lddx) = _mat(X, T, K, X.dtype, "X"), _mat(W, V, K, X.dtype, "W"), _mat(dX, T, K, X.dtype, "dX")
     wt, ldwt = _mat(Wt, K, V, X.dtype, "Wt") if Wt is not None else (None, 0)
     ws, n = _ws(workspace, X, T, K, V, True, ldw, stream)
+    launchable(host, T > 0, "vocab.loss_grad")
     _check(_lib.dsv_vocab_loss_grad(_code(X.dtype), T, K, V, x, ldx, w, ldw, wt, ldwt,
                                     _vec(target, T, torch.int32, "target"), _vec(weight, T, torch.float32, "weight"),
                                     _vec(loss, T, torch.float32, "loss"), dx, lddx, _ptr(ws), n, _stream_handle(stream)),

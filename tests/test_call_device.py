@@ -65,3 +65,18 @@ def test_pinned_tensors_beside_the_gpus():
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(a, b)) and torch.equal(*losses)
     assert _marshal.where(q, kept) == 0 and _marshal.where(kept) == -2
+
+
+@pytest.mark.gpu
+def test_the_loss_refuses_what_the_other_calls_refuse():
+    from paper_2607_28848_amd import vocab
+    X, W, target = torch.zeros((6, 64)), torch.zeros((50, 64)), torch.zeros(6, dtype=torch.int32)
+    calls = [lambda x, w, t, **how: vocab.loss(x, w, t, **how), lambda x, w, t, **how: vocab.loss_grad(x, w, t, **how)]
+    for call in calls:
+        for bad in ((X, W.cuda(), target.cuda()), (X.cuda(), W, target.cuda()), (X.cuda(), W.cuda(), target), (X, W, target)):
+            with pytest.raises(ValueError):
+                call(*bad)
+        with pytest.raises(ValueError):
+            call(X.cuda(), W.cuda(), target.cuda(), loss=torch.zeros(6))
+    with pytest.raises(ValueError):
+        vocab.loss_grad(X.cuda(), W.cuda(), target.cuda(), dX=X.clone())

@@ -78,3 +78,17 @@ def test_without_a_gpu_the_library_answers(entered, call, monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_available", lambda: False)
     call()
     assert len(entered) == 1
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_the_loss_refuses_them_too(entered, grad):
+    def call(T):
+        X, how = torch.zeros((T, 16)), dict(loss=torch.zeros(T), workspace=torch.zeros(256, dtype=torch.uint8), stream=STREAM)
+        if grad:
+            how["dX"] = X.clone()
+        (vocab.loss_grad if grad else vocab.loss)(X, torch.zeros((8, 16)), POS[:T], **how)
+    with pytest.raises(ValueError, match="host memory"):
+        call(6)
+    assert not entered
+    call(0)
+    assert len(entered) == 1
