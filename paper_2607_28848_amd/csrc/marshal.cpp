@@ -8,7 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
-#include <cstring>
+#include <string>
 
 namespace {
 
@@ -54,8 +54,11 @@ PyObject* view(PyObject*, PyObject* const* a, Py_ssize_t n) {
   } else if (shape.size() == 2 && shape[0] == rows && shape[1] == heads * d) {
     row = stride[0], head = d * stride[1], one = stride[1];
   } else {
-    return PyErr_Format(PyExc_ValueError, "%S must be [%lld][%lld][%lld], got another shape (%zu dimensions)", name,
-                        (long long)rows, (long long)heads, (long long)d, shape.size());
+    std::string got;
+    for (const int64_t x : shape) got += (got.empty() ? "" : ", ") + std::to_string(x);
+    if (shape.size() == 1) got += ',';
+    return PyErr_Format(PyExc_ValueError, "%S must be [%lld][%lld][%lld], got (%s)", name, (long long)rows, (long long)heads,
+                        (long long)d, got.c_str());
   }
   if (one != 1 && rows) return PyErr_Format(PyExc_ValueError, "%S: the elements of a head must be contiguous", name);
   // the library takes a stride of 0 for the dense one
