@@ -83,12 +83,15 @@ struct Chunk<float> {
   }
 };
 
-// Cosine and sine of pos * freq radians.  The angle in quarter turns is formed and reduced to [-1/2, 1/2] in 64 bits;
-// what is left, at most pi / 4, goes through the Taylor series of both (next terms below 3e-9 and 2e-10 of the value).
+// Cosine and sine of pos * freq radians.  The frequency in quarter turns is held in two 64-bit parts, and the angle less its
+// whole quarters, in [-1/2, 1/2], is one fma, so nothing is rounded before the reduction (an angle of 2^31 quarters in 64 bits
+// is up to 2.4e-7 of one off); what is left, at most pi / 4, goes through the Taylor series of both (next terms below 3e-9 and
+// 2e-10 of the value).
 __device__ __forceinline__ float2 turn_of(int pos, double freq) {
-  const double quarters = (double)pos * (freq * 0.63661977236758134308);  // 2 / pi
-  const double whole = rint(quarters);
-  const float x = (float)((quarters - whole) * 1.57079632679489661923), x2 = x * x;
+  constexpr double kHigh = 0.6366197723675814, kLow = -3.935735335036497e-17;  // 2 / pi
+  const double f = freq * kHigh, f_low = fma(freq, kHigh, -f) + freq * kLow;
+  const double p = pos, whole = rint(p * f);
+  const float x = (float)((fma(p, f, -whole) + p * f_low) * 1.57079632679489661923), x2 = x * x;
   const float s = x + x * x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880))));
   const float c = 1.f + x2 * (-0.5f + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 + x2 * (-1.f / 3628800)))));
   const int turn = (int)(whole - 4. * floor(whole * 0.25));  // 0 to 3
