@@ -523,9 +523,10 @@ int dsv_gemm_config(const dsv_plan* plan, dsv_dtype dtype, int32_t K, int32_t N,
  *     u = x w / sqrt(mean(x^2) + eps)
  *     y_a = u_a cos t - u_b sin t,  y_b = u_b cos t + u_a sin t,  t = p freq[i]
  * for the pairs (a, b) = (i, i + rotated / 2), or (2 i, 2 i + 1) where interleaved, of
- * i < rotated / 2; the elements from `rotated` on keep u.  Angles (up to
- * 2^50 radians) are reduced to a quarter turn before they are rounded, so far positions
- * turn as exactly as near ones; norms and rotations are fp32, every output is rounded once.  Backward, with g the upstream gradient turned back:
+ * i < rotated / 2; the elements from `rotated` on keep u.  Angles (up to 2^50 radians) are
+ * reduced to a quarter turn before they are rounded, so far positions turn as exactly as
+ * near ones; norms and rotations are fp32, every output is rounded once.  Backward, with
+ * g the upstream gradient turned back:
  *     dw += g x / sqrt(mean(x^2) + eps)          (over rows and heads)
  *     dx = (g w - x mean(g w x) / (mean(x^2) + eps)) / sqrt(mean(x^2) + eps)
  * No atomics: repeated calls give the same bits.  The norm squares in fp32: a vector

@@ -172,6 +172,14 @@ __device__ __forceinline__ float square_sum(const float (&x)[16]) {
   return s;
 }
 
+// 1 / sqrt(x) to half a step and a little: the instruction's result, off by up to a whole one, and a Newton step whose
+// residue 1 - x r^2 is formed without rounding x r.  The kernels wait for memory meanwhile.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float r = __builtin_amdgcn_rsqf(x), t = x * r;
+  const float rest = fmaf(-fmaf(x, r, -t), r, fmaf(-t, r, 1.f));
+  return x < INFINITY ? fmaf(0.5f * rest, r, r) : r;
+}
+
 template <typename T>
 __device__ __forceinline__ T* element(const AttnView& t, int64_t row, int h) {
   return static_cast<T*>(t.ptr) + row * t.row + h * t.head;
@@ -208,7 +216,7 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs a) {
       if (weight) {
         float wt[16];
         weight_of<D>(weight, at, wt);
-        const float r = __builtin_amdgcn_rsqf(sum * (1.f / D) + a.eps);
+        const float r = inverse_root(sum * (1.f / D) + a.eps);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = v[i] * r * wt[i];
       }
@@ -258,7 +266,7 @@ __global__ __launch_bounds__(256, 4) void rope_bwd_kernel(RopeArgs a) {
         px.get(x), qx.get(x + 8);
         float wt[16], dot = 0.f;
         weight_of<D>(k.weight, at, wt);
-        const float r = __builtin_amdgcn_rsqf(head_sum<LPH>(square_sum(x)) * (1.f / D) + a.eps);
+        const float r = inverse_root(head_sum<LPH>(square_sum(x)) * (1.f / D) + a.eps);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           x[e] *= r;
