@@ -566,7 +566,7 @@ typedef struct {
  * Q_out may be Q itself, the same address and strides; without slots K_out may be K.
  * Errors: DSV_ERR_ARG (null or misaligned pointer, negative count), DSV_ERR_RANGE (dtype,
  * heads, head_dim, rotated, flag, eps), DSV_ERR_SIZE (strides, overlapping outputs, more
- * than 2^31 - 1 work items).
+ * than 2^32 - 1 work items: 64 for each row and share of its heads).
  */
 int dsv_rope_fwd(dsv_dtype dtype, const dsv_rope* rope, const dsv_attn_view* Q, const dsv_attn_view* K,
                  const dsv_attn_view* V, const int32_t* slots, int32_t n_slots, const dsv_attn_view* Q_out,
@@ -733,7 +733,7 @@ int dsv_vocab_workspace(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_
 
 /* The losses alone (scoring): the head is read once.  Errors: DSV_ERR_ARG (null or
  * misaligned pointer, T < 0), DSV_ERR_RANGE (dtype), DSV_ERR_SIZE (shape, stride,
- * workspace). */
+ * workspace, T or the tiles of the logits from 2^24 on). */
 int dsv_vocab_loss(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const void* X, int32_t ldx, const void* W,
                    int32_t ldw, const int32_t* target, float* loss, void* workspace, size_t workspace_bytes,
                    void* hip_stream);
@@ -766,9 +766,9 @@ int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const 
  * bf16 mode dX keeps its accuracy where student and teacher agree; the others are rounded
  * to bf16 once.  No atomics: repeated calls give the same bits.
  *
- * ids [T][k] int32 and teacher [T][k] fp32, dense, 4-byte aligned; 1 <= k <= 1024
- * (DSV_ERR_SIZE).  temperature positive and finite, as are 1 / tau and, in fp32, log2 e /
- * tau (DSV_ERR_RANGE).  Other errors as dsv_vocab_loss and dsv_vocab_loss_grad.
+ * ids [T][k] int32 and teacher [T][k] fp32, dense, 4-byte aligned; 1 <= k <= 1024, and T
+ * times the groups of 16 entries below 2^24 (DSV_ERR_SIZE).  temperature positive and finite,
+ * as are 1 / tau and, in fp32, log2 e / tau (DSV_ERR_RANGE).  Other errors as dsv_vocab_loss and dsv_vocab_loss_grad.
  */
 int dsv_vocab_distill_workspace(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, int32_t k, int32_t ldw, int32_t grad,
                                 size_t* bytes);

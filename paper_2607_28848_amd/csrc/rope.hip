@@ -434,7 +434,7 @@ extern "C" int dsv_rope_fwd(dsv_dtype dt, const dsv_rope* r, const dsv_attn_view
   const int blocks = (a.hq + a.hkv + a.hv + hpw - 1) / hpw, shared = dt == DSV_BF16 ? (blocks + 2) / 3 : blocks;
   a.split = (int64_t)r->n * shared < kFwdWaves ? blocks : shared;
   const int64_t groups = ((int64_t)r->n * a.split + 3) / 4;
-  if (groups > INT32_MAX) return DSV_ERR_SIZE;
+  if (groups > UINT32_MAX / 256) return DSV_ERR_SIZE;  // a grid's work items are counted in 32 bits
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (dt == DSV_BF16)
     return status(r->interleaved ? launch_fwd<uint16_t, true>(a, d, groups, s) : launch_fwd<uint16_t, false>(a, d, groups, s));

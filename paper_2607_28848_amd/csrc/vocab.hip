@@ -553,11 +553,17 @@ int check_shape(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int32_t ldw, int6
   return stride(ldw, K, w);
 }
 
+// A logits tile's rows.
+int tile_rows(bool bf, int tw, int32_t T) { return !bf ? vocab_f32_rows(T) : tw < 256 ? tw : T <= 128 ? 128 : 256; }
+
+// Workgroups of 256 in a launch: its work items are counted in 32 bits.
+constexpr int64_t kMostGroups = UINT32_MAX / 256;
+
 // Tiles of 64 rows have six buffers where each has a CU to itself, else four, which leave room for two on a CU (one row of
 // 4096 against 5000: 22 us with six, 25 with four; 45 rows of 816 against 113000: 65 and 57).
 template <bool GRAD, bool KD>
 hipError_t launch_logits(const VocabArgs& a, int cus, hipStream_t s) {
-  const int tm = a.tw < 256 ? a.tw : a.T <= 128 ? 128 : 256;
+  const int tm = tile_rows(true, a.tw, a.T);
   const unsigned tiles = (unsigned)(a.n_ct * (int64_t)((a.T + tm - 1) / tm));
   const dim3 grid(tiles + (KD ? a.n_entry : 0));
   if (a.tw == 64 && tiles <= (unsigned)cus)
@@ -612,8 +618,11 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   const Entries en = entries(pc.total, a.T, a.k);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
   if (ws_bytes < (kd ? en.total : pc.total)) return DSV_ERR_SIZE;
-  // the first launch's workgroups
-  if (kd && (int64_t)a.T * entry_groups(a.k) + (int64_t)((a.T + 31) / 32) * (pc.width / pc.tw) > INT32_MAX) return DSV_ERR_SIZE;
+  const int64_t all_entries = kd ? (int64_t)a.T * entry_groups(a.k) : 0;
+  // the entries' workgroups, ahead of the tiles (when they are few) or on their own; the rows'
+  if (std::max((int64_t)a.T, all_entries) > kMostGroups ||
+      (int64_t)((a.T - 1) / tile_rows(bf, pc.tw, a.T) + 1) * (pc.width / pc.tw) + kEntriesAhead * cus > kMostGroups)
+    return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
   char* b = static_cast<char*>(ws);
   a.P = a.keep ? b + pc.p : nullptr;
@@ -640,7 +649,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     a.first = i == 0;
     a.last = i + 1 == pc.n;
     a.split = pc.split;
-    const int64_t n_entry = kd && a.first ? (int64_t)a.T * entry_groups(a.k) : 0;
+    const int64_t n_entry = a.first ? all_entries : 0;
     // ahead of the tiles, or on their own
     const bool apart = n_entry > kEntriesAhead * cus;
     a.n_entry = apart ? 0 : (int32_t)n_entry;
