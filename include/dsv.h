@@ -759,12 +759,12 @@ int dsv_vocab_loss_grad(dsv_dtype dtype, int32_t T, int32_t K, int32_t V, const 
  * different temperatures alike is the caller's, in weight).  An id outside [0, V) is no
  * entry (padding); a teacher logit of -infinity is an entry of q = 0.  A row without an
  * entry of q > 0 has loss 0 and dx zeros, whatever it holds.  The same id twice: two
- * entries, each with its q (so the loss can be below 0 there).  Teacher logits are finite or
- * -infinity; others give NaN.  The cross entropy's conventions hold else: the logits are
- * never held whole, shapes, strides, alignment, Wt, and its workspace but for the entries'
- * room.  The student's terms at the teacher's ids are formed apart in fp32 or more, so in
- * bf16 mode dX keeps its accuracy where student and teacher agree; the others are rounded
- * to bf16 once.  No atomics: repeated calls give the same bits.
+ * entries, each with its q (so the loss can be below 0 there, and only there).  Teacher
+ * logits are finite or -infinity; others give NaN.  The cross entropy's conventions hold
+ * else: the logits are never held whole, shapes, strides, alignment, Wt, and its workspace
+ * but for the entries' room.  The student's terms at the teacher's ids are formed apart in fp32 or more, so where
+ * student and teacher agree dX keeps its accuracy in bf16 mode, and a loss near 0 its own in
+ * both; the other terms are rounded to bf16 once.  No atomics: repeated calls give the same bits.
  *
  * ids [T][k] int32 and teacher [T][k] fp32, dense, 4-byte aligned; 1 <= k <= 1024, and T
  * times the groups of 16 entries below 2^24 (DSV_ERR_SIZE).  temperature positive and finite,

@@ -22,16 +22,17 @@ struct VocabArgs {
   int32_t v0, vn;
   int32_t tw, n_ct;       // width and number of the piece's column tiles
   int32_t first, last;    // the piece is the first / the last
-  int32_t grad;           // the gradient is wanted
-  int32_t keep;           // P is kept
+  int32_t grad;
   // Exponents are base 2: a row's reference r stands for 2^r.
-  void* P;                // [T][ldp] 2^(z log2 e - reference) of the piece, the target's left out (keep)
+  void* P;                // [T][ldp] 2^(c z - reference) of the piece, the target's or the entries' left out (grad)
   int64_t ldp;
   float2* stats;          // [T][ld_stats] per column tile: reference, sum of its P
   int64_t ld_stats;
   float* ref;             // [T] the row's reference
-  float* others;          // [T] sum of the terms that are not the target's, at the reference
-  float* term;            // [T] the target's term at the reference (after the last piece)
+  float* others;          // [T] sum of the terms that are not the target's or the entries', at the reference; distillation:
+                          // after the last piece the sum of all
+  float* term;            // [T] the target's term at the reference (after the last piece); distillation: whether the row has
+                          // an entry of share > 0 (0: no, 2: and one of them names an earlier one's token)
   float* alpha;           // [T] what the sums so far are multiplied by (the reference moved)
   // Distillation: k entries a row, [T][k] each, and what the rows' sums of them come to.
   const int32_t* ids;
@@ -44,7 +45,7 @@ struct VocabArgs {
                           // at an earlier one
   float* share;           // the teacher's probability of it; below 0 (or -0) until the first fold where its token stands earlier
   double* log_share;      // its logarithm, base 2
-  double* base;           // [T] sum of share (log_share - c z)
+  double* base;           // [T] sum of the probabilities (in 64 bits) times log_share - c z
   // second product: contraction in `split` ranges of split_len columns, each with its own sums
   float* O;               // [split][T][K]
   int32_t split, split_len;

@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.h"
 #include "dsv.h"
@@ -23,7 +24,6 @@
 
 namespace dsv {
 namespace {
-
 
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -47,6 +47,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
   __shared__ __attribute__((aligned(1024))) char smem0[kStage];
   __shared__ __attribute__((aligned(1024))) char smem1[kStage];
   __shared__ float red[3][2][TM];  // [maximum, sum, reference][column half][row]
+  __shared__ __attribute__((aligned(16))) uint32_t mark[KD ? TM : 1][TN / 32];  // the entries' elements
   const int n_m = (a.T + TM - 1) / TM, ahead = KD ? a.n_entry : 0;
   if (KD && (int)blockIdx.x < ahead) {
     entry_exponents<uint16_t>(a, blockIdx.x);
@@ -63,6 +64,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
   const int turn = n_m == 1 ? nt : 0;
   const uint16_t* const X = static_cast<const uint16_t*>(a.X) + (int64_t)m0 * a.ldx;
   const uint16_t* const W = static_cast<const uint16_t*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw;
+  // The entries: few rows' ids wait in registers for the end of the tile's stream, which they would delay; whole tiles
+  // have no registers for that.
+  struct None {
+    __device__ __forceinline__ None(const VocabArgs&, int, uint32_t (&)[1][TN / 32]) {}
+  };
+  std::conditional_t<KD, EntryMarks<TM, TN, FM == 8 ? 8 : 2>, None> marks(a, m0, mark);
+  if constexpr (KD && FM == 8) {
+    __syncthreads();
+    marks.put(mark, a.v0 + n0, cols);
+  }
   char* idle = smem0;
   if constexpr (NB == 2) {
     idle = tile_nt<FM>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, smem0, smem1, acc);
@@ -84,6 +95,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
       tile_ring<uint16_t, FM, FN, 6>(X, a.ldx, a.T - m0, W, a.ldw, cols, a.K, turn, ring, acc);
     }
   }
+  if constexpr (KD && FM < 8) marks.put(mark, a.v0 + n0, cols);
   const int c0 = wn * WN + 4 * g4;  // column of acc[.][j][v]: c0 + 16 j + v
   // The sums are read twice and never written: in registers of the matrix core from the first to the last.
 #pragma unroll
@@ -119,6 +131,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
       const float have = !a.first && in ? a.ref[row] : 0.f;
       const float ref = tile_reference(m, have, a.first), base = ref == -INFINITY ? 0.f : ref;
       const int tc = !KD && in ? a.target[row] - a.v0 - n0 - c0 : -1;  // the target's column, from the lane's first
+      uint32_t marked[WN / 32];  // the lane's bits, from bit 4 g4 on
+      if constexpr (KD)
+#pragma unroll
+        for (int w = 0; w < WN / 32; ++w) marked[w] = mark[r][wn * (WN / 32) + w] >> (4 * g4);
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
@@ -127,9 +143,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, NB == 2 
         for (int v = 0; v < 4; ++v) {
           const float z = acc[i][j][v];
           e[v] = __builtin_amdgcn_exp2f(z * a.c - base);
-          if (tc == 16 * j + v) e[v] = 0.f;
+          if (!KD && tc == 16 * j + v) e[v] = 0.f;
           if (cols < TN && c0 + 16 * j + v >= cols) e[v] = 0.f;
-          sum += e[v];
+          if (!KD) sum += e[v];
+        }
+        if constexpr (KD) {
+          const uint32_t out = marked[j / 2] >> 16 * (j & 1) & 15;
+          if (out) {  // few
+#pragma unroll
+            for (int v = 0; v < 4; ++v) e[v] = out >> v & 1 ? 0.f : e[v];
+          }
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sum += e[v];
         }
         if constexpr (GRAD)
           *reinterpret_cast<uint2*>(slice + (16 * h + l15) * SRS + 2 * (16 * j + 4 * g4)) =
@@ -260,9 +285,11 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a) {
 // reference are brought to the row's.  After the last piece the target's logit, its term and the loss, in 64 bits: the
 // logarithm and the logit nearly cancel for a sure row, and there is one of each per row (one row against 128256 of
 // 4096: the loss is off by 8e-7 in the root mean square with the logit from the products, whose sums are fp32).
-// KD (distillation): no target, and the entries' terms come out of P.  Where P holds the terms as they were summed (fp32), the entries' are taken out of the sum as well and the ones
-// of entry_exponents put in: a sure row's total and its largest term then have the same error, which drops out of p - q
-// (333 rows against 5003 of 512: dX off by 2.6e-6 in the root mean square with the products' own terms in the sum).
+// KD (distillation): the entries are left out as the target is, and entry_exponents' terms put in behind the last piece, S of
+// them beside R others: a sure row's total and its largest term then have the same error, which drops out of p - q (fp32, 333
+// rows against 5003 of 512: dX off by 2.6e-6 in the root mean square with the products' own terms in the sum).  The loss is
+// sum q (log q - log of the student's share among the entries), which 64 bits hold, and log (1 + R / S): near 0 it keeps the
+// accuracy of R.
 template <typename T, bool KD>
 __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
   __shared__ float red[4];
@@ -296,11 +323,10 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     moved |= x.x != ref;
   }
   sum = block_sum<4>(sum, red);
-  float others = 0.f;  // the first thread's
   if (threadIdx.x == 0) {
     const float f = have == -INFINITY ? 0.f : exp2f(have - ref);
-    others = (a.first ? 0.f : a.others[row] * f) + sum;
-    if (!KD) a.others[row] = others;
+    const float others = (a.first ? 0.f : a.others[row] * f) + sum;
+    a.others[row] = others;
     a.ref[row] = ref;
     a.alpha[row] = f;
     if (!KD && a.last) {
@@ -314,7 +340,7 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     }
   }
   T* P = static_cast<T*>(a.P) + (int64_t)row * a.ldp;
-  if (a.keep && __syncthreads_or(moved)) {
+  if (a.grad && __syncthreads_or(moved)) {
     constexpr int E = 16 / sizeof(T);
     for (int64_t c = threadIdx.x * E; c < (int64_t)a.n_ct * a.tw; c += 256 * E) {
       const float r = st[c / a.tw].x;
@@ -332,46 +358,43 @@ __global__ __launch_bounds__(256) void vocab_fold_kernel(VocabArgs a) {
     }
   }
   if constexpr (KD) {
-    constexpr bool F32 = sizeof(T) == 4;
     if (a.first && !a.shares_ahead) teacher_shares(a, row);  // an entry's are its thread's own in what follows
-    if (a.first) {
-      // what the loss takes from the entries, and each token's exponent at its first entry alone
-      double sum = 0.;
-      for (int j = threadIdx.x; j < a.k; j += 256) {
-        const int64_t at = (int64_t)row * a.k + j;
+    // The first piece: what the loss takes from the entries, and each token's exponent at its first entry alone.  The last:
+    // their terms.
+    double sum = 0., put = 0.;
+    bool twice = false;
+    for (int j = threadIdx.x; (a.first || a.last) && j < a.k; j += 256) {
+      const int64_t at = (int64_t)row * a.k + j;
+      double x = a.exponent[at];
+      if (a.first) {
         const float share = a.share[at];
-        if (share != 0.f) sum += fabs(share) * (a.log_share[at] - a.exponent[at]);
+        const double log_share = a.log_share[at], q = log_share == -INFINITY ? 0. : exp2(log_share);
+        if (q != 0.) sum += q * (log_share - x);
         if (__float_as_uint(share) >> 31) {
           a.share[at] = -share;
-          a.exponent[at] = -INFINITY;
+          a.exponent[at] = x = -INFINITY;
+          twice |= q != 0.;
         }
       }
+      if (a.last && x != -INFINITY) put += exp2(x - ref);  // -infinity: no entry, or one that another stands for
+    }
+    if (a.first) {
       sum = block_sum<4>(sum, red64);
-      if (threadIdx.x == 0) a.base[row] = sum;
-    }
-    __syncthreads();
-    double put = 0.;  // what comes into the sum: all of it that is to, in the last piece
-    float out = 0.f;
-    for (int j = threadIdx.x; a.keep && j < a.k; j += 256) {
-      const double x = a.exponent[(int64_t)row * a.k + j];
-      if (x == -INFINITY) continue;  // none, or one that another entry stands for
-      const int at = a.ids[(int64_t)row * a.k + j] - a.v0;
-      if ((uint32_t)at < (uint32_t)a.vn) {
-        if constexpr (F32) out += P[at];
-        P[at] = 0;
+      twice = __syncthreads_or(twice);
+      if (threadIdx.x == 0) {
+        a.base[row] = sum;
+        if (twice) a.term[row] = 2.f;
       }
-      if (F32 && a.last) put += exp2(x - ref);
     }
-    if (F32) {
-      out = block_sum<4>(out, red);
-      if (a.last) put = block_sum<4>(put, red64);
-    }
+    if (!a.last) return;
+    put = block_sum<4>(put, red64);
     if (threadIdx.x == 0) {
-      const float rest = F32 ? others - out : others;
-      const double total = (rest < 0.f ? 0.f : rest) + put;  // a NaN stays one
-      a.others[row] = (float)total;
-      if (a.last && a.loss)
-        a.loss[row] = a.term[row] == 0.f ? 0.f : (float)((a.base[row] + log2(total) + ref) * 0.69314718055994531);
+      const double others = a.others[row], base = a.base[row];
+      a.others[row] = (float)(others + put);
+      double loss = others < put ? base + log2(put) + ref + log1p(others / put) * 1.4426950408889634
+                                 : base + log2(others + put) + ref;
+      if (loss < 0. && a.term[row] == 1.f) loss = 0.;  // entries of different tokens: rounding, in 64 bits
+      if (a.loss) a.loss[row] = a.term[row] == 0.f ? 0.f : (float)(loss * 0.69314718055994531);
     }
   }
 }
@@ -486,16 +509,14 @@ int logits_tile(int32_t T, int64_t width, int cus) {
 
 constexpr int64_t kPieceBytes = 256 << 20;  // of P: the size of the last-level cache
 
-// kd: a distillation, whose sums in fp32 need P for the losses alone as well (vocab_fold).
-Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool grad, bool kd, int cus) {
+Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool grad, int cus) {
   Pieces r{};
   const bool bf = dt == DSV_BF16;
   const int64_t size = bf ? 2 : 4;
   r.tw = bf ? 256 : 128;
   int64_t width = (V + r.tw - 1) / r.tw * r.tw;
   r.split = 1;
-  const bool keep = grad || (kd && !bf);
-  if (keep) {
+  if (grad) {
     // P within its room; 32-bit offsets of the second product's reads of W and of a tile's (up to 256) rows of P
     const int64_t most = std::min({kPieceBytes / (size * std::max(T, 1)), ((int64_t)1 << 30) / (size * ldw),
                                    (((int64_t)1 << 31) - 1) / (size * 256)}) / r.tw * r.tw;
@@ -526,7 +547,7 @@ Pieces pieces(dsv_dtype dt, int32_t T, int32_t K, int32_t V, int64_t ldw, bool g
     at += align256(bytes);
     return o;
   };
-  r.p = room(keep ? (size_t)T * r.width * size : 0);
+  r.p = room(grad ? (size_t)T * r.width * size : 0);
   r.stats = room((size_t)T * (r.width / r.tw) * sizeof(float2));
   r.rows = room((size_t)T * 4 * sizeof(float));
   r.o = room(grad ? (size_t)r.split * T * K * sizeof(float) : 0);
@@ -613,8 +634,7 @@ Entries entries(size_t from, int32_t T, int32_t k) {
 int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
   const bool bf = dt == DSV_BF16, kd = a.k > 0;
   const int cus = device_cus();
-  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, kd, cus);
-  a.keep = a.grad || (kd && !bf);
+  const Pieces pc = pieces(dt, a.T, a.K, a.V, a.ldw, a.grad != 0, cus);
   const Entries en = entries(pc.total, a.T, a.k);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return DSV_ERR_ARG;
   if (ws_bytes < (kd ? en.total : pc.total)) return DSV_ERR_SIZE;
@@ -625,7 +645,7 @@ int run(VocabArgs a, dsv_dtype dt, void* ws, size_t ws_bytes, hipStream_t s) {
     return DSV_ERR_SIZE;
   if (a.T == 0) return DSV_OK;
   char* b = static_cast<char*>(ws);
-  a.P = a.keep ? b + pc.p : nullptr;
+  a.P = a.grad ? b + pc.p : nullptr;
   a.ldp = pc.width;
   a.stats = reinterpret_cast<float2*>(b + pc.stats);
   a.ld_stats = pc.width / pc.tw;
@@ -691,7 +711,7 @@ extern "C" int dsv_vocab_workspace(dsv_dtype dt, int32_t T, int32_t K, int32_t V
   int64_t w = 0;
   const int rc = check_shape(dt, T, K, V, ldw, &w);
   if (rc != DSV_OK) return rc;
-  *bytes = pieces(dt, T, K, V, w, grad != 0, false, device_cus()).total;
+  *bytes = pieces(dt, T, K, V, w, grad != 0, device_cus()).total;
   return DSV_OK;
 }
 
@@ -756,7 +776,7 @@ extern "C" int dsv_vocab_distill_workspace(dsv_dtype dt, int32_t T, int32_t K, i
   const int rc = check_shape(dt, T, K, V, ldw, &w);
   if (rc != DSV_OK) return rc;
   if (k < 1 || k > kMaxEntries) return DSV_ERR_SIZE;
-  *bytes = entries(pieces(dt, T, K, V, w, grad != 0, true, device_cus()).total, T, k).total;
+  *bytes = entries(pieces(dt, T, K, V, w, grad != 0, device_cus()).total, T, k).total;
   return DSV_OK;
 }
 

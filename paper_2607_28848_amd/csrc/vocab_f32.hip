@@ -9,6 +9,8 @@
 // 25 us and 23 for the products, 52 a pass: two waves a SIMD for 16 steps, and the tiles' start and end.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "gemm_tile.h"
 #include "vocab.h"
@@ -134,6 +136,7 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   __shared__ __attribute__((aligned(1024))) char b1[kStage];
   __shared__ __attribute__((aligned(1024))) char b2[kStage];
   __shared__ float red[2][2][TM];
+  __shared__ __attribute__((aligned(16))) uint32_t mark[KD ? TM : 1][4];  // the entries' elements
   // the row tiles of a column tile one after the other: they share the head's rows in L2
   const int ahead = KD ? a.n_entry : 0;
   if (KD && (int)blockIdx.x < ahead) {
@@ -145,9 +148,14 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
   const int m0 = TM * mt, n0 = 128 * nt, cols = min(128, a.vn - n0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l15 = lane & 15;
   f32x4 acc[FM][4];
+  struct None {
+    __device__ __forceinline__ None(const VocabArgs&, int, uint32_t (&)[1][4]) {}
+  };
+  std::conditional_t<KD, EntryMarks<TM, 128, 2>, None> marks(a, m0, mark);
   char* const ring[3] = {b0, b1, b2};
   tile_ring<float, FM, 4, 3>(static_cast<const float*>(a.X) + (int64_t)m0 * a.ldx, a.ldx, a.T - m0,
                              static_cast<const float*>(a.W) + (int64_t)(a.v0 + n0) * a.ldw, a.ldw, cols, a.K, 0, ring, acc);
+  if constexpr (KD) marks.put(mark, a.v0 + n0, cols);
   const int c0 = 64 * wn + 4 * (lane >> 4);
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
@@ -173,17 +181,21 @@ __global__ __launch_bounds__(256) void vocab_f32_logits_kernel(VocabArgs a) {
     ref[i] = tile_reference(m, have, a.first);
     const float base = ref[i] == -INFINITY ? 0.f : ref[i];
     const int t = !KD && in ? a.target[row] - a.v0 - n0 - c0 : -1;
+    uint32_t marked[2];  // the lane's bits, from bit 4 (l / 16) on
+    if constexpr (KD)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) marked[w] = mark[r][2 * wn + w] >> (4 * (lane >> 4));
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         float e = exp2f(acc[i][j][v] * a.c - base);
-        if (t == 16 * j + v) e = 0.f;
+        if (KD ? (marked[j / 2] >> (16 * (j & 1) + v)) & 1 : t == 16 * j + v) e = 0.f;
         sum += e;
         acc[i][j][v] = e;
       }
-      if (a.keep && in)
+      if (a.grad && in)
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.P) + (int64_t)row * a.ldp + n0 + c0 + 16 * j) = acc[i][j];
     }
     sum = quad_sum(sum);
