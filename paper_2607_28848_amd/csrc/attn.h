@@ -18,7 +18,8 @@ struct AttnArgs {
   const int32_t* seqs;   // sequence descriptors (attn_plan.h)
   const int32_t* items;  // the launch's work items
   int32_t n_items;       // fp32 launches
-  int32_t parts;         // fp32 dK and dV: ranges of a key head's query heads
+  int32_t parts;         // fp32 dK and dV: ranges of a key head's query heads, or of the steps of
+  int32_t cut;           // the first `cut` items, with a window (the others are whole)
   int32_t hq, hkv, group, d;
   int32_t n_q;           // row length of lse ([hq][n_q])
   int64_t train_q;       // row length of delta ([hq][train_q])
@@ -31,7 +32,7 @@ struct AttnArgs {
   // Sums of pieces, by slot.  Split form: [slot][hkv][kAttnPackRows][D] sums of 2^(s - m) v, and
   // [slot][hkv][2][kAttnPackRows] m and sum of 2^(s - m).  Forward tiles: the same with hq and kAttnFwdRows.
   // Query tiles: [slot][hq][kAttnBwdRows][D].  Key tiles: [slot][hkv][dK, dV][kAttnBwdRows][D].
-  // fp32 key tiles: [item][hkv][part][dK, dV][kAttnF32Rows][D].
+  // fp32 key tiles (cut ones): [item][hkv][part][dK, dV][kAttnF32Rows][D].
   float* part_o;
   float* part_ml;
   // A join's first part (forward tiles, dQ): its sums, items and workgroups; the rest is as above.

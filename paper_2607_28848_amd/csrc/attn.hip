@@ -967,13 +967,21 @@ struct Workspace {
 };
 
 // fp32 key tiles of short batches are fewer than the CUs: the query heads of a key head are then divided among so many
-// workgroups; with a window, whose sinks' tile has every query of its sequence, all of a tile's steps among four (three
+// workgroups; with a window, whose sinks' tile has every query of its sequence, the steps of f32_cut tiles among four (three
 // samples of 357 rows, 8 heads on 2 of 64, window 101, forward and backward: 71 us in one part, 50 in two, 39 in four, 43 in
 // six; three of 403, 8 on 2 of 128, window 23: 155, 89, 63, 74).
 int f32_parts(const dsv_attn_plan& p) {
   if (p.windowed) return 4;
   const int64_t tiles = std::max<int64_t>(1, (int64_t)p.n_f32_dk * p.hkv);
   return (int)std::min<int64_t>(p.hq / p.hkv, (kAttnDkSlots + tiles - 1) / tiles);
+}
+// The tiles that are: all where they are fewer than the CUs, else with a window the long ones alone, since the parts' sums are
+// written and read again, 4 x 16 rows of two gradients a tile (in fp32, window 256, sinks of 4, all and the long ones: four samples
+// of 2048, 8 heads on 2 of 64, 267 us and 235; eight of 4096, 32 on 8 of 128, 11.6 ms with 1.08 GB of workspace and 9.9 with
+// 8 MB; under the limit one of 800, window 500, 8 on 2 of 64, 46 and 112).
+int f32_cut(const dsv_attn_plan& p) {
+  if (!p.windowed) return f32_parts(p) > 1 ? p.n_f32_dk : 0;
+  return (int64_t)p.n_f32_dk * p.hkv < kAttnDkSlots ? p.n_f32_dk : p.f32_dk_long;
 }
 
 Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
@@ -996,10 +1004,8 @@ Workspace carve(const dsv_attn_plan& p, dsv_dtype dt) {
   w.delta = room((size_t)p.train_q * p.hq);
   w.lse2 = room(bf ? (size_t)p.train_q * p.hq : 0);
   w.dq = room(bf ? (size_t)p.dq_slots * p.hq * kAttnBwdRows * p.d : 0);
-  const int parts = f32_parts(p);
-  w.dk = room(bf          ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d
-              : parts > 1 ? (size_t)p.n_f32_dk * p.hkv * parts * 2 * kAttnF32Rows * p.d
-                          : 0);
+  w.dk = room(bf ? (size_t)p.dk_slots * p.hkv * 2 * kAttnBwdRows * p.d
+                 : (size_t)f32_cut(p) * p.hkv * f32_parts(p) * 2 * kAttnF32Rows * p.d);
   w.total = std::max<size_t>(256, std::max(at, fwd));
   return w;
 }
@@ -1133,6 +1139,7 @@ extern "C" int dsv_attn_bwd(const dsv_attn_plan* p, dsv_dtype dt, double scale, 
     a.items = p->dptr(p->lay.f32_dk_items);
     a.n_items = p->n_f32_dk;
     a.parts = f32_parts(*p);
+    a.cut = f32_cut(*p);
     return status(launch_attn_f32_grad(a, p->dptr(p->lay.f32_dq_items), p->n_f32_dq, s));
   }
   if (dt == DSV_F32) {

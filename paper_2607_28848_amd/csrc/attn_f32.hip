@@ -260,10 +260,13 @@ __global__ __launch_bounds__(256) void attn_f32_dq_kernel(AttnArgs a) {
 // dK and dV of 16 keys of one key head over the queries that see the first of them, of all the key head's query
 // heads (so the sums over them need no atomics), or of one of a.parts ranges of them, whose sums go to the workspace
 // (32 us whole, 10.3 and 4.0 for the join in four parts: the first batch above).
-// WIN: in one launch with dq_tile, so delta is formed here as it is there; the parts are ranges of all the tile's steps.
+// WIN: in one launch with dq_tile, so delta is formed here as it is there; the parts are ranges of all the tile's steps, and
+// the tiles behind the first a.cut are whole.
 template <int D, bool WIN, int NW>
 __device__ __forceinline__ void dk_tile(const AttnArgs& a, int block, float* red) {
-  const int part = block % a.parts, tile = block / a.parts, item = tile / a.hkv, g = tile % a.hkv;
+  const int whole = WIN ? block - a.cut * a.hkv * a.parts : -1, parts = whole < 0 ? a.parts : 1;
+  const int part = whole < 0 ? block % parts : 0, tile = whole < 0 ? block / parts : a.cut * a.hkv + whole;
+  const int item = tile / a.hkv, g = tile % a.hkv;
   const Seq s(a, a.items[2 * item]);
   const int k0 = a.items[2 * item + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15;
@@ -279,7 +282,7 @@ __device__ __forceinline__ void dk_tile(const AttnArgs& a, int block, float* red
   const int q_end = WIN && k0 >= a.sinks ? (int)min((int64_t)s.ql, (int64_t)min(k0 + 16, s.kl) - 1 - off + a.window) : s.ql;
   const int per_head = q_first < q_end ? (q_end - q_first + 15) / 16 : 0;
   const int64_t all = WIN ? (int64_t)per_head * a.group : a.group;
-  const int step = WIN ? 1 : per_head, n0 = (int)(part * all / a.parts) * step, n1 = (int)((part + 1) * all / a.parts) * step;
+  const int step = WIN ? 1 : per_head, n0 = (int)(part * all / parts) * step, n1 = (int)((part + 1) * all / parts) * step;
   for (int n = n0 + wave; n < n1; n += NW) {
     const int h = g * a.group + n / per_head, qt = q_first + n % per_head * 16;
     float qv[D / 4], ov[D / 4], qc[4][D / 16], oc[4][D / 16], lse[4], delta[4];
@@ -329,7 +332,7 @@ __device__ __forceinline__ void dk_tile(const AttnArgs& a, int block, float* red
     for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * NW) {
       const int r = i / (D / 4), c = 4 * (i % (D / 4));
       const f32x4 x = gather<D, NW>(red, r, c);
-      if (a.parts > 1)
+      if (parts > 1)
         *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)block * 2 + half) * 16 + r) * D + c) = x;
       else if (k0 + r < s.kl)
         *reinterpret_cast<f32x4*>(static_cast<float*>(t.ptr) + ((int64_t)s.ck + k0 + r) * t.row + g * t.head + c) = x;
@@ -415,15 +418,15 @@ hipError_t launch_attn_f32_dk(const AttnArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_attn_f32_grad(AttnArgs a, const int32_t* dq_items, int32_t n_dq, hipStream_t s) {
-  const int64_t tiles = a.n_items * (int64_t)a.hkv;
-  a.first_groups = (int32_t)(tiles * a.parts);
+  const int64_t cut = a.cut * (int64_t)a.hkv;
+  a.first_groups = (int32_t)(cut * a.parts + (a.n_items - a.cut) * (int64_t)a.hkv);
   a.first_join = dq_items;
   a.delta = nullptr;
   const dim3 grid((unsigned)(a.first_groups + (int64_t)n_dq * a.hq));
   if (grid.x == 0) return hipSuccess;
   if (a.d == 64) hipLaunchKernelGGL(attn_f32_grad_kernel<64>, grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL(attn_f32_grad_kernel<128>, grid, dim3(256), 0, s, a);
-  return join_parts(a, tiles, s);
+  return join_parts(a, cut, s);
 }
 
 }  // namespace dsv

@@ -311,6 +311,9 @@ int build(const dsv_attn_seq* seqs, int32_t n, int32_t n_q, int32_t n_kv, int32_
   p.n_dk = ck.n_items, p.n_dk_join = ck.n_join, p.dk_slots = ck.n_slots;
   const std::vector<int32_t> w3 = f32.words(), w3q = f32_dq.words(),
                              w3k = f32_dk.words();
+  const auto& kt = f32_dk.t;  // sorted by now, and work is -first
+  const size_t some = std::partition_point(kt.begin(), kt.end(), [](const auto& e) { return e.first < 0; }) - kt.begin();
+  for (size_t i = 0; i < some; ++i) p.f32_dk_long += kt[i].first < 2 * kt[some / 2].first;
   int64_t most = std::max({p.n_fwd, p.n_dk, p.n_dq});
   most = std::max(most, count(w3, 2, &p.n_f32));
   most = std::max(most, count(split_items, kAttnSplitWords, &p.n_split));

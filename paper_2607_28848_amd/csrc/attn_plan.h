@@ -88,6 +88,7 @@ struct dsv_attn_plan {
   int32_t n_fwd = 0, n_fwd_join = 0, fwd_slots = 0, n_dk_join = 0, dk_slots = 0;  // *_slots: pieces with sums of their own
   int32_t n_dq_join = 0, dq_slots = 0;
   int32_t n_f32 = 0, n_split = 0, n_join = 0, n_dq = 0, n_dk = 0, n_f32_dq = 0, n_f32_dk = 0;
+  int32_t f32_dk_long = 0;    // of the fp32 key tiles the first ones, with more than twice the usual one's queries
   std::vector<int32_t> meta;  // packed blob, host image
   dsv::AttnLayout lay{};
   void* d_meta = nullptr;     // device copy (nullptr: host-only plan)
