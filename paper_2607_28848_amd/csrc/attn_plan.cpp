@@ -9,9 +9,9 @@
 #include <algorithm>
 #include <array>
 #include <functional>
+#include <map>
 #include <new>
 #include <numeric>
-#include <queue>
 
 #include "attn_plan.h"
 
@@ -41,23 +41,27 @@ struct Cut {
 };
 
 // The time, in steps, that the tiles take in pieces of at most `piece` steps, longest first, each on the slot
-// that is free first.  join: steps that a piece's own sums cost.
+// that is free first.  join: steps that a piece's own sums cost.  Pieces of one length and slots that are free at one time
+// are taken together: the tiles behind a window are nearly all alike, and up to 16 schedules are tried (eight samples of 16384,
+// window 64, sinks: 5.9 ms a plan piece by piece, 0.94 so, 0.86 without a window).
 template <typename F>
 int64_t makespan(const std::vector<int64_t>& steps, int64_t copies, F pieces_of, int slots, int64_t join) {
-  std::vector<int64_t> len;
+  std::map<int64_t, int64_t, std::greater<int64_t>> pieces;  // length: number
   for (int64_t s : steps) {
     const int64_t n = pieces_of(s);
-    for (int64_t k = 0; k < n * copies; ++k) len.push_back((s + n - 1) / n + (n > 1 ? join : 0));
+    pieces[(s + n - 1) / n + (n > 1 ? join : 0)] += n * copies;
   }
-  std::sort(len.begin(), len.end(), std::greater<int64_t>());
-  std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> free_at;
-  for (int i = 0; i < slots; ++i) free_at.push(0);
+  std::map<int64_t, int64_t> free_at{{0, slots}};  // time: slots
   int64_t end = 0;
-  for (int64_t l : len) {
-    const int64_t t = free_at.top() + l;
-    free_at.pop();
-    free_at.push(t);
-    end = std::max(end, t);
+  for (const auto& [length, number] : pieces) {
+    for (int64_t left = number; left > 0;) {
+      const auto first = free_at.begin();
+      const int64_t n = std::min(left, first->second), t = first->first + length;
+      left -= n;
+      free_at[t] += n;
+      end = std::max(end, t);
+      if ((first->second -= n) == 0) free_at.erase(first);
+    }
   }
   return end;
 }
