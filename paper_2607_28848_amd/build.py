@@ -74,7 +74,7 @@ def build_marshal(verbose: bool = False) -> str:
     tmp = MARSHAL + ".tmp%d" % os.getpid()
     try:
         out = _run(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall",
-                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, '-DDSV_TORCH="%s"' % torch.__version__]
                    + [x for p in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]] for x in ("-isystem", p)]
                    + [os.path.join(CSRC, "marshal.cpp"), "-o", tmp] + ["-L" + p for p in cpp_extension.library_paths()]
                    + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)

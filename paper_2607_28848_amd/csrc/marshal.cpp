@@ -116,4 +116,24 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module); }
+// The module reads torch's tensors as its headers lay them out: ImportError under another torch or Python than it was built for
+// (DSV_TORCH: torch.__version__ then).
+PyMODINIT_FUNC PyInit__marshal() {
+  const std::string python = std::to_string(PY_MAJOR_VERSION) + "." + std::to_string(PY_MINOR_VERSION) + ".";
+  PyObject* torch = PyImport_ImportModule("torch");
+  PyObject* version = torch ? PyObject_GetAttrString(torch, "__version__") : nullptr;
+  PyObject* text = version ? PyObject_Str(version) : nullptr;
+  const char* found = text ? PyUnicode_AsUTF8(text) : nullptr;
+  PyObject* made = nullptr;
+  if (found) {
+    if (std::string(found) != DSV_TORCH || std::string(Py_GetVersion()).rfind(python, 0) != 0)
+      PyErr_Format(PyExc_ImportError, "_marshal.so was built for torch %s and Python %s*, this is torch %s and Python %s: build it again",
+                   DSV_TORCH, python.c_str(), found, Py_GetVersion());
+    else
+      made = PyModule_Create(&module);
+  }
+  Py_XDECREF(text);
+  Py_XDECREF(version);
+  Py_XDECREF(torch);
+  return made;
+}
