@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_distill import check, make, oracle
+from test_gpu_distill import check, make, oracle, run
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -110,3 +110,13 @@ def test_gradient_against_differences(along):
     if along:
         assert tolerance < 0.05 * abs(exact)
     assert abs(num - ana) <= tolerance
+
+
+@pytest.mark.parametrize("T,V,k", [(300, 131080, 1024), (130, 131072, 999), (257, 131072, 3), (100, 131080, 1023), (17, 131072, 1)])
+def test_entries_of_whole_tiles(T, V, k):
+    """bf16 tiles of 256 and 128 rows and 256 columns with many entries and few, at the tiles' first and last columns among them."""
+    X, W, ids, teacher, weight = make(T, 64, V, k, BF, seed=21)
+    edges = torch.tensor([0, 255, 256, V - 1, 511, 512, 65535, 65536], dtype=torch.int32)[:k].cuda()
+    ids[::3, :len(edges)] = edges
+    ids[T - 1, 0] = V - 1
+    run(X, W, ids, teacher, 1.0, weight)
