@@ -68,7 +68,7 @@ __device__ __forceinline__ void teacher_shares(const VocabArgs& a, int64_t row) 
 // P and of the sums.  The tile's rows of ids are one run of memory, four a load whatever their alignment.  The first B loads a
 // thread go out at the start, and a barrier stands between that and put(); mark is complete behind the barrier after it.  16 rows
 // of 20 entries against 128256 of 4096: 197 us a call so, 193 with the entries' terms left in the sums; 1024 of 64 and 8192, with
-// the gradient, 3.59 ms and 3.57.
+// the gradient, 3.75 ms and 3.73.
 template <int TM, int TN, int B>
 struct EntryMarks {
   struct __attribute__((packed, aligned(4))) Four {
